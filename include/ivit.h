@@ -48,7 +48,7 @@ typedef enum {
     IVIT_ERR_NULL = -1,       /* a required pointer is NULL                                  */
     IVIT_ERR_SHAPE = -2,      /* a dimension is negative, zero where not allowed, too large,
                                  or not a multiple the kernels need                          */
-    IVIT_ERR_PARAM = -3,      /* an integer parameter is outside its stated range            */
+    IVIT_ERR_PARAM = -3,      /* a parameter is outside its stated range                     */
     IVIT_ERR_ALIGN = -4,      /* a pointer is not aligned as stated                          */
     IVIT_ERR_WORKSPACE = -5,  /* workspace is NULL or smaller than ivit_workspace_bytes()    */
     IVIT_ERR_HIP = -6         /* the HIP runtime reported an error at launch                 */
@@ -291,7 +291,7 @@ int ivit_window_attention_ex(void* stream, const int8_t* qkv, const int8_t* rel_
  * `capacity` entries) with, per launch in launch order: elapsed milliseconds, kind (1 I-LayerNorm, 2 Dense,
  * 3 Dense + residual, 4 Dense + ShiftGELU, 5 attention, 6 Shiftmax, 7 ShiftGELU, 8 token assembly, 9 patch-merging
  * gather, 10 mean pooling, 11 the token-wise layers of a block in one kernel, 12 the constants of such
- * launches prepared), algorithmic integer operations (2 per int8 multiply-accumulate; 0 for row-wise kernels)
+ * launches prepared, 13 root-mean-square norm, 14 Dense with real scales, 15 gated activation to int8), algorithmic integer operations (2 per int8 multiply-accumulate; 0 for row-wise kernels)
  * and algorithmic HBM bytes (each operand read once, each result written once); *count receives the number of
  * launches seen.
  * One trace at a time per process, not thread-safe; launches beyond max_launches make ivit_trace_end
@@ -405,6 +405,65 @@ size_t ivit_swin_workspace_bytes(const ivit_swin_params* p, int32_t B);
  * without tok_index. */
 int ivit_forward_swin(void* stream, const int8_t* patches, int8_t* logits, const ivit_swin_params* p, int32_t B,
                       void* workspace, size_t workspace_bytes);
+
+/* ---- Float layers around int8 products: scales taken at run time. ----------------------------------------------
+ * The layers above requantise by dyadic numbers fixed beforehand.  The three below are for models whose activations
+ * are quantised per token as they come, with the residual stream in floating point: int8 rows with one real scale
+ * each, int8 x int8 -> int32 products as everywhere in this library, and an epilogue in 32-bit floating point.  One
+ * encoder block is  rmsnorm_quant -> linear_scaled -> attention -> linear_scaled (+ residual) -> rmsnorm_quant ->
+ * linear_scaled -> gated_quant -> linear_scaled (+ residual);  linear_scaled with an int8 result at a fixed step gives
+ * the packed qkv tensor of ivit_attention, and one x_scale for all rows takes its output.
+ *
+ *  - Elements are float32, float16 or bfloat16 (ivit_type); scales, gamma and bias are float32.  Leading dimensions
+ *    (ld...) count elements between rows, at least the row's length and at most 2^31 - 1.  Float tensors need the
+ *    alignment of one element only.
+ *  - Sums, norms and the epilogue are held in 32 bits; int8 products are summed exactly.  A value is rounded once,
+ *    where it is stored, to nearest, ties to even.  A float result beyond the range of its type becomes infinite.
+ *  - An int8 row q with scale s stands for s q.  s = max |v| / 127 and q = round(v / s) over the row's values v; a row of
+ *    zeros has s = 0 and zeros, a row that holds a NaN or an infinite value (or whose largest leaves the range of
+ *    float32) has s = NaN and zeros.
+ *  - Results do not depend on the grid or the order in which anything ran: equal calls give equal bits. */
+typedef enum { IVIT_F32 = 0, IVIT_F16 = 1, IVIT_BF16 = 2, IVIT_I8 = 3 } ivit_type;
+
+/* Activations: x, max(x, 0), x sigma(x), x Phi(x), the tanh form of the former
+ * x (1 + tanh(sqrt(2 / pi) (x + 0.044715 x^3))) / 2, and x sigma(1.702 x), the function that ShiftGELU approximates
+ * (Sec. 3.4, Eq. 17). */
+typedef enum { IVIT_ACT_NONE = 0, IVIT_ACT_RELU = 1, IVIT_ACT_SILU = 2, IVIT_ACT_GELU = 3, IVIT_ACT_GELU_TANH = 4,
+               IVIT_ACT_GELU_SIGMOID = 5 } ivit_activation;
+
+/* Root-mean-square norm with the residual's addition:
+ *   h = x + residual;   sum = h;   n = h / sqrt(mean(h^2) + eps) * gamma
+ * x, residual (nullable), sum (nullable) [rows, C] of `type`; gamma float32 [C], nullable (ones).  n is formed from h
+ * before its rounding to `type`.  Result: y_scale != NULL: int8 rows y [rows, C] and their scales y_scale [rows]; y_scale
+ * == NULL: n itself, of `type`.  A mean square beyond the range of float32 counts as infinite (n = 0 where h is finite).
+ * sum may be x or residual themselves, and so may a y of `type` (the same pointer and leading dimension); no other overlap.
+ * Requirements: 0 <= rows < 2^31, 1 <= C <= 32768, eps > 0 and finite.
+ * Errors: NULL, SHAPE, PARAM (type, eps), ALIGN, HIP. */
+int ivit_rmsnorm_quant(void* stream, const void* x, int64_t ldx, const void* residual, int64_t ld_residual,
+                       const float* gamma, float eps, void* sum, int64_t ld_sum, void* y, int64_t ldy, float* y_scale,
+                       int64_t rows, int32_t C, int32_t type);
+
+/* Dense with scales, bias, activation and residual:
+ *   y[m][n] = act(x_scale[m] * w_scale[n] * sum_k x[m][k] w[n][k] + bias[n]) + residual[m][n]
+ * x int8 [M, K] (ldx elements between rows, a multiple of 16, at most 2^22), w int8 [N, K] dense; the full range of int8,
+ * -128 included.  x_scale float32 [M], or one value for all rows if one_scale != 0; w_scale float32 [N]; bias float32 [N]
+ * or NULL.  y [M, N] of y_type; residual [M, N] of y_type or NULL.  y_type == IVIT_I8: y = clamp8(round(act(..) / y_step)),
+ * without a residual (y_step is ignored otherwise; a NaN gives 0).  residual may be y itself (same pointer and leading
+ * dimension); no other overlap.
+ * Requirements: 0 <= M < 2^31, N >= 1, 16 <= K <= 65536, K % 16 == 0; x and w 16-byte aligned; y_step a normal number whose
+ * reciprocal is one too.
+ * Errors: NULL, SHAPE, PARAM (act, y_type, y_step, a residual with IVIT_I8), ALIGN, HIP. */
+int ivit_linear_scaled(void* stream, const int8_t* x, int64_t ldx, const float* x_scale, int32_t one_scale,
+                       const int8_t* w, const float* w_scale, const float* bias, int32_t act, const void* residual,
+                       int64_t ld_residual, void* y, int64_t ldy, int32_t y_type, float y_step, int64_t M, int32_t N,
+                       int32_t K);
+
+/* The hidden rows of an MLP to int8: v = act(x[:, 0 .. C)) * x[:, C .. 2 C) if gated != 0 (the gate's channels first), else
+ * v = act(x[:, 0 .. C)); act may be IVIT_ACT_NONE (with gated == 0: any rows to int8).  x of `type`, rows of 2 C or C elements;
+ * y int8 [rows, C] and y_scale float32 [rows], which may not overlap x.
+ * Requirements: 0 <= rows < 2^31, 1 <= C <= 32768.  Errors: NULL, SHAPE, PARAM (type, act), ALIGN, HIP. */
+int ivit_gated_quant(void* stream, const void* x, int64_t ldx, int8_t* y, int64_t ldy, float* y_scale, int64_t rows,
+                     int32_t C, int32_t type, int32_t act, int32_t gated);
 
 /* ---- Host helpers: the floating-point side of a quantised model -> the integers this library takes. --------
  * Pure host code on HOST pointers; nothing is launched.  They realise Sec. 3.1 Eq. 6 (symmetric uniform

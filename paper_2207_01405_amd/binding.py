@@ -22,11 +22,12 @@ EXPORTS = ("ivit_strerror", "ivit_build_id", "ivit_linear_requant", "ivit_shiftm
            "ivit_forward_image", "ivit_attention_masked", "ivit_window_attention", "ivit_window_attention_ex", "ivit_patch_merge_gather",
            "ivit_mean_pool", "ivit_swin_window_index", "ivit_swin_shift_mask", "ivit_swin_workspace_bytes",
            "ivit_forward_swin", "ivit_shiftgelu_rowmax", "ivit_encoder_block_static", "ivit_linear_requant_ex",
-           "ivit_last_hip_error", "ivit_probe_mfma_rate", "ivit_ilayernorm_limits")
+           "ivit_last_hip_error", "ivit_probe_mfma_rate", "ivit_ilayernorm_limits", "ivit_rmsnorm_quant",
+           "ivit_linear_scaled", "ivit_gated_quant")
 
 KIND_NAMES = {1: "ilayernorm", 2: "gemm", 3: "gemm_residual", 4: "gemm_gelu", 5: "attention", 6: "shiftmax",
               7: "shiftgelu", 8: "embed_tokens", 9: "patch_merge_gather", 10: "mean_pool",
-              11: "gemm_token_block", 12: "gemm_token_tables"}
+              11: "gemm_token_block", 12: "gemm_token_tables", 13: "rmsnorm", 14: "gemm_scaled", 15: "gated"}
 
 
 class ShiftParams(C.Structure):
@@ -180,6 +181,13 @@ def load():
     lib.ivit_dyadic_from_float.argtypes = [C.c_double, i32, C.POINTER(Dyadic)]
     lib.ivit_shift_params_from_scale.restype = C.c_int
     lib.ivit_shift_params_from_scale.argtypes = [C.c_double, i32, i32, i32, C.POINTER(ShiftParams)]
+    f32 = C.c_float
+    lib.ivit_rmsnorm_quant.restype = C.c_int
+    lib.ivit_rmsnorm_quant.argtypes = [_P, _P, i64, _P, i64, _P, f32, _P, i64, _P, i64, _P, i64, i32, i32]
+    lib.ivit_linear_scaled.restype = C.c_int
+    lib.ivit_linear_scaled.argtypes = [_P, _P, i64, _P, i32, _P, _P, _P, i32, _P, i64, _P, i64, i32, f32, i64, i32, i32]
+    lib.ivit_gated_quant.restype = C.c_int
+    lib.ivit_gated_quant.argtypes = [_P, _P, i64, _P, i64, _P, i64, i32, i32, i32, i32]
     lib.ivit_trace_begin.restype = C.c_int; lib.ivit_trace_begin.argtypes = [i32]
     lib.ivit_trace_end.restype = C.c_int
     lib.ivit_trace_end.argtypes = [C.POINTER(C.c_float), C.POINTER(i32), C.POINTER(i64), C.POINTER(i64), i32,
@@ -564,3 +572,108 @@ def ivit_forward_swin(patches, logits, params, B, workspace, stream=None):
                                   workspace.numel() * workspace.element_size())
     _check(st, "ivit_forward_swin")
     return logits
+
+
+# ------------------------------------------------------------------ float layers around int8 products
+ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3, "gelu_tanh": 4, "gelu_sigmoid": 5}
+_TYPES = None           # torch dtype -> ivit_type (torch is imported by the first call)
+
+
+def _type(t, where):
+    global _TYPES
+    if _TYPES is None:
+        import torch
+        _TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2, torch.int8: 3}
+    k = _TYPES.get(t.dtype)
+    if k is None:
+        raise ValueError("%s: no tensors of %s" % (where, t.dtype))
+    return k
+
+
+def _rows(t, rows, cols, kind, device, where):
+    """Leading dimension of a two-dimensional tensor of the expected shape and type whose rows are dense."""
+    s = t.stride()
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols or (s[1] != 1 and cols > 1):
+        raise ValueError("%s: a tensor of %s with strides %s, wanted [%d, %d] with dense rows" % (where, tuple(t.shape), s, rows, cols))
+    if _type(t, where) != kind or t.get_device() != device:
+        raise ValueError("%s: a tensor of %s on %s, wanted ivit_type %d on device %d" % (where, t.dtype, t.device, kind, device))
+    return s[0] if rows > 1 else cols
+
+
+def _vector(t, n, device, where):
+    """Pointer of a dense float32 vector of n values (None: NULL)."""
+    if t is None:
+        return None
+    if t.numel() != n or not t.is_contiguous() or _type(t, where) != 0 or t.get_device() != device:
+        raise ValueError("%s: wanted %d dense float32 values on device %d, got %s of %s on %s" % (where, n, device, tuple(t.shape), t.dtype, t.device))
+    return t.data_ptr()
+
+
+def _launch_stream(stream, device, where):
+    """The stream of a call on tensors of this device, which has to be the current one (a kernel is launched there)."""
+    if device < 0:
+        raise ValueError("%s: tensors have to be on a GPU" % where)
+    import torch
+    if torch.cuda.current_device() != device:
+        raise ValueError("%s: tensors on device %d, but device %d is the current one" % (where, device, torch.cuda.current_device()))
+    if stream is None:
+        return torch.cuda.current_stream().cuda_stream
+    if not isinstance(stream, int) and stream.device_index != device:
+        raise ValueError("%s: tensors on device %d, a stream of device %d" % (where, device, stream.device_index))
+    return _stream(stream)
+
+
+def _activation(act, where):
+    k = ACTIVATIONS.get(act)
+    if k is None:
+        raise ValueError("%s: activation %r (one of %s)" % (where, act, ", ".join(ACTIVATIONS)))
+    return k
+
+
+def ivit_rmsnorm_quant(x, gamma, y, y_scale, eps, residual=None, sum_out=None, stream=None):
+    """x, residual, sum_out: [rows, C] float tensors of one type; gamma: float32 [C] or None; y: int8 with y_scale float32
+    [rows], or of x's type with y_scale None.  Returns y."""
+    where = "ivit_rmsnorm_quant"
+    rows, Cc = x.shape
+    kind, dev = _type(x, where), x.get_device()
+    st = load().ivit_rmsnorm_quant(
+        _launch_stream(stream, dev, where), x.data_ptr(), _rows(x, rows, Cc, kind, dev, where),
+        _ptr(residual), 0 if residual is None else _rows(residual, rows, Cc, kind, dev, where), _vector(gamma, Cc, dev, where), eps,
+        _ptr(sum_out), 0 if sum_out is None else _rows(sum_out, rows, Cc, kind, dev, where),
+        y.data_ptr(), _rows(y, rows, Cc, kind if y_scale is None else 3, dev, where), _vector(y_scale, rows, dev, where), rows, Cc, kind)
+    _check(st, where)
+    return y
+
+
+def ivit_linear_scaled(x, x_scale, w, w_scale, y, bias=None, act="none", residual=None, y_step=None, stream=None):
+    """x: int8 [M, K]; x_scale: float32, M values or one; w: dense int8 [N, K]; w_scale, bias: float32 [N]; y: [M, N] float32, float16
+    or bfloat16, with a residual of the same type or None, or int8 with y_step.  Returns y."""
+    where = "ivit_linear_scaled"
+    M, K = x.shape
+    N, dev = w.shape[0], x.get_device()
+    kind, ns = _type(y, where), x_scale.numel()
+    ldw = _rows(w, N, K, 3, dev, where)
+    if ldw != K:
+        raise ValueError("%s: the weights have to be dense" % where)
+    if kind == 3 and y_step is None:
+        raise ValueError("%s: an int8 result needs y_step" % where)
+    one = ns == 1 and M != 1
+    st = load().ivit_linear_scaled(
+        _launch_stream(stream, dev, where), x.data_ptr(), _rows(x, M, K, 3, dev, where), _vector(x_scale, 1 if one else M, dev, where), one,
+        w.data_ptr(), _vector(w_scale, N, dev, where), _vector(bias, N, dev, where), _activation(act, where), _ptr(residual),
+        0 if residual is None else _rows(residual, M, N, kind, dev, where), y.data_ptr(), _rows(y, M, N, kind, dev, where), kind,
+        0.0 if y_step is None else y_step, M, N, K)
+    _check(st, where)
+    return y
+
+
+def ivit_gated_quant(x, y, y_scale, act="silu", gated=True, stream=None):
+    """x: [rows, 2 C] (gated: the gate's channels first) or [rows, C] float; y: int8 [rows, C]; y_scale: float32 [rows].  Returns y."""
+    where = "ivit_gated_quant"
+    rows, Cc = y.shape
+    kind, dev = _type(x, where), x.get_device()
+    st = load().ivit_gated_quant(
+        _launch_stream(stream, dev, where), x.data_ptr(), _rows(x, rows, 2 * Cc if gated else Cc, kind, dev, where),
+        y.data_ptr(), _rows(y, rows, Cc, 3, dev, where), _vector(y_scale, rows, dev, where), rows, Cc, kind, _activation(act, where), bool(gated))
+    _check(st, where)
+    return y

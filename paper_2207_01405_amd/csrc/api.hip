@@ -3,6 +3,7 @@
 #include "../../include/ivit.h"
 
 #include <algorithm>
+#include <cmath>
 #include <cstdio>
 #include <cstdlib>
 #include <mutex>
@@ -270,7 +271,7 @@ const char* ivit_strerror(int status) {
         case IVIT_OK: return "ok";
         case IVIT_ERR_NULL: return "a required pointer is NULL";
         case IVIT_ERR_SHAPE: return "unsupported shape";
-        case IVIT_ERR_PARAM: return "integer parameter out of range";
+        case IVIT_ERR_PARAM: return "parameter out of range";
         case IVIT_ERR_ALIGN: return "pointer not aligned as required";
         case IVIT_ERR_WORKSPACE: return "workspace missing or too small";
         case IVIT_ERR_HIP: return "HIP runtime error at launch";
@@ -693,6 +694,64 @@ int ivit_forward_swin(void* stream, const int8_t* patches, int8_t* logits, const
     if ((st = ivit_mean_pool(stream, buf[cur ^ 1], pooled, B, gl * gl, Cl, p->pool_rq)) != IVIT_OK) return st;
     return ivit_linear_requant(stream, pooled, p->w_head, p->bias_head, p->head_rq_b, p->head_rq_c, nullptr, one, nullptr,
                                one, logits, B, p->n_classes, Cl);
+}
+
+// ---- Float layers around int8 products
+
+static int check_rows(const void* p, int64_t ld, int64_t cols, int type) {
+    if (ld < cols || ld > 0x7fffffffLL) return IVIT_ERR_SHAPE;
+    return aligned(p, (size_t)ivit::element_bytes(type)) ? IVIT_OK : IVIT_ERR_ALIGN;
+}
+
+int ivit_rmsnorm_quant(void* stream, const void* x, int64_t ldx, const void* residual, int64_t ld_residual, const float* gamma,
+                       float eps, void* sum, int64_t ld_sum, void* y, int64_t ldy, float* y_scale, int64_t rows, int32_t C,
+                       int32_t type) {
+    if (type != IVIT_F32 && type != IVIT_F16 && type != IVIT_BF16) return IVIT_ERR_PARAM;
+    if (rows < 0 || rows > 0x7fffffffLL || C < 1 || C > 32768) return IVIT_ERR_SHAPE;
+    if (!(eps > 0.0f) || !std::isfinite(eps)) return IVIT_ERR_PARAM;
+    if (rows == 0) return IVIT_OK;
+    if (!x || !y) return IVIT_ERR_NULL;
+    int st;
+    if ((st = check_rows(x, ldx, C, type)) != IVIT_OK || (st = check_rows(y, ldy, C, y_scale ? IVIT_I8 : type)) != IVIT_OK) return st;
+    if (residual && (st = check_rows(residual, ld_residual, C, type)) != IVIT_OK) return st;
+    if (sum && (st = check_rows(sum, ld_sum, C, type)) != IVIT_OK) return st;
+    if (!aligned(gamma, 4) || !aligned(y_scale, 4)) return IVIT_ERR_ALIGN;
+    const ivit::RmsNormArgs a{x, residual, gamma, sum, y, y_scale, ldx, ld_residual, ld_sum, ldy, rows, C, type, eps};
+    return hip_status(ivit::launch_rmsnorm(static_cast<hipStream_t>(stream), a));
+}
+
+int ivit_linear_scaled(void* stream, const int8_t* x, int64_t ldx, const float* x_scale, int32_t one_scale, const int8_t* w,
+                       const float* w_scale, const float* bias, int32_t act, const void* residual, int64_t ld_residual, void* y,
+                       int64_t ldy, int32_t y_type, float y_step, int64_t M, int32_t N, int32_t K) {
+    if (act < IVIT_ACT_NONE || act > IVIT_ACT_GELU_SIGMOID || y_type < IVIT_F32 || y_type > IVIT_I8) return IVIT_ERR_PARAM;
+    if (y_type == IVIT_I8 && (residual || !std::isnormal(y_step) || !(y_step > 0.0f) || !std::isnormal(1.0f / y_step))) return IVIT_ERR_PARAM;
+    if (M < 0 || M > 0x7fffffffLL || N < 1 || K < 16 || K > 65536 || (K & 15)) return IVIT_ERR_SHAPE;
+    if ((M + 31) / 32 * (((int64_t)N + 31) / 32) > 0x7fffffffLL) return IVIT_ERR_SHAPE;       // (tiles are counted in 32 bits)
+    if (!w || !w_scale) return IVIT_ERR_NULL;
+    if (M > 0 && (!x || !x_scale || !y)) return IVIT_ERR_NULL;             // an empty tensor may have no storage
+    if (!aligned(w, 16) || !aligned(w_scale, 4) || !aligned(bias, 4)) return IVIT_ERR_ALIGN;
+    if (M == 0) return IVIT_OK;
+    if (ldx < K || ldx > (1 << 22) || (ldx & 15)) return IVIT_ERR_SHAPE;
+    if (!aligned(x, 16) || !aligned(x_scale, 4)) return IVIT_ERR_ALIGN;
+    int st;
+    if ((st = check_rows(y, ldy, N, y_type)) != IVIT_OK) return st;
+    if (residual && (st = check_rows(residual, ld_residual, N, y_type)) != IVIT_OK) return st;
+    const ivit::ScaledArgs a{x, x_scale, w, w_scale, bias, residual, y, ldx, ld_residual, ldy, M, N, K, act, y_type, one_scale != 0, y_step};
+    return hip_status(ivit::launch_linear_scaled(static_cast<hipStream_t>(stream), a));
+}
+
+int ivit_gated_quant(void* stream, const void* x, int64_t ldx, int8_t* y, int64_t ldy, float* y_scale, int64_t rows, int32_t C,
+                     int32_t type, int32_t act, int32_t gated) {
+    if (type != IVIT_F32 && type != IVIT_F16 && type != IVIT_BF16) return IVIT_ERR_PARAM;
+    if (act < IVIT_ACT_NONE || act > IVIT_ACT_GELU_SIGMOID) return IVIT_ERR_PARAM;
+    if (rows < 0 || rows > 0x7fffffffLL || C < 1 || C > 32768) return IVIT_ERR_SHAPE;
+    if (rows == 0) return IVIT_OK;
+    if (!x || !y || !y_scale) return IVIT_ERR_NULL;
+    int st;
+    if ((st = check_rows(x, ldx, gated ? 2 * C : C, type)) != IVIT_OK || (st = check_rows(y, ldy, C, IVIT_I8)) != IVIT_OK) return st;
+    if (!aligned(y_scale, 4)) return IVIT_ERR_ALIGN;
+    const ivit::GatedArgs a{x, y, y_scale, ldx, ldy, rows, C, type, act, gated != 0};
+    return hip_status(ivit::launch_gated(static_cast<hipStream_t>(stream), a));
 }
 
 }  // extern "C"

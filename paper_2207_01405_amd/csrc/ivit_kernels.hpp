@@ -95,13 +95,31 @@ struct AttentionArgs {
 };
 hipError_t launch_attention(hipStream_t s, const AttentionArgs& a);
 
+// Operators around int8 Dense layers whose scales are real numbers taken at run time (rows_scaled.hip, gemm_scaled.hip).
+// Types and activations: the values of ivit_type and ivit_activation of the C header.  Leading dimensions count elements.
+enum { TYPE_F32 = 0, TYPE_F16 = 1, TYPE_BF16 = 2, TYPE_I8 = 3 };
+enum { ACT_NONE = 0, ACT_RELU = 1, ACT_SILU = 2, ACT_GELU = 3, ACT_GELU_TANH = 4, ACT_GELU_SIGMOID = 5 };
+constexpr int64_t element_bytes(int type) { return type == TYPE_F32 ? 4 : type == TYPE_I8 ? 1 : 2; }
+struct RmsNormArgs {
+    const void* x; const void* residual; const float* gamma; void* sum; void* y; float* y_scale;    // y_scale: y is int8; nullptr: of `type`
+    int64_t ldx, ld_res, ld_sum, ldy, rows; int C, type; float eps;
+};
+hipError_t launch_rmsnorm(hipStream_t s, const RmsNormArgs& a);
+struct GatedArgs { const void* x; int8_t* y; float* y_scale; int64_t ldx, ldy, rows; int C, type, act; bool gated; };
+hipError_t launch_gated(hipStream_t s, const GatedArgs& a);
+struct ScaledArgs {
+    const int8_t* x; const float* x_scale; const int8_t* w; const float* w_scale; const float* bias; const void* residual; void* y;
+    int64_t ldx, ld_res, ldy, M; int N, K, act, y_type; bool one_scale; float y_step;
+};
+hipError_t launch_linear_scaled(hipStream_t s, const ScaledArgs& a);
+
 // Number of compute units of the current device (cached); used to size persistent grids.
 int num_cus();
 
 // Kinds of launches reported by the trace (ivit_trace_end); values are part of the C ABI.
 enum LaunchKind { KIND_ILAYERNORM = 1, KIND_GEMM = 2, KIND_GEMM_RESIDUAL = 3, KIND_GEMM_GELU = 4,
                   KIND_ATTENTION = 5, KIND_SHIFTMAX = 6, KIND_SHIFTGELU = 7, KIND_EMBED = 8, KIND_PATCH_MERGE = 9, KIND_MEAN_POOL = 10,
-                  KIND_TOKEN_BLOCK = 11, KIND_TOKEN_TABLES = 12 };
+                  KIND_TOKEN_BLOCK = 11, KIND_TOKEN_TABLES = 12, KIND_RMSNORM = 13, KIND_GEMM_SCALED = 14, KIND_GATED = 15 };
 
 // Brackets one kernel launch with two HIP events on its stream while a trace is active; otherwise a no-op.
 // ops = algorithmic integer operations (2 per int8 multiply-accumulate), bytes = algorithmic HBM bytes.

@@ -1,0 +1,256 @@
+// Rows that leave as int8 values with a scale each: the root-mean-square norm with the residual's addition in front, and the
+// (gated) activation of an MLP's hidden rows.
+//
+//   norm:  h = x + r,  n = h / sqrt(mean(h^2) + eps) gamma        gate:  v = act(g) u  or  act(g)
+//   s = max |v| / 127,  q = round(v / s)
+//
+// Both are bound by memory: an element is 10 to 20 operations for 3 to 7 bytes.  A group of TPR threads holds a row in
+// registers, NV pieces of eight elements a thread, so that x is read once; one reduction over the group gives the norm its sum of
+// squares and its largest |h gamma| together: the factor 1 / sqrt(..) is the same for a row's elements, so q needs h gamma only
+// and s takes the factor once.
+#include "scaled_common.hpp"
+
+namespace ivit {
+namespace {
+
+using namespace scaled;
+
+constexpr uint32_t kInf = 0x7f800000u;         // the bits of |v|, as unsigned numbers, are in the order of |v|; NaN comes last
+
+// What a row's int8 form needs: the factors of v, and the scale of a row whose v still lack `factor`.  A row of zeros (or whose
+// factor leaves nothing of it) has the scale 0; a row with a NaN or an infinite value NaN, and zeros.
+struct Quant { float up, inv, scale; };
+__device__ __forceinline__ Quant quant_of(uint32_t top_bits, float factor) {
+    const float top = __uint_as_float(top_bits);
+    if (top_bits >= kInf) return Quant{0.0f, 0.0f, __uint_as_float(0x7fc00000u)};
+    const float scale = top * factor / 127.0f, up = top < 0x1p-90f ? 0x1p64f : 1.0f;      // (127 / top has to be finite)
+    if (scale == 0.0f) return Quant{0.0f, 0.0f, 0.0f};
+    return Quant{up, 127.0f / (top * up), scale};
+}
+
+template <int TPR, int BLOCK> struct Group {
+    static constexpr int ROWS = BLOCK / TPR, WAVES = TPR > 64 ? TPR / 64 : 1;
+    // the sum and the largest of the bits over the threads of a row, every one of them getting both
+    static __device__ __forceinline__ void reduce(float& sum, uint32_t& top) {
+#pragma unroll
+        for (int m = (TPR < 64 ? TPR : 64) / 2; m > 0; m >>= 1) {
+            sum += __shfl_xor(sum, m);
+            top = max(top, (uint32_t)__shfl_xor((int)top, m));
+        }
+        if constexpr (TPR > 64) {
+            static_assert(TPR == BLOCK, "a row of several wavefronts is the workgroup's");
+            __shared__ float s[WAVES];
+            __shared__ uint32_t t[WAVES];
+            if ((threadIdx.x & 63) == 0) { s[threadIdx.x >> 6] = sum; t[threadIdx.x >> 6] = top; }
+            __syncthreads();
+            sum = 0.0f; top = 0;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) { sum += s[w]; top = max(top, t[w]); }
+        }
+    }
+};
+
+__device__ __forceinline__ void store_q(int8_t* p, const v8f& v, const Quant& q, int n) {
+    uint32_t w[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[e] = q.inv == 0.0f ? 0u : round_bits(v[e] * q.up, q.inv);
+    typedef uint32_t v2u __attribute__((ext_vector_type(2), aligned(1)));
+    const v2u out = {pack4(w[0], w[1], w[2], w[3]), pack4(w[4], w[5], w[6], w[7])};
+    if (n >= 8) { *reinterpret_cast<v2u*>(p) = out; return; }
+#pragma unroll
+    for (int e = 0; e < 7; ++e)
+        if (e < n) p[e] = (int8_t)(out[e >> 2] >> (8 * (e & 3)));
+}
+
+// Piece v of thread t starts at element 8 (t + TPR v).  One that would run over the end of the row starts eight elements before the
+// end instead: its first `twice` elements are also in the piece before, where they count; results that both hold are stored twice,
+// with the same value.  So no load waits for a branch.  (All loads of a row have returned before its first store: behind the
+// reduction, and behind the barrier in it.  A row may be written where it was read.)
+struct Piece { int at, twice; };
+__device__ __forceinline__ Piece piece_of(int i, int C) {
+    const int c = 8 * i, at = min(c, C - 8);
+    return Piece{at, c - at};
+}
+
+struct NormParams {
+    const void* x; const void* r; const float* gamma; void* sum; void* y; float* scale;
+    int64_t ldx, ldr, ld_sum, ldy, rows; int C; float eps;
+};
+
+// SHORT: fewer than eight elements a row (TPR = 8, NV = 1): the first thread takes them one by one
+template <class T, int NV, int TPR, int BLOCK, bool I8, bool SHORT>
+__global__ __launch_bounds__(BLOCK) void rmsnorm_kernel(NormParams P) {
+    using G = Group<TPR, BLOCK>;
+    const int t = threadIdx.x % TPR, C = P.C;
+    const int64_t mine = (int64_t)blockIdx.x * G::ROWS + threadIdx.x / TPR, row = min64(mine, P.rows - 1);
+    const T* const x = static_cast<const T*>(P.x) + row * P.ldx;
+    const T* const r = static_cast<const T*>(P.r) + row * P.ldr;
+    v8f h[NV], g[NV];
+    Piece p[NV];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        p[v] = SHORT ? Piece{0, t ? 8 : 0} : piece_of(t + TPR * v, C);
+        h[v] = SHORT ? load_some(x, C) : load8(x + p[v].at);
+    }
+    if (P.r) {
+#pragma unroll
+        for (int v = 0; v < NV; ++v) h[v] += SHORT ? load_some(r, C) : load8(r + p[v].at);
+    }
+    if (P.gamma) {
+#pragma unroll
+        for (int v = 0; v < NV; ++v) g[v] = SHORT ? load_some(P.gamma, C) : load8(P.gamma + p[v].at);
+    } else {
+#pragma unroll
+        for (int v = 0; v < NV; ++v) g[v] = v8f{1, 1, 1, 1, 1, 1, 1, 1};
+    }
+    float sum = 0.0f;
+    uint32_t top = 0;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        if (p[v].twice == 0) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum = __builtin_fmaf(h[v][e], h[v][e], sum);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (e >= p[v].twice) sum = __builtin_fmaf(h[v][e], h[v][e], sum);
+        }
+        if (I8) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(h[v][e] * g[v][e]) & 0x7fffffffu);
+        }
+    }
+    G::reduce(sum, top);
+    const float factor = 1.0f / __builtin_sqrtf(sum / (float)C + P.eps);
+    const Quant q = quant_of(top, factor);
+    if (mine >= P.rows) return;
+    if (I8 && t == 0) P.scale[row] = q.scale;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        if (p[v].twice >= 8) continue;
+        const int n = SHORT ? C : 8;
+        if (P.sum) {
+            T* s = static_cast<T*>(P.sum) + row * P.ld_sum + p[v].at;
+            if (SHORT) store_some(s, h[v], n); else store8(s, h[v]);
+        }
+        h[v] *= g[v];
+        if (I8) {
+            store_q(static_cast<int8_t*>(P.y) + row * P.ldy + p[v].at, h[v], q, n);
+        } else {
+            T* y = static_cast<T*>(P.y) + row * P.ldy + p[v].at;
+            if (SHORT) store_some(y, h[v] * factor, n); else store8(y, h[v] * factor);
+        }
+    }
+}
+
+struct GateParams { const void* x; int8_t* y; float* scale; int64_t ldx, ldy, rows; int C, act; };
+
+template <class T, int NV, int TPR, int BLOCK, bool GATED, bool SHORT>
+__global__ __launch_bounds__(BLOCK) void gated_kernel(GateParams P) {
+    using G = Group<TPR, BLOCK>;
+    using Raw = typename Eight<T>::at;
+    using Mem = typename Eight<T>::mem;
+    const int t = threadIdx.x % TPR, C = P.C;
+    const int64_t mine = (int64_t)blockIdx.x * G::ROWS + threadIdx.x / TPR, row = min64(mine, P.rows - 1);
+    const T* const x = static_cast<const T*>(P.x) + row * P.ldx;
+    Raw a[NV], b[NV];
+    Piece p[NV];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        p[v] = SHORT ? Piece{0, t ? 8 : 0} : piece_of(t + TPR * v, C);
+        if (SHORT) {
+            a[v] = __builtin_convertvector(load_some(x, C), Raw);
+            if (GATED) b[v] = __builtin_convertvector(load_some(x + C, C), Raw);
+        } else {
+            a[v] = *reinterpret_cast<const Mem*>(x + p[v].at);
+            if (GATED) b[v] = *reinterpret_cast<const Mem*>(x + C + p[v].at);
+        }
+    }
+    v8f h[NV];
+    float none = 0.0f;
+    uint32_t top = 0;
+    auto form = [&](auto act) __attribute__((always_inline)) {
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const v8f f = __builtin_convertvector(a[v], v8f);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) h[v][e] = activation<decltype(act)::value>(f[e]);
+            if (GATED) h[v] *= __builtin_convertvector(b[v], v8f);
+        }
+    };
+    with_activation(P.act, form);
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(h[v][e]) & 0x7fffffffu);
+    G::reduce(none, top);
+    const Quant q = quant_of(top, 1.0f);
+    if (mine >= P.rows) return;
+    if (t == 0) P.scale[row] = q.scale;
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+        if (p[v].twice < 8) store_q(P.y + row * P.ldy + p[v].at, h[v], q, SHORT ? C : 8);
+}
+
+// f(NV, TPR, BLOCK, SHORT) for rows of C elements: the fewest threads a row that hold it in a few pieces each
+template <class F> hipError_t with_group(int C, F&& f) {
+    const int pieces = (C + 7) / 8;
+#define IVIT_GROUP(nv, tpr, block, s) f(std::integral_constant<int, nv>(), std::integral_constant<int, tpr>(), std::integral_constant<int, block>(), std::integral_constant<bool, s>())
+    if (C < 8) return IVIT_GROUP(1, 8, 256, true);
+    if (pieces <= 8) return IVIT_GROUP(1, 8, 256, false);
+    if (pieces <= 16) return IVIT_GROUP(1, 16, 256, false);
+    if (pieces <= 32) return IVIT_GROUP(1, 32, 256, false);
+    if (pieces <= 64) return IVIT_GROUP(1, 64, 256, false);
+    if (pieces <= 256) return IVIT_GROUP(1, 256, 256, false);
+    if (pieces <= 512) return IVIT_GROUP(2, 256, 256, false);
+    if (pieces <= 1024) return IVIT_GROUP(4, 256, 256, false);
+    if (pieces <= 2048) return IVIT_GROUP(2, 1024, 1024, false);
+    return IVIT_GROUP(4, 1024, 1024, false);
+#undef IVIT_GROUP
+}
+
+template <class T> hipError_t norm_of(hipStream_t s, const RmsNormArgs& a) {
+    return with_group(a.C, [&](auto nv, auto tpr, auto block, auto few) {
+        constexpr int NV = nv, TPR = tpr, BLOCK = block, ROWS = BLOCK / TPR;
+        constexpr bool SHORT = few;
+        const NormParams P{a.x, a.residual, a.gamma, a.sum, a.y, a.y_scale, a.ldx, a.ld_res, a.ld_sum, a.ldy, a.rows, a.C, a.eps};
+        const dim3 grid((unsigned)((a.rows + ROWS - 1) / ROWS));
+        if (a.y_scale) hipLaunchKernelGGL((rmsnorm_kernel<T, NV, TPR, BLOCK, true, SHORT>), grid, dim3(BLOCK), 0, s, P);
+        else hipLaunchKernelGGL((rmsnorm_kernel<T, NV, TPR, BLOCK, false, SHORT>), grid, dim3(BLOCK), 0, s, P);
+        return hipGetLastError();
+    });
+}
+
+template <class T> hipError_t gate_of(hipStream_t s, const GatedArgs& a) {
+    return with_group(a.C, [&](auto nv, auto tpr, auto block, auto few) {
+        constexpr int NV = nv, TPR = tpr, BLOCK = block, ROWS = BLOCK / TPR;
+        constexpr bool SHORT = few;
+        const GateParams P{a.x, a.y, a.y_scale, a.ldx, a.ldy, a.rows, a.C, a.act};
+        const dim3 grid((unsigned)((a.rows + ROWS - 1) / ROWS));
+        if (a.gated) hipLaunchKernelGGL((gated_kernel<T, NV, TPR, BLOCK, true, SHORT>), grid, dim3(BLOCK), 0, s, P);
+        else hipLaunchKernelGGL((gated_kernel<T, NV, TPR, BLOCK, false, SHORT>), grid, dim3(BLOCK), 0, s, P);
+        return hipGetLastError();
+    });
+}
+
+}  // namespace
+
+hipError_t launch_rmsnorm(hipStream_t s, const RmsNormArgs& a) {
+    if (a.rows == 0) return hipSuccess;
+    const int64_t e = element_bytes(a.type), n = a.rows * a.C;
+    TraceScope trace(s, KIND_RMSNORM, 0, n * e * (1 + (a.residual != nullptr) + (a.sum != nullptr)) + n * (a.y_scale ? 1 : e));
+    if (a.type == TYPE_F16) return norm_of<_Float16>(s, a);
+    if (a.type == TYPE_BF16) return norm_of<__bf16>(s, a);
+    return norm_of<float>(s, a);
+}
+
+hipError_t launch_gated(hipStream_t s, const GatedArgs& a) {
+    if (a.rows == 0) return hipSuccess;
+    const int64_t e = element_bytes(a.type), n = a.rows * a.C;
+    TraceScope trace(s, KIND_GATED, 0, n * e * (a.gated ? 2 : 1) + n);
+    if (a.type == TYPE_F16) return gate_of<_Float16>(s, a);
+    if (a.type == TYPE_BF16) return gate_of<__bf16>(s, a);
+    return gate_of<float>(s, a);
+}
+
+}  // namespace ivit
