@@ -1,70 +1,431 @@
 // int8 x int8 -> int32 Dense on the gfx950 matrix cores with real scales and the epilogue of a float layer:
 //   y[m][n] = act(s_x[m] s_w[n] sum_k x[m][k] w[n][k] + bias[n]) + r[m][n]
 //
-// The plain form: a wavefront computes 32 tokens x 32 channels straight from memory.  The weights are the MFMA "A" operand, so a lane
-// holds channels 8 q + 4 g + r of token lane % 32 (q, r = 0 .. 3; g = lane / 32).
+// A workgroup of GM x GN wavefronts computes one tile of 32 MT GM tokens x 32 NT GN channels.  Both operands stream through S LDS
+// stages of 128 bytes of K, filled by LDS-direct loads S - 1 stages ahead (no register pass, one barrier per stage); the 16-byte
+// pieces of a row are permuted by an XOR with bits of the row number, so that the fragment reads are spread over the banks.  The
+// weights are the MFMA "A" operand and the loads put the channel rows in such an order that a lane ends up with 16 NT consecutive
+// channels of one token.
+#include "linear_rows.hpp"
 #include "regst_common.hpp"
 #include "scaled_common.hpp"
 
 namespace ivit {
 namespace {
 
+using namespace regst;
 using namespace scaled;
 
-__device__ __forceinline__ void store_one(void* y, int64_t at, int type, float v, float inv_step) {
-    if (type == TYPE_BF16) static_cast<__bf16*>(y)[at] = (__bf16)v;
-    else if (type == TYPE_F16) static_cast<_Float16*>(y)[at] = (_Float16)v;
-    else if (type == TYPE_F32) static_cast<float*>(y)[at] = v;
-    else static_cast<int8_t*>(y)[at] = (int8_t)clamp8((int32_t)__builtin_rintf(v * inv_step));
-}
-__device__ __forceinline__ float load_one(const void* p, int64_t at, int type) {
-    return type == TYPE_BF16 ? (float)static_cast<const __bf16*>(p)[at] : type == TYPE_F16 ? (float)static_cast<const _Float16*>(p)[at]
-                                                                                          : static_cast<const float*>(p)[at];
+typedef float v4f __attribute__((ext_vector_type(4)));
+
+// Tiles in bands of `height` rows of tiles, column by column within a band; each XCD takes a contiguous range of that order.  What
+// an XCD works on at one time is then a patch of the result about as high as wide, and its L2 takes in the fewest rows of either operand.
+struct TileOrder {
+    FastDiv band, full, last;                  // tiles of a band; its height; that of the last one
+    uint32_t tiles, per_xcd, last_band;
+    __device__ __forceinline__ bool tile(uint32_t block, uint32_t& tm, uint32_t& tn) const {
+        const uint32_t t = (block % NXCD) * per_xcd + block / NXCD;
+        if (t >= tiles) return false;
+        uint32_t in, row;
+        const uint32_t b = band.divide(t, in);
+        tn = b == last_band ? last.divide(in, row) : full.divide(in, row);
+        tm = b * full.d + row;
+        return true;
+    }
+    TileOrder() = default;
+    TileOrder(uint32_t rows, uint32_t cols, uint32_t height)
+        : band(height * cols), full(height), last((rows - 1) % height + 1), tiles(rows * cols), per_xcd((rows * cols + NXCD - 1) / NXCD),
+          last_band((rows - 1) / height) {}
+};
+
+struct GsParams {
+    const int8_t* x; const float* x_scale; const int8_t* w; const float* w_scale; const float* bias; const void* residual; void* y;
+    int64_t ldx, ld_res, ldy, M; int N, K, act, one_scale; float inv_step;
+    TileOrder order;
+};
+
+template <int TYPE> using Stored = std::conditional_t<TYPE == TYPE_F32, float, std::conditional_t<TYPE == TYPE_F16, _Float16,
+                                   std::conditional_t<TYPE == TYPE_BF16, __bf16, int8_t>>>;
+
+// A chunk: the 16 bytes of 16, 8 or 4 consecutive results of a row.
+template <int TYPE> struct Chunk {
+    using T = Stored<TYPE>;
+    static constexpr int E = 16 / (int)sizeof(T);
+    typedef float vf __attribute__((ext_vector_type(E)));
+    typedef T vt __attribute__((ext_vector_type(E)));
+    typedef T mem __attribute__((ext_vector_type(E), aligned(sizeof(T))));
+    static __device__ __forceinline__ v4i pack(vf v, float inv_step) {
+        if constexpr (TYPE == TYPE_I8) {
+            v4i o;
+#pragma unroll
+            for (int d = 0; d < 4; ++d) {
+                uint32_t q[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) q[e] = (uint32_t)clamp8((int32_t)__builtin_rintf(v[4 * d + e] * inv_step));     // (NaN: 0)
+                o[d] = (int)pack4(q[0], q[1], q[2], q[3]);
+            }
+            return o;
+        } else {
+            return __builtin_bit_cast(v4i, __builtin_convertvector(v, vt));
+        }
+    }
+    static __device__ __forceinline__ vf unpack(v4i v) { return __builtin_convertvector(__builtin_bit_cast(vt, v), vf); }
+    // the first n elements at p, which may have the alignment of one
+    static __device__ __forceinline__ v4i load(const T* p, int n) {
+        if (n >= E) return __builtin_bit_cast(v4i, (vt)*reinterpret_cast<const mem*>(p));
+        vt v = {};
+#pragma unroll
+        for (int e = 0; e < E - 1; ++e)
+            if (e < n) v[e] = p[e];
+        return __builtin_bit_cast(v4i, v);
+    }
+    static __device__ __forceinline__ void store(T* p, v4i w, int n) {
+        const vt v = __builtin_bit_cast(vt, w);
+        if (n >= E) { *reinterpret_cast<mem*>(p) = v; return; }
+#pragma unroll
+        for (int e = 0; e < E - 1; ++e)
+            if (e < n) p[e] = v[e];
+    }
+};
+
+template <int MT, int NT, int GM, int GN, int BK> struct GsTile {
+    static constexpr int W = GM * GN, TM = 32 * MT * GM, TN = 32 * NT * GN, LR = 1024 / BK;      // LR: rows a load instruction fills
+    static_assert(TM % (LR * W) == 0 && TN % (LR * W) == 0, "a load instruction of all wavefronts fills rows of one operand");
+    static_assert(TN % 64 == 0 && TN / 64 <= W, "the constants of 64 channels a wavefront");
+};
+
+template <int TYPE, int MT, int NT, int GM, int GN, int S, int BK>
+__global__ __launch_bounds__((64 * GM * GN), (GM * GN == 4 && MT * NT == 16 ? 1 : 2)) void gemm_scaled_kernel(GsParams P) {
+    using TL = GsTile<MT, NT, GM, GN, BK>;
+    using T = Stored<TYPE>;
+    constexpr int W = TL::W, TM = TL::TM, TN = TL::TN, LR = TL::LR, XI = TM / (LR * W), WI = TN / (LR * W), DP = XI + WI, STG = (TM + TN) * BK;
+    constexpr int PC = BK / 16;                           // 16-byte pieces of a row of a stage
+    __shared__ __align__(16) int8_t lds[S * STG];
+    __shared__ __align__(16) float ws_s[TN], bias_s[TN];
+
+    const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int li = lane & 31, lg = lane >> 5, wm = wv / GN, wn = wv % GN;
+
+    uint32_t tm, tn;
+    if (!P.order.tile(blockIdx.x, tm, tn)) return;
+    const int64_t m0 = (int64_t)tm * TM;
+    const int n0 = (int)tn * TN;
+    const int K = P.K, N = P.N;
+    const int rows = (int)min64(P.M - m0, TM);
+
+    // this lane's outputs: tokens row0 + 32 tt, channels n0 + cl + 16 ct .. + 15
+    const int row0 = wm * 32 * MT + li, cl = wn * 32 * NT + 16 * NT * lg;
+    if (wv < TN / 64) {                       // the channels' constants, 64 channels a wavefront
+        const uint32_t off = 4u * min(n0 + 64 * wv + lane, N - 1);
+        dma4(uniform_ptr(reinterpret_cast<const int8_t*>(P.w_scale)), off, lds_offset(reinterpret_cast<const int8_t*>(ws_s + 64 * wv)));
+        if (P.bias) dma4(uniform_ptr(reinterpret_cast<const int8_t*>(P.bias)), off, lds_offset(reinterpret_cast<const int8_t*>(bias_s + 64 * wv)));
+        else bias_s[64 * wv + lane] = 0.0f;
+    }
+    float xs[MT];
+#pragma unroll
+    for (int tt = 0; tt < MT; ++tt) xs[tt] = P.x_scale[P.one_scale ? 0 : m0 + min(row0 + 32 * tt, rows - 1)];
+
+    // (32-bit offsets from the tile's first row: 255 rows of at most 2^22 bytes)
+    // Load instruction i of a wavefront fills LDS rows LR (W i + wavefront) + lane / PC, PC lanes a row; the lane lands in physical
+    // piece p = lane % PC of row r and fetches piece p ^ mix(r).  Rows past the last token or channel repeat it (never stored),
+    // pieces past the end of a row its last piece (never multiplied, see below).
+    auto mix = [](int r) __attribute__((always_inline)) { return (r >> 1) & (PC - 1); };
+    const int ld_r = LR * wv + lane / PC, ld_col = 16 * ((lane % PC) ^ mix(ld_r));
+    const int8_t* xg = uniform_ptr(P.x + m0 * P.ldx);
+    const int8_t* wg = uniform_ptr(P.w + (int64_t)n0 * K);
+    uint32_t off[DP];
+#pragma unroll
+    for (int i = 0; i < DP; ++i) {
+        if (i < XI) {
+            off[i] = (uint32_t)min(LR * W * i + ld_r, rows - 1) * (uint32_t)P.ldx + ld_col;
+        } else {
+            // row 8 q + 4 g + r of MFMA tile ct holds channel 16 NT g + 16 ct + 4 q + r of the wavefront's 32 NT: that is
+            // accumulator register 4 q + r of lane group g
+            const int R = LR * W * (i - XI) + ld_r, ct = (R >> 5) % NT, rr = R & 31;
+            const int ch = (R / (32 * NT)) * 32 * NT + 16 * NT * ((rr >> 2) & 1) + 16 * ct + 4 * (rr >> 3) + (rr & 3);
+            off[i] = (uint32_t)min(ch, N - 1 - n0) * (uint32_t)K + ld_col;
+        }
+    }
+    auto buffer = [](const int8_t* p) __attribute__((always_inline)) {
+        const uint64_t a = (uint64_t)p;
+        return v4i{(int)(uint32_t)a, (int)(uint32_t)(a >> 32), (int)kTileBytes, 0x00020000};
+    };
+    const v4i x_buf = buffer(xg), w_buf = buffer(wg);
+    const int stages = (K + BK - 1) / BK, k_last = K - (stages - 1) * BK;      // bytes of K in the last stage: 16 .. BK
+    const uint32_t lds0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)(lds_offset(lds) + wv * 1024));
+    // A stage's loads: stage `is` goes to buffer is % S, known where the loads stand.  A lane whose piece lies past the end of
+    // the rows moves back to the last one (the last stage only).  One scalar offset serves both operands.
+    const int back = max(ld_col - (k_last - 16), 0), moves = k_last < BK ? stages - 1 : -1;
+    int is = 0;
+    uint32_t k_off = 0;
+    auto issue = [&](auto buf_c) __attribute__((always_inline)) {
+        if (is == moves) {
+#pragma unroll
+            for (int i = 0; i < DP; ++i) off[i] -= back;
+        }
+        static_for<DP>([&](auto i_c) __attribute__((always_inline)) {
+            constexpr int i = decltype(i_c)::value;
+            load_lds<decltype(buf_c)::value * STG + i * W * 1024>(i < XI ? x_buf : w_buf, off[i], k_off, lds0);
+        });
+        ++is;
+        k_off += BK;
+    };
+    // PIPE: the tiles of four products a k-step and more (see below)
+    constexpr bool PIPE = MT * NT >= 4;
+    static_for<PIPE ? S : S - 1>([&](auto buf) __attribute__((always_inline)) {
+        if (decltype(buf)::value < stages) issue(buf);
+    });
+
+    v16i acc[NT][MT];
+#pragma unroll
+    for (int ct = 0; ct < NT; ++ct)
+#pragma unroll
+        for (int tt = 0; tt < MT; ++tt) acc[ct][tt] = sums_from(0);
+    constexpr int KS = BK / 32, AHEAD = MT * NT == 1 ? KS : 2;      // fragments are read AHEAD - 1 k-steps before their use
+    int fx[KS], fw[KS];                                   // where this lane's fragments of k-step kk lie (buffer 0)
+#pragma unroll
+    for (int kk = 0; kk < KS; ++kk) {
+        const int col = 16 * ((2 * kk + lg) ^ mix(li));
+        fx[kk] = row0 * BK + col;
+        fw[kk] = (TM + wn * 32 * NT + li) * BK + col;
+    }
+    struct Frag { v4i a[NT], b[MT]; };
+    // fragment i of k-step kk, in the order of their use: the first of the weights, those of the tokens, the other ones
+    auto read_one = [&](Frag& f, int i, int kk, int buf) __attribute__((always_inline)) {
+        if (i >= 1 && i <= MT) f.b[i - 1] = *reinterpret_cast<const v4i*>(lds + fx[kk] + buf * STG + (i - 1) * 32 * BK);
+        else f.a[i ? i - MT : 0] = *reinterpret_cast<const v4i*>(lds + fw[kk] + buf * STG + (i ? i - MT : 0) * 32 * BK);
+    };
+    auto read_frag = [&](Frag& f, int kk, int buf) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < NT + MT; ++i) read_one(f, i, kk, buf);
+    };
+    auto multiply = [&](const Frag& f) __attribute__((always_inline)) {
+#pragma unroll
+        for (int ct = 0; ct < NT; ++ct)
+#pragma unroll
+            for (int tt = 0; tt < MT; ++tt) acc[ct][tt] = __builtin_amdgcn_mfma_i32_32x32x32_i8(f.a[ct], f.b[tt], acc[ct][tt], 0, 0, 0);
+    };
+    static_assert(S >= 2 && S <= 4 && (S - 1) * DP + 2 <= 63, "wait counts");
+    int s = 0;
+    const int full = k_last == BK ? stages : stages - 1;  // a last stage of less than 128 bytes comes after the loop
+    // all loads but those of the `left` stages requested last have arrived, and LDS reads returned, for everybody
+    auto arrive_but = [&](int left) __attribute__((always_inline)) {
+        if (left <= 0) arrive<0>();
+        else if (S <= 3 || left == 1) arrive<DP>();
+        else arrive<2 * DP>();
+    };
+    if constexpr (PIPE) {
+        // All S buffers are filled to begin with.  In front of the last k-step of stage s, whose fragments are in registers then, stage
+        // s + 1 has to have arrived; behind the barrier there nobody reads stage s any more: its buffer takes stage s + S, and the first
+        // fragments of stage s + 1 come under the products of that last k-step.  So no stage begins with a wait.  Reads and requests stand
+        // one by one between the products: a wavefront issues in order, and eight reads at a stretch hold it for longer than a product takes.
+        Frag f[2];
+        arrive_but(min(stages, S) - 1 >= S - 1 ? S - 1 : 0);
+        read_frag(f[0], 0, 0);
+        auto body = [&](auto buf_c, auto more_c) __attribute__((always_inline)) {
+            constexpr int buf = decltype(buf_c)::value, nb = (buf + 1) % S;
+            constexpr bool MORE = decltype(more_c)::value;            // there is a stage s + S (false: maybe)
+            static_for<KS>([&](auto kk_c) __attribute__((always_inline)) {
+                constexpr int kk = decltype(kk_c)::value;
+                constexpr bool last = kk == KS - 1;
+                if constexpr (last) {
+                    if constexpr (MORE) {
+                        arrive<(S - 2) * DP>();
+                        if (is == moves) {
+#pragma unroll
+                            for (int i = 0; i < DP; ++i) off[i] -= back;
+                        }
+                    } else if (s + 1 < stages) {
+                        arrive_but(min(stages - 2 - s, S - 2));
+                        if (is < stages) issue(buf_c);
+                    }
+                }
+                constexpr int READS = NT + MT, DO = READS + (last && MORE ? DP : 0), N_MUL = NT * MT;
+                static_for<N_MUL>([&](auto i_c) __attribute__((always_inline)) {
+                    constexpr int i = decltype(i_c)::value, ct = i / MT, tt = i % MT;
+                    acc[ct][tt] = __builtin_amdgcn_mfma_i32_32x32x32_i8(f[kk & 1].a[ct], f[kk & 1].b[tt], acc[ct][tt], 0, 0, 0);
+                    constexpr int from = i * DO / N_MUL, to = (i + 1) * DO / N_MUL;
+                    static_for<to - from>([&](auto d_c) __attribute__((always_inline)) {
+                        constexpr int d = from + decltype(d_c)::value;
+                        if constexpr (d < READS) read_one(f[(kk + 1) & 1], d, last ? 0 : kk + 1, last ? nb : buf);
+                        else load_lds<buf * STG + (d - READS) * W * 1024>(d - READS < XI ? x_buf : w_buf, off[d - READS], k_off, lds0);
+                    });
+                    __builtin_amdgcn_sched_barrier(0);
+                });
+                if constexpr (last && MORE) { ++is; k_off += BK; }
+            });
+            ++s;
+        };
+        static_assert(KS % 2 == 0, "the first fragments of every stage go to the same registers");
+#pragma unroll 1
+        while (s + 2 * S <= stages)
+            static_for<S>([&](auto buf) __attribute__((always_inline)) { body(buf, std::true_type()); });
+#pragma unroll 1
+        while (s < full)
+            static_for<S>([&](auto buf) __attribute__((always_inline)) { if (s < full) body(buf, std::false_type()); });
+    } else {
+        // Stage s: its loads have arrived when at most those of the later stages requested so far (S - 2, fewer at the end)
+        // are outstanding; behind the barrier nobody reads stage s - 1 any more and its buffer takes stage s + S - 1.  Those
+        // loads go out behind the first fragment reads.
+        auto body = [&](auto buf_c) __attribute__((always_inline)) {
+            constexpr int buf = decltype(buf_c)::value;
+            arrive_but(min(stages - 1 - s, S - 2));
+            Frag f[AHEAD];
+            static_for<AHEAD - 1>([&](auto kk) __attribute__((always_inline)) { read_frag(f[decltype(kk)::value], decltype(kk)::value, buf); });
+            if (is < stages) issue(std::integral_constant<int, (buf + S - 1) % S>());
+            static_for<KS>([&](auto kk_c) __attribute__((always_inline)) {
+                constexpr int kk = decltype(kk_c)::value;
+                if constexpr (kk + AHEAD - 1 < KS) read_frag(f[(kk + AHEAD - 1) % AHEAD], kk + AHEAD - 1, buf);
+                multiply(f[kk % AHEAD]);
+            });
+            ++s;
+        };
+#pragma unroll 1
+        while (s < full)
+            static_for<S>([&](auto buf) __attribute__((always_inline)) { if (s < full) body(buf); });
+    }
+    if (full < stages) {                                  // what is left of K; of its last 32 bytes maybe the first half only
+        arrive<0>();
+        const int buf = s % S;
+        static_for<KS>([&](auto kk_c) __attribute__((always_inline)) {
+            constexpr int kk = decltype(kk_c)::value;
+            if (32 * kk >= k_last) return;
+            Frag f;
+            read_frag(f, kk, buf);
+            if (32 * kk + 16 >= k_last && lg) {
+#pragma unroll
+                for (int ct = 0; ct < NT; ++ct) f.a[ct] = v4i{0, 0, 0, 0};
+            }
+            multiply(f);
+        });
+    }
+
+    // ---- epilogue.  A lane has 16 NT consecutive channels of a token, and its neighbour those of the next one: stored from there, every
+    // instruction would touch 64 lines and fill none.  So a wavefront turns its results over in LDS that it has for itself
+    // (REGION bytes), SLOTS times 32 tokens at once, and lines leave whole; a residual comes in the same way.  Chunk c of a row
+    // stands at c ^ swz(row), which spreads rows over the banks.
+    using CK = Chunk<TYPE>;
+    constexpr int RB = 32 * NT * (int)sizeof(T), CH = RB / 16, MINE = NT * (int)sizeof(T);     // bytes and chunks of a row; a lane's chunks
+    constexpr int REGION = S * STG / W / 1024 * 1024, FIT = REGION / (32 * RB), SLOTS = FIT >= MT ? MT : FIT >= 2 && MT % 2 == 0 ? 2 : 1;
+    constexpr int MOVES = RB / 32;                        // instructions of 64 chunks that move a slot
+    static_assert(FIT >= 1 && MT % SLOTS == 0, "room for 32 rows");
+    auto swz = [](int r) __attribute__((always_inline)) { return CH >= 8 ? r & (CH - 1) : (r / (8 / CH)) & (CH - 1); };
+    __syncthreads();                                      // (nobody reads operands any more)
+    int8_t* const own = lds + wv * REGION;
+    const int wc0 = n0 + wn * 32 * NT;                    // the wavefront's first channel
+    // chunk i of this lane when rows move: row and column within a slot
+    const int mv_row = lane / CH, mv_ch = lane % CH;
+    constexpr int MV_ROWS = 64 / CH;
+#pragma unroll 1
+    for (int t0 = 0; t0 < MT; t0 += SLOTS) {
+        const int64_t mw = m0 + wm * 32 * MT + 32 * t0;   // the first token of the slots
+        const int left = rows - (wm * 32 * MT + 32 * t0); // tokens from there on
+        if constexpr (TYPE != TYPE_I8) {
+            if (P.residual) {
+                v4i r[SLOTS * MOVES];
+#pragma unroll
+                for (int i = 0; i < SLOTS * MOVES; ++i) {
+                    const int row = MV_ROWS * i + mv_row, n = N - (wc0 + CK::E * mv_ch);
+                    r[i] = v4i{0, 0, 0, 0};
+                    if (row < left && n > 0)
+                        r[i] = CK::load(static_cast<const T*>(P.residual) + (mw + row) * P.ld_res + wc0 + CK::E * mv_ch, n);
+                }
+#pragma unroll
+                for (int i = 0; i < SLOTS * MOVES; ++i) {
+                    const int row = MV_ROWS * i + mv_row;
+                    *reinterpret_cast<v4i*>(own + row * RB + 16 * (mv_ch ^ swz(row))) = r[i];
+                }
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+            }
+        }
+        with_activation(P.act, [&](auto act) __attribute__((always_inline)) {
+#pragma unroll
+            for (int j = 0; j < MINE; ++j) {
+                const int c = cl + CK::E * j;             // first channel of the chunk in the tile
+                typename CK::vf ws, bi;
+#pragma unroll
+                for (int e = 0; e < CK::E; e += 4) {
+                    const v4f a = *reinterpret_cast<const v4f*>(&ws_s[c + e]), b = *reinterpret_cast<const v4f*>(&bias_s[c + e]);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) { ws[e + k] = a[k]; bi[e + k] = b[k]; }
+                }
+                static_for<MT>([&](auto tt_c) __attribute__((always_inline)) {
+                    constexpr int tt = decltype(tt_c)::value;
+                    if (tt < t0 || tt >= t0 + SLOTS) return;
+                    int8_t* const at = own + (32 * (tt % SLOTS) + li) * RB + 16 * ((MINE * lg + j) ^ swz(li));
+                    typename CK::vf v;
+#pragma unroll
+                    for (int e = 0; e < CK::E; ++e) {
+                        constexpr int PER = 16 / CK::E;   // chunks of the 16 results of an MFMA tile
+                        v[e] = activation<decltype(act)::value>(__builtin_fmaf((float)acc[j / PER][tt][CK::E * (j % PER) + e] * ws[e], xs[tt], bi[e]));
+                    }
+                    if constexpr (TYPE != TYPE_I8) {
+                        if (P.residual) v += CK::unpack(*reinterpret_cast<const v4i*>(at));
+                    }
+                    *reinterpret_cast<v4i*>(at) = CK::pack(v, P.inv_step);
+                });
+                __builtin_amdgcn_sched_barrier(0);        // keep the register footprint of the epilogue small
+            }
+        });
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int i = 0; i < SLOTS * MOVES; ++i) {
+            const int row = MV_ROWS * i + mv_row, n = N - (wc0 + CK::E * mv_ch);
+            const v4i v = *reinterpret_cast<const v4i*>(own + row * RB + 16 * (mv_ch ^ swz(row)));
+            if (row < left && n > 0) CK::store(static_cast<T*>(P.y) + (mw + row) * P.ldy + wc0 + CK::E * mv_ch, v, n);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    }
 }
 
-__global__ __launch_bounds__(256) void gemm_scaled_kernel(ScaledArgs P, uint32_t tiles_n, uint32_t tiles) {
-    const int lane = threadIdx.x & 63, li = lane & 31, lg = lane >> 5;
-    const uint32_t tile = blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (tile >= tiles) return;
-    const int64_t m = (int64_t)(tile / tiles_n) * 32 + li;
-    const int n0 = (int)(tile % tiles_n) * 32, N = P.N, K = P.K;
-    const int8_t* xp = P.x + min64(m, P.M - 1) * P.ldx;
-    const int8_t* wp = P.w + (int64_t)min(n0 + li, N - 1) * K;
-    v16i acc = {};
-    for (int k = 16 * lg; k - 16 * lg < K; k += 32) {
-        v4i a = {0, 0, 0, 0}, b = {0, 0, 0, 0};
-        if (k < K) {
-            a = *reinterpret_cast<const v4i*>(wp + k);
-            b = *reinterpret_cast<const v4i*>(xp + k);
-        }
-        acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(a, b, acc, 0, 0, 0);
+int64_t g_h = 4;
+template <int TYPE, int MT, int NT, int GM, int GN, int S, int BK = 128> hipError_t launch_tile(hipStream_t s, const ScaledArgs& a) {
+    using TL = GsTile<MT, NT, GM, GN, BK>;
+    GsParams P;
+    P.x = a.x; P.x_scale = a.x_scale; P.w = a.w; P.w_scale = a.w_scale; P.bias = a.bias; P.residual = a.residual; P.y = a.y;
+    P.ldx = a.ldx; P.ld_res = a.ld_res; P.ldy = a.ldy; P.M = a.M; P.N = a.N; P.K = a.K; P.act = a.act; P.one_scale = a.one_scale;
+    P.inv_step = a.y_type == TYPE_I8 ? 1.0f / a.y_step : 0.0f;
+    const int64_t tm = (a.M + TL::TM - 1) / TL::TM, tn = (a.N + TL::TN - 1) / TL::TN, grid = (tm * tn + NXCD - 1) / NXCD * NXCD;
+    if (grid > 0x7fffffffLL) return hipErrorInvalidValue;
+    P.order = TileOrder((uint32_t)tm, (uint32_t)tn, (uint32_t)(tm < g_h ? tm : g_h));
+    hipLaunchKernelGGL((gemm_scaled_kernel<TYPE, MT, NT, GM, GN, S, BK>), dim3((unsigned)grid), dim3(64 * TL::W), 0, s, P);
+    return hipGetLastError();
+}
+
+int force_tile = -1;
+template <int TYPE> hipError_t launch_type(hipStream_t s, const ScaledArgs& a) {
+    const int64_t tiles = ((a.M + 63) / 64) * (((int64_t)a.N + 63) / 64), cus = num_cus();
+    int f = force_tile;
+    if (f < 0) f = tiles <= 3 * cus ? 0 : tiles <= 12 * cus ? 1 : 2;
+    switch (f) {
+        case 0: return launch_tile<TYPE, 1, 1, 2, 2, 3>(s, a);
+        case 1: return launch_tile<TYPE, 2, 2, 2, 2, 2>(s, a);
+        case 2: return launch_tile<TYPE, 4, 2, 2, 4, 2>(s, a);
+        case 3: return launch_tile<TYPE, 4, 4, 2, 2, 2>(s, a);
+        case 4: return launch_tile<TYPE, 1, 1, 4, 2, 4>(s, a);
+        case 5: return launch_tile<TYPE, 2, 1, 2, 4, 3>(s, a);
+        case 6: return launch_tile<TYPE, 4, 4, 2, 2, 4, 64>(s, a);
+        case 8: return launch_tile<TYPE, 4, 2, 2, 4, 4, 64>(s, a);
+        default: return launch_tile<TYPE, 2, 2, 4, 2, 3>(s, a);
     }
-    if (m >= P.M) return;
-    const float sx = P.x_scale[P.one_scale ? 0 : m], inv_step = P.y_type == TYPE_I8 ? 1.0f / P.y_step : 0.0f;
-    with_activation(P.act, [&](auto act) __attribute__((always_inline)) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const int n = n0 + 8 * (e >> 2) + 4 * lg + (e & 3);
-            if (n >= N) continue;
-            float v = (float)acc[e] * (sx * P.w_scale[n]);
-            if (P.bias) v += P.bias[n];
-            v = activation<decltype(act)::value>(v);
-            if (P.residual) v += load_one(P.residual, m * P.ld_res + n, P.y_type);
-            store_one(P.y, m * P.ldy + n, P.y_type, v, inv_step);
-        }
-    });
 }
 
 }  // namespace
+extern "C" void ivit_dbg_force_tile(int f) { force_tile = f < 0 ? -1 : f % 100; g_h = f >= 100 ? f / 100 : 4; }
 
 hipError_t launch_linear_scaled(hipStream_t s, const ScaledArgs& a) {
     if (a.M == 0) return hipSuccess;
     TraceScope trace(s, KIND_GEMM_SCALED, 2 * a.M * a.N * a.K,
                      a.M * a.K + (int64_t)a.N * a.K + a.M * a.N * element_bytes(a.y_type) * (a.residual ? 2 : 1));
-    const int64_t tn = (a.N + 31) / 32, tiles = (a.M + 31) / 32 * tn, grid = (tiles + 3) / 4;
-    if (tiles > 0x7fffffffLL) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(gemm_scaled_kernel, dim3((unsigned)grid), dim3(256), 0, s, a, (uint32_t)tn, (uint32_t)tiles);
-    return hipGetLastError();
+    switch (a.y_type) {
+        case TYPE_F16: return launch_type<TYPE_F16>(s, a);
+        case TYPE_BF16: return launch_type<TYPE_BF16>(s, a);
+        case TYPE_I8: return launch_type<TYPE_I8>(s, a);
+        default: return launch_type<TYPE_F32>(s, a);
+    }
 }
 
 }  // namespace ivit

@@ -34,17 +34,6 @@ struct StParams {
 typedef int v4i_w __attribute__((ext_vector_type(4), aligned(4)));     // 16 bytes at any address of words
 typedef int v4i_any __attribute__((ext_vector_type(4), aligned(1)));   // 16 bytes at any address
 
-// 16 bytes per lane from a buffer into LDS at lds + AT (the wait state is the one that such a load needs after m0 was written)
-template <int AT> __device__ __forceinline__ void load_lds(const v4i& buf, uint32_t off, uint32_t more, uint32_t lds) {
-    asm volatile("s_add_u32 m0, %0, %4\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
-                 : : "s"(lds), "v"(off), "s"(buf), "s"(more), "i"(AT) : "memory", "m0", "scc");
-}
-
-// every load but the newest N of this wavefront has arrived, its LDS reads have returned, and so for all wavefronts
-template <int N> __device__ __forceinline__ void arrive() {
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(N) : "memory");
-}
-
 // XS > 0: the rows of x are normalised first (I-LayerNorm, Sec. 3.5, Eq. 19-20).  The token rows of the tile, all of K
 // (K <= 128 XS), are fetched at once and stay in LDS, where they are normalised in place; only the weights stream.  Every
 // workgroup of a row of tiles repeats that work, so the four wavefronts stand side by side: 32 tokens x 128 channels.

@@ -1,5 +1,5 @@
 // Pieces shared by the Dense kernels built on LDS-direct loads (gemm_rs.hip, gemm_ks.hip, gemm_tl.hip, gemm_st.hip,
-// token_block.hip): those loads, scalar pointers, the median of three, the token order of the MFMA "A" operand.
+// token_block.hip, gemm_scaled.hip): those loads, scalar pointers, the median of three, the token order of the MFMA "A" operand.
 #pragma once
 #include <type_traits>
 #include <utility>
@@ -50,6 +50,17 @@ __device__ __forceinline__ void dma4(const void* base, uint32_t off, uint32_t ds
                  : : "s"(__builtin_amdgcn_readfirstlane(dst)), "v"(off), "s"(base) : "memory", "m0");
 }
 __device__ __forceinline__ void wait_vm0() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// 16 bytes per lane from a buffer into LDS at lds + AT (the wait state is the one that such a load needs after m0 was written)
+template <int AT> __device__ __forceinline__ void load_lds(const v4i& buf, uint32_t off, uint32_t more, uint32_t lds) {
+    asm volatile("s_add_u32 m0, %0, %4\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+                 : : "s"(lds), "v"(off), "s"(buf), "s"(more), "i"(AT) : "memory", "m0", "scc");
+}
+
+// every load but the newest N of this wavefront has arrived, its LDS reads have returned, and so for all wavefronts
+template <int N> __device__ __forceinline__ void arrive() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(N) : "memory");
+}
 
 __device__ __forceinline__ int32_t med3(int32_t v, int32_t lo, int32_t hi) {
     int32_t m;
