@@ -577,36 +577,42 @@ def ivit_forward_swin(patches, logits, params, B, workspace, stream=None):
 # ------------------------------------------------------------------ float layers around int8 products
 ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3, "gelu_tanh": 4, "gelu_sigmoid": 5}
 _TYPES = None           # torch dtype -> ivit_type (torch is imported by the first call)
+_FLOAT32 = _INT8 = None
+
+
+def _setup():
+    global _TYPES, _FLOAT32, _INT8
+    import torch
+    _FLOAT32, _INT8 = torch.float32, torch.int8
+    _TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2, torch.int8: 3}
 
 
 def _type(t, where):
-    global _TYPES
     if _TYPES is None:
-        import torch
-        _TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2, torch.int8: 3}
+        _setup()
     k = _TYPES.get(t.dtype)
     if k is None:
         raise ValueError("%s: no tensors of %s" % (where, t.dtype))
     return k
 
 
-def _rows(t, rows, cols, kind, device, where):
+def _rows(t, shape, dtype, device, where):
     """Leading dimension of a two-dimensional tensor of the expected shape and type whose rows are dense."""
-    s = t.stride()
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols or (s[1] != 1 and cols > 1):
-        raise ValueError("%s: a tensor of %s with strides %s, wanted [%d, %d] with dense rows" % (where, tuple(t.shape), s, rows, cols))
-    if _type(t, where) != kind or t.get_device() != device:
-        raise ValueError("%s: a tensor of %s on %s, wanted ivit_type %d on device %d" % (where, t.dtype, t.device, kind, device))
-    return s[0] if rows > 1 else cols
+    if t.shape == shape and t.dtype is dtype and t.get_device() == device:
+        s = t.stride()
+        if s[1] == 1 or shape[1] == 1:
+            return s[0] if shape[0] > 1 else shape[1]
+    raise ValueError("%s: a tensor of %s, %s with strides %s on %s, wanted %s, %s with dense rows on device %d" % (
+        where, tuple(t.shape), t.dtype, t.stride(), t.device, tuple(shape), dtype, device))
 
 
 def _vector(t, n, device, where):
     """Pointer of a dense float32 vector of n values (None: NULL)."""
     if t is None:
         return None
-    if t.numel() != n or not t.is_contiguous() or _type(t, where) != 0 or t.get_device() != device:
-        raise ValueError("%s: wanted %d dense float32 values on device %d, got %s of %s on %s" % (where, n, device, tuple(t.shape), t.dtype, t.device))
-    return t.data_ptr()
+    if t.numel() == n and t.dtype is _FLOAT32 and t.get_device() == device and t.is_contiguous():
+        return t.data_ptr()
+    raise ValueError("%s: wanted %d dense float32 values on device %d, got %s of %s on %s" % (where, n, device, tuple(t.shape), t.dtype, t.device))
 
 
 def _launch_stream(stream, device, where):
@@ -614,10 +620,11 @@ def _launch_stream(stream, device, where):
     if device < 0:
         raise ValueError("%s: tensors have to be on a GPU" % where)
     import torch
-    if torch.cuda.current_device() != device:
-        raise ValueError("%s: tensors on device %d, but device %d is the current one" % (where, device, torch.cuda.current_device()))
+    current = torch.cuda.current_device()
+    if current != device:
+        raise ValueError("%s: tensors on device %d, but device %d is the current one" % (where, device, current))
     if stream is None:
-        return torch.cuda.current_stream().cuda_stream
+        return torch.cuda.current_stream(device).cuda_stream
     if not isinstance(stream, int) and stream.device_index != device:
         raise ValueError("%s: tensors on device %d, a stream of device %d" % (where, device, stream.device_index))
     return _stream(stream)
@@ -634,14 +641,16 @@ def ivit_rmsnorm_quant(x, gamma, y, y_scale, eps, residual=None, sum_out=None, s
     """x, residual, sum_out: [rows, C] float tensors of one type; gamma: float32 [C] or None; y: int8 with y_scale float32
     [rows], or of x's type with y_scale None.  Returns y."""
     where = "ivit_rmsnorm_quant"
-    rows, Cc = x.shape
-    kind, dev = _type(x, where), x.get_device()
+    kind, shape, dtype, dev = _type(x, where), x.shape, x.dtype, x.get_device()
+    rows, Cc = shape
     st = load().ivit_rmsnorm_quant(
-        _launch_stream(stream, dev, where), x.data_ptr(), _rows(x, rows, Cc, kind, dev, where),
-        _ptr(residual), 0 if residual is None else _rows(residual, rows, Cc, kind, dev, where), _vector(gamma, Cc, dev, where), eps,
-        _ptr(sum_out), 0 if sum_out is None else _rows(sum_out, rows, Cc, kind, dev, where),
-        y.data_ptr(), _rows(y, rows, Cc, kind if y_scale is None else 3, dev, where), _vector(y_scale, rows, dev, where), rows, Cc, kind)
-    _check(st, where)
+        _launch_stream(stream, dev, where), x.data_ptr(), _rows(x, shape, dtype, dev, where),
+        None if residual is None else residual.data_ptr(), 0 if residual is None else _rows(residual, shape, dtype, dev, where),
+        _vector(gamma, Cc, dev, where), eps,
+        None if sum_out is None else sum_out.data_ptr(), 0 if sum_out is None else _rows(sum_out, shape, dtype, dev, where),
+        y.data_ptr(), _rows(y, shape, dtype if y_scale is None else _INT8, dev, where), _vector(y_scale, rows, dev, where), rows, Cc, kind)
+    if st:
+        _check(st, where)
     return y
 
 
@@ -649,31 +658,34 @@ def ivit_linear_scaled(x, x_scale, w, w_scale, y, bias=None, act="none", residua
     """x: int8 [M, K]; x_scale: float32, M values or one; w: dense int8 [N, K]; w_scale, bias: float32 [N]; y: [M, N] float32, float16
     or bfloat16, with a residual of the same type or None, or int8 with y_step.  Returns y."""
     where = "ivit_linear_scaled"
+    kind, dtype, dev = _type(y, where), y.dtype, x.get_device()
     M, K = x.shape
-    N, dev = w.shape[0], x.get_device()
-    kind, ns = _type(y, where), x_scale.numel()
-    ldw = _rows(w, N, K, 3, dev, where)
-    if ldw != K:
-        raise ValueError("%s: the weights have to be dense" % where)
+    wshape = w.shape
+    N = wshape[0]
+    if len(wshape) != 2 or wshape[1] != K or not w.is_contiguous() or w.dtype is not _INT8 or w.get_device() != dev:
+        raise ValueError("%s: weights of %s, %s on %s, wanted dense int8 [N, %d] on device %d" % (where, tuple(wshape), w.dtype, w.device, K, dev))
     if kind == 3 and y_step is None:
         raise ValueError("%s: an int8 result needs y_step" % where)
-    one = ns == 1 and M != 1
+    one = M != 1 and x_scale.numel() == 1
+    out = (M, N)
     st = load().ivit_linear_scaled(
-        _launch_stream(stream, dev, where), x.data_ptr(), _rows(x, M, K, 3, dev, where), _vector(x_scale, 1 if one else M, dev, where), one,
-        w.data_ptr(), _vector(w_scale, N, dev, where), _vector(bias, N, dev, where), _activation(act, where), _ptr(residual),
-        0 if residual is None else _rows(residual, M, N, kind, dev, where), y.data_ptr(), _rows(y, M, N, kind, dev, where), kind,
-        0.0 if y_step is None else y_step, M, N, K)
-    _check(st, where)
+        _launch_stream(stream, dev, where), x.data_ptr(), _rows(x, (M, K), _INT8, dev, where), _vector(x_scale, 1 if one else M, dev, where), one,
+        w.data_ptr(), _vector(w_scale, N, dev, where), _vector(bias, N, dev, where), _activation(act, where),
+        None if residual is None else residual.data_ptr(), 0 if residual is None else _rows(residual, out, dtype, dev, where),
+        y.data_ptr(), _rows(y, out, dtype, dev, where), kind, 0.0 if y_step is None else y_step, M, N, K)
+    if st:
+        _check(st, where)
     return y
 
 
 def ivit_gated_quant(x, y, y_scale, act="silu", gated=True, stream=None):
     """x: [rows, 2 C] (gated: the gate's channels first) or [rows, C] float; y: int8 [rows, C]; y_scale: float32 [rows].  Returns y."""
     where = "ivit_gated_quant"
-    rows, Cc = y.shape
-    kind, dev = _type(x, where), x.get_device()
+    kind, dev, shape = _type(x, where), x.get_device(), y.shape
+    rows, Cc = shape
     st = load().ivit_gated_quant(
-        _launch_stream(stream, dev, where), x.data_ptr(), _rows(x, rows, 2 * Cc if gated else Cc, kind, dev, where),
-        y.data_ptr(), _rows(y, rows, Cc, 3, dev, where), _vector(y_scale, rows, dev, where), rows, Cc, kind, _activation(act, where), bool(gated))
-    _check(st, where)
+        _launch_stream(stream, dev, where), x.data_ptr(), _rows(x, (rows, 2 * Cc) if gated else shape, x.dtype, dev, where),
+        y.data_ptr(), _rows(y, shape, _INT8, dev, where), _vector(y_scale, rows, dev, where), rows, Cc, kind, _activation(act, where), bool(gated))
+    if st:
+        _check(st, where)
     return y

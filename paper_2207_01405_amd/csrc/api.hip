@@ -736,7 +736,8 @@ int ivit_linear_scaled(void* stream, const int8_t* x, int64_t ldx, const float* 
     int st;
     if ((st = check_rows(y, ldy, N, y_type)) != IVIT_OK) return st;
     if (residual && (st = check_rows(residual, ld_residual, N, y_type)) != IVIT_OK) return st;
-    const ivit::ScaledArgs a{x, x_scale, w, w_scale, bias, residual, y, ldx, ld_residual, ldy, M, N, K, act, y_type, one_scale != 0, y_step};
+    const ivit::ScaledArgs a{x, x_scale, w, w_scale, bias, residual, y, ldx, ld_residual, ldy, M, N, K, act, y_type, one_scale != 0,
+                             y_type == IVIT_I8 ? 1.0f / y_step : 0.0f};
     return hip_status(ivit::launch_linear_scaled(static_cast<hipStream_t>(stream), a));
 }
 

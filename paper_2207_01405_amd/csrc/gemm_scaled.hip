@@ -306,34 +306,38 @@ __global__ __launch_bounds__((64 * GM * GN), (GM * GN == 4 && MT * NT == 16 ? 1 
     // stands at c ^ swz(row), which spreads rows over the banks.
     using CK = Chunk<TYPE>;
     constexpr int RB = 32 * NT * (int)sizeof(T), CH = RB / 16, MINE = NT * (int)sizeof(T);     // bytes and chunks of a row; a lane's chunks
-    constexpr int REGION = S * STG / W / 1024 * 1024, FIT = REGION / (32 * RB), SLOTS = FIT >= MT ? MT : FIT >= 2 && MT % 2 == 0 ? 2 : 1;
+    constexpr int REGION = S * STG / W / 1024 * 1024, FIT = REGION / (32 * RB), SLOTS = FIT >= MT && MT * RB <= 512 ? MT : 1;      // (at most 16 chunks of a residual in registers)
     constexpr int MOVES = RB / 32;                        // instructions of 64 chunks that move a slot
     static_assert(FIT >= 1 && MT % SLOTS == 0, "room for 32 rows");
     auto swz = [](int r) __attribute__((always_inline)) { return CH >= 8 ? r & (CH - 1) : (r / (8 / CH)) & (CH - 1); };
     __syncthreads();                                      // (nobody reads operands any more)
     int8_t* const own = lds + wv * REGION;
-    const int wc0 = n0 + wn * 32 * NT;                    // the wavefront's first channel
-    // chunk i of this lane when rows move: row and column within a slot
-    const int mv_row = lane / CH, mv_ch = lane % CH;
+    // chunk i of this lane when rows move: row MV_ROWS i + mv_row of the slots, channels from c_mv on
     constexpr int MV_ROWS = 64 / CH;
+    const int mv_row = lane / CH, c_mv = n0 + wn * 32 * NT + CK::E * (lane % CH);
+    const bool whole = n0 + (wn + 1) * 32 * NT <= N;      // (of all lanes) no channel of the wavefront's is past the last
+    auto at_mv = [&](int i) __attribute__((always_inline)) {
+        const int row = MV_ROWS * i + mv_row;
+        return own + row * RB + 16 * ((lane % CH) ^ swz(row));
+    };
 #pragma unroll 1
     for (int t0 = 0; t0 < MT; t0 += SLOTS) {
         const int64_t mw = m0 + wm * 32 * MT + 32 * t0;   // the first token of the slots
         const int left = rows - (wm * 32 * MT + 32 * t0); // tokens from there on
+        if (left <= 0) break;
         if constexpr (TYPE != TYPE_I8) {
             if (P.residual) {
-                v4i r[SLOTS * MOVES];
+                const T* const res = static_cast<const T*>(P.residual) + mw * P.ld_res + c_mv;
+                if (whole) {
+                    v4i r[SLOTS * MOVES];
 #pragma unroll
-                for (int i = 0; i < SLOTS * MOVES; ++i) {
-                    const int row = MV_ROWS * i + mv_row, n = N - (wc0 + CK::E * mv_ch);
-                    r[i] = v4i{0, 0, 0, 0};
-                    if (row < left && n > 0)
-                        r[i] = CK::load(static_cast<const T*>(P.residual) + (mw + row) * P.ld_res + wc0 + CK::E * mv_ch, n);
-                }
+                    for (int i = 0; i < SLOTS * MOVES; ++i) r[i] = CK::load(res + min(MV_ROWS * i + mv_row, left - 1) * P.ld_res, CK::E);
 #pragma unroll
-                for (int i = 0; i < SLOTS * MOVES; ++i) {
-                    const int row = MV_ROWS * i + mv_row;
-                    *reinterpret_cast<v4i*>(own + row * RB + 16 * (mv_ch ^ swz(row))) = r[i];
+                    for (int i = 0; i < SLOTS * MOVES; ++i) *reinterpret_cast<v4i*>(at_mv(i)) = r[i];
+                } else {
+#pragma unroll 1
+                    for (int i = 0; i < SLOTS * MOVES; ++i)
+                        *reinterpret_cast<v4i*>(at_mv(i)) = CK::load(res + min(MV_ROWS * i + mv_row, left - 1) * P.ld_res, N - c_mv);
                 }
                 __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
                 __builtin_amdgcn_wave_barrier();
@@ -370,61 +374,92 @@ __global__ __launch_bounds__((64 * GM * GN), (GM * GN == 4 && MT * NT == 16 ? 1 
         });
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
+        T* const y = static_cast<T*>(P.y) + mw * P.ldy + c_mv;
+        if (whole) {
 #pragma unroll
-        for (int i = 0; i < SLOTS * MOVES; ++i) {
-            const int row = MV_ROWS * i + mv_row, n = N - (wc0 + CK::E * mv_ch);
-            const v4i v = *reinterpret_cast<const v4i*>(own + row * RB + 16 * (mv_ch ^ swz(row)));
-            if (row < left && n > 0) CK::store(static_cast<T*>(P.y) + (mw + row) * P.ldy + wc0 + CK::E * mv_ch, v, n);
+            for (int i = 0; i < SLOTS * MOVES; ++i) {
+                const v4i v = *reinterpret_cast<const v4i*>(at_mv(i));
+                if (MV_ROWS * i + mv_row < left) CK::store(y + (MV_ROWS * i + mv_row) * P.ldy, v, CK::E);
+            }
+        } else {
+#pragma unroll 1
+            for (int i = 0; i < SLOTS * MOVES; ++i) {
+                const v4i v = *reinterpret_cast<const v4i*>(at_mv(i));
+                if (MV_ROWS * i + mv_row < left) CK::store(y + (MV_ROWS * i + mv_row) * P.ldy, v, N - c_mv);
+            }
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
     }
 }
 
-int64_t g_h = 4;
+constexpr int64_t kBand = 4;                   // rows of tiles in a band
 template <int TYPE, int MT, int NT, int GM, int GN, int S, int BK = 128> hipError_t launch_tile(hipStream_t s, const ScaledArgs& a) {
     using TL = GsTile<MT, NT, GM, GN, BK>;
     GsParams P;
     P.x = a.x; P.x_scale = a.x_scale; P.w = a.w; P.w_scale = a.w_scale; P.bias = a.bias; P.residual = a.residual; P.y = a.y;
     P.ldx = a.ldx; P.ld_res = a.ld_res; P.ldy = a.ldy; P.M = a.M; P.N = a.N; P.K = a.K; P.act = a.act; P.one_scale = a.one_scale;
-    P.inv_step = a.y_type == TYPE_I8 ? 1.0f / a.y_step : 0.0f;
+    P.inv_step = a.inv_step;
     const int64_t tm = (a.M + TL::TM - 1) / TL::TM, tn = (a.N + TL::TN - 1) / TL::TN, grid = (tm * tn + NXCD - 1) / NXCD * NXCD;
     if (grid > 0x7fffffffLL) return hipErrorInvalidValue;
-    P.order = TileOrder((uint32_t)tm, (uint32_t)tn, (uint32_t)(tm < g_h ? tm : g_h));
+    P.order = TileOrder((uint32_t)tm, (uint32_t)tn, (uint32_t)(tm < kBand ? tm : kBand));
     hipLaunchKernelGGL((gemm_scaled_kernel<TYPE, MT, NT, GM, GN, S, BK>), dim3((unsigned)grid), dim3(64 * TL::W), 0, s, P);
     return hipGetLastError();
 }
 
-int force_tile = -1;
-template <int TYPE> hipError_t launch_type(hipStream_t s, const ScaledArgs& a) {
-    const int64_t tiles = ((a.M + 63) / 64) * (((int64_t)a.N + 63) / 64), cus = num_cus();
-    int f = force_tile;
-    if (f < 0) f = tiles <= 3 * cus ? 0 : tiles <= 12 * cus ? 1 : 2;
-    switch (f) {
-        case 0: return launch_tile<TYPE, 1, 1, 2, 2, 3>(s, a);
-        case 1: return launch_tile<TYPE, 2, 2, 2, 2, 2>(s, a);
-        case 2: return launch_tile<TYPE, 4, 2, 2, 4, 2>(s, a);
-        case 3: return launch_tile<TYPE, 4, 4, 2, 2, 2>(s, a);
-        case 4: return launch_tile<TYPE, 1, 1, 4, 2, 4>(s, a);
-        case 5: return launch_tile<TYPE, 2, 1, 2, 4, 3>(s, a);
-        case 6: return launch_tile<TYPE, 4, 4, 2, 2, 4, 64>(s, a);
-        case 8: return launch_tile<TYPE, 4, 2, 2, 4, 4, 64>(s, a);
-        default: return launch_tile<TYPE, 2, 2, 4, 2, 3>(s, a);
+// Which tile.  us measured on 256 CUs, bf16 results, inputs in turn.
+enum Form { ROWS, T64, T128X64, T128X8, T256X128, T256, T128 };
+Form form_of(const ScaledArgs& a) {
+    const int64_t cus = num_cus();
+    auto tiles = [&](int64_t m, int64_t n) { return ((a.M + m - 1) / m) * ((a.N + n - 1) / n); };
+    auto rounds = [&](int64_t m, int64_t n, int64_t per_cu) { return (tiles(m, n) + per_cu * cus - 1) / (per_cu * cus); };
+    // Few rows: the kernel whose wavefronts split K, while two of its 32 x 32 tiles a CU take the shape (that kernel's and 64 x 64:
+    // 64 x 4096 x 4096 6.6 and 11.1, 128 x 4096 x 4096 8.7 and 11.2, 394 x 384 x 384 3.0 and 3.4, 788 x 384 x 1536 5.2 and 5.1; three a CU:
+    // 64 x 11008 x 4096 14.4 and 12.1, 394 x 1536 x 384 4.7 and 3.6), and for up to 32 rows always (16 x 32000 x 4096 28.0 and 33.7).
+    if (a.M <= 32 || rounds(32, 32, 2) <= 1) return ROWS;
+    // Rows of 768 bytes and more: the smallest tile that gives every CU at most one workgroup (64 x 64, 128 x 64, 128 x 128, 256 x 128,
+    // 256 x 256: 1024 x 1024 x 1024 4.6, 5.4, 6.8; 512 x 4096 x 4096 16.1, 14.8, 18.4; 1024 x 4096 x 4096 34, 26, 21.8, 25.7; 512 x 11008 x
+    // 4096 44, 37, 36, 27.7, 41; 1024 x 11008 x 4096 -, -, 56, 54, 46.7).  Shorter rows gain nothing by it (1576 x 1536 x 384 6.1, 9.1, 7.2).
+    if (a.K >= 768) {
+        if (tiles(64, 64) <= cus) return T64;
+        if (tiles(128, 64) <= cus) return T128X64;
+        if (tiles(128, 128) <= cus) return T128X8;
+        if (tiles(256, 128) <= cus) return T256X128;
+        // A round of 256 x 256 (one a CU) against one of 128 x 128 (two a CU, half the work): 62 and 36 at K = 4096; 8192 x 8192 x 4096
+        // 248 and 290, 4096 x 16384 x 4096 247 and 301; with 1024 bytes of K the gain is gone (50432 x 768 x 768 54.4 and 54.6).
+        if (rounds(256, 256, 1) * 10 <= rounds(128, 128, 2) * 6) return T256;
+        return T128;
+    }
+    // up to three 64 x 64 tiles a CU, and where 128 channels would be half padding: 64 x 64 (1576 x 1536 x 384 6.1 and 8.2 with 128 x 128, 3152 x
+    // 1536 x 384, 4.7 tiles a CU, 8.1 and 7.9; 300000 x 64 x 64 16.1 and 22.5)
+    if (rounds(64, 64, 3) <= 1 || a.N <= 64) return T64;
+    return T128;
+}
+
+template <int TYPE> hipError_t launch_type(hipStream_t s, const ScaledArgs& a, Form form) {
+    switch (form) {
+        case T64: return launch_tile<TYPE, 1, 1, 2, 2, 3>(s, a);
+        case T128X64: return launch_tile<TYPE, 1, 1, 4, 2, 4>(s, a);
+        case T128X8: return launch_tile<TYPE, 2, 1, 2, 4, 3>(s, a);
+        case T256X128: return launch_tile<TYPE, 2, 2, 4, 2, 3>(s, a);
+        case T256: return launch_tile<TYPE, 4, 2, 2, 4, 2>(s, a);
+        default: return launch_tile<TYPE, 2, 2, 2, 2, 2>(s, a);
     }
 }
 
 }  // namespace
-extern "C" void ivit_dbg_force_tile(int f) { force_tile = f < 0 ? -1 : f % 100; g_h = f >= 100 ? f / 100 : 4; }
 
 hipError_t launch_linear_scaled(hipStream_t s, const ScaledArgs& a) {
     if (a.M == 0) return hipSuccess;
     TraceScope trace(s, KIND_GEMM_SCALED, 2 * a.M * a.N * a.K,
                      a.M * a.K + (int64_t)a.N * a.K + a.M * a.N * element_bytes(a.y_type) * (a.residual ? 2 : 1));
+    const Form form = form_of(a);
+    if (form == ROWS) return launch_linear_scaled_rows(s, a);
     switch (a.y_type) {
-        case TYPE_F16: return launch_type<TYPE_F16>(s, a);
-        case TYPE_BF16: return launch_type<TYPE_BF16>(s, a);
-        case TYPE_I8: return launch_type<TYPE_I8>(s, a);
-        default: return launch_type<TYPE_F32>(s, a);
+        case TYPE_F16: return launch_type<TYPE_F16>(s, a, form);
+        case TYPE_BF16: return launch_type<TYPE_BF16>(s, a, form);
+        case TYPE_I8: return launch_type<TYPE_I8>(s, a, form);
+        default: return launch_type<TYPE_F32>(s, a, form);
     }
 }
 

@@ -109,9 +109,10 @@ struct GatedArgs { const void* x; int8_t* y; float* y_scale; int64_t ldx, ldy, r
 hipError_t launch_gated(hipStream_t s, const GatedArgs& a);
 struct ScaledArgs {
     const int8_t* x; const float* x_scale; const int8_t* w; const float* w_scale; const float* bias; const void* residual; void* y;
-    int64_t ldx, ld_res, ldy, M; int N, K, act, y_type; bool one_scale; float y_step;
+    int64_t ldx, ld_res, ldy, M; int N, K, act, y_type; bool one_scale; float inv_step;
 };
 hipError_t launch_linear_scaled(hipStream_t s, const ScaledArgs& a);
+hipError_t launch_linear_scaled_rows(hipStream_t s, const ScaledArgs& a);      // few rows (gemm_scaled_rows.hip)
 
 // Number of compute units of the current device (cached); used to size persistent grids.
 int num_cus();
