@@ -450,7 +450,7 @@ int ivit_rmsnorm_quant(void* stream, const void* x, int64_t ldx, const void* res
  * or NULL.  y [M, N] of y_type; residual [M, N] of y_type or NULL.  y_type == IVIT_I8: y = clamp8(round(act(..) / y_step)),
  * without a residual (y_step is ignored otherwise; a NaN gives 0).  residual may be y itself (same pointer and leading
  * dimension); no other overlap.
- * Requirements: 0 <= M < 2^31, N >= 1, 16 <= K <= 65536, K % 16 == 0; x and w 16-byte aligned; y_step a normal number whose
+ * Requirements: 0 <= M < 2^31, 1 <= N <= 2^24, 16 <= K <= 65536, K % 16 == 0; x and w 16-byte aligned; y_step a normal number whose
  * reciprocal is one too.
  * Errors: NULL, SHAPE, PARAM (act, y_type, y_step, a residual with IVIT_I8), ALIGN, HIP. */
 int ivit_linear_scaled(void* stream, const int8_t* x, int64_t ldx, const float* x_scale, int32_t one_scale,

@@ -577,13 +577,15 @@ def ivit_forward_swin(patches, logits, params, B, workspace, stream=None):
 # ------------------------------------------------------------------ float layers around int8 products
 ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3, "gelu_tanh": 4, "gelu_sigmoid": 5}
 _TYPES = None           # torch dtype -> ivit_type (torch is imported by the first call)
-_FLOAT32 = _INT8 = None
+_FLOAT32 = _INT8 = _current_device = _raw_stream = None
 
 
 def _setup():
-    global _TYPES, _FLOAT32, _INT8
+    global _TYPES, _FLOAT32, _INT8, _current_device, _raw_stream
     import torch
-    _FLOAT32, _INT8 = torch.float32, torch.int8
+    _FLOAT32, _INT8, _current_device = torch.float32, torch.int8, torch.cuda.current_device
+    # the handle alone, where torch has it: making a Stream object for it costs more than a launch
+    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
     _TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2, torch.int8: 3}
 
 
@@ -619,12 +621,11 @@ def _launch_stream(stream, device, where):
     """The stream of a call on tensors of this device, which has to be the current one (a kernel is launched there)."""
     if device < 0:
         raise ValueError("%s: tensors have to be on a GPU" % where)
-    import torch
-    current = torch.cuda.current_device()
+    current = _current_device()
     if current != device:
         raise ValueError("%s: tensors on device %d, but device %d is the current one" % (where, device, current))
     if stream is None:
-        return torch.cuda.current_stream(device).cuda_stream
+        return _raw_stream(device)
     if not isinstance(stream, int) and stream.device_index != device:
         raise ValueError("%s: tensors on device %d, a stream of device %d" % (where, device, stream.device_index))
     return _stream(stream)

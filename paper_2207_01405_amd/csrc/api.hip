@@ -725,8 +725,7 @@ int ivit_linear_scaled(void* stream, const int8_t* x, int64_t ldx, const float* 
                        int64_t ldy, int32_t y_type, float y_step, int64_t M, int32_t N, int32_t K) {
     if (act < IVIT_ACT_NONE || act > IVIT_ACT_GELU_SIGMOID || y_type < IVIT_F32 || y_type > IVIT_I8) return IVIT_ERR_PARAM;
     if (y_type == IVIT_I8 && (residual || !std::isnormal(y_step) || !(y_step > 0.0f) || !std::isnormal(1.0f / y_step))) return IVIT_ERR_PARAM;
-    if (M < 0 || M > 0x7fffffffLL || N < 1 || K < 16 || K > 65536 || (K & 15)) return IVIT_ERR_SHAPE;
-    if ((M + 31) / 32 * (((int64_t)N + 31) / 32) > 0x7fffffffLL) return IVIT_ERR_SHAPE;       // (tiles are counted in 32 bits)
+    if (M < 0 || M > 0x7fffffffLL || N < 1 || N > (1 << 24) || K < 16 || K > 65536 || (K & 15)) return IVIT_ERR_SHAPE;
     if (!w || !w_scale) return IVIT_ERR_NULL;
     if (M > 0 && (!x || !x_scale || !y)) return IVIT_ERR_NULL;             // an empty tensor may have no storage
     if (!aligned(w, 16) || !aligned(w_scale, 4) || !aligned(bias, 4)) return IVIT_ERR_ALIGN;

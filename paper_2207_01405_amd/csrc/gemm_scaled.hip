@@ -401,7 +401,6 @@ template <int TYPE, int MT, int NT, int GM, int GN, int S, int BK = 128> hipErro
     P.ldx = a.ldx; P.ld_res = a.ld_res; P.ldy = a.ldy; P.M = a.M; P.N = a.N; P.K = a.K; P.act = a.act; P.one_scale = a.one_scale;
     P.inv_step = a.inv_step;
     const int64_t tm = (a.M + TL::TM - 1) / TL::TM, tn = (a.N + TL::TN - 1) / TL::TN, grid = (tm * tn + NXCD - 1) / NXCD * NXCD;
-    if (grid > 0x7fffffffLL) return hipErrorInvalidValue;
     P.order = TileOrder((uint32_t)tm, (uint32_t)tn, (uint32_t)(tm < kBand ? tm : kBand));
     hipLaunchKernelGGL((gemm_scaled_kernel<TYPE, MT, NT, GM, GN, S, BK>), dim3((unsigned)grid), dim3(64 * TL::W), 0, s, P);
     return hipGetLastError();
@@ -455,12 +454,24 @@ hipError_t launch_linear_scaled(hipStream_t s, const ScaledArgs& a) {
                      a.M * a.K + (int64_t)a.N * a.K + a.M * a.N * element_bytes(a.y_type) * (a.residual ? 2 : 1));
     const Form form = form_of(a);
     if (form == ROWS) return launch_linear_scaled_rows(s, a);
-    switch (a.y_type) {
-        case TYPE_F16: return launch_type<TYPE_F16>(s, a, form);
-        case TYPE_BF16: return launch_type<TYPE_BF16>(s, a, form);
-        case TYPE_I8: return launch_type<TYPE_I8>(s, a, form);
-        default: return launch_type<TYPE_F32>(s, a, form);
+    // (a grid may have 2^32 threads; N is at most 2^24)
+    const int64_t most = 64 * (((int64_t)1 << 22) / ((a.N + 63) / 64)), e = element_bytes(a.y_type);
+    for (int64_t m = 0; m < a.M; m += most) {
+        ScaledArgs b = a;
+        b.x += m * a.ldx; b.M = min64(a.M - m, most);
+        if (!a.one_scale) b.x_scale += m;
+        if (a.residual) b.residual = static_cast<const int8_t*>(a.residual) + m * a.ld_res * e;
+        b.y = static_cast<int8_t*>(a.y) + m * a.ldy * e;
+        hipError_t st;
+        switch (a.y_type) {
+            case TYPE_F16: st = launch_type<TYPE_F16>(s, b, form); break;
+            case TYPE_BF16: st = launch_type<TYPE_BF16>(s, b, form); break;
+            case TYPE_I8: st = launch_type<TYPE_I8>(s, b, form); break;
+            default: st = launch_type<TYPE_F32>(s, b, form);
+        }
+        if (st != hipSuccess) return st;
     }
+    return hipSuccess;
 }
 
 }  // namespace ivit

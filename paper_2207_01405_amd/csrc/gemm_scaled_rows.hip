@@ -184,7 +184,6 @@ __global__ __launch_bounds__(64 * W) void gemm_scaled_rows_kernel(ScaledArgs P, 
 template <int CT, int XT, int D> hipError_t launch(hipStream_t s, const ScaledArgs& a) {
     const int steps = (a.K + 127) / 128, count = (steps + W - 1) / W;
     const int64_t tn = (a.N + 16 * CT - 1) / (16 * CT), tiles = (a.M + 8 * XT - 1) / (8 * XT) * tn;
-    if (tiles > 0x7fffffffLL) return hipErrorInvalidValue;
     hipLaunchKernelGGL((gemm_scaled_rows_kernel<CT, XT, D>), dim3((unsigned)tiles), dim3(64 * W), 0, s, a, steps, count, FastDiv((uint32_t)tn));
     return hipGetLastError();
 }

@@ -38,7 +38,7 @@ __device__ __forceinline__ int32_t clamp8_sum(int32_t a, int32_t b) { return cla
 
 // 64-bit minimum / maximum as a compare and a select (the min / max templates of the HIP headers, instantiated for
 // int64_t, go through double precision).
-__device__ __forceinline__ int64_t min64(int64_t a, int64_t b) { return a < b ? a : b; }
+__host__ __device__ __forceinline__ int64_t min64(int64_t a, int64_t b) { return a < b ? a : b; }
 __device__ __forceinline__ int64_t max64(int64_t a, int64_t b) { return a > b ? a : b; }
 
 // (b v + rnd 2^(c-1)) >> c with the full 64-bit product; any 1 <= c <= 62.  rnd = 1: round(b v / 2^c) half up (Eq. 8

@@ -192,16 +192,25 @@ __global__ __launch_bounds__(BLOCK) void gated_kernel(GateParams P) {
         if (p[v].twice < 8) store_q(P.y + row * P.ldy + p[v].at, h[v], q, SHORT ? C : 8);
 }
 
-// f(NV, TPR, BLOCK, SHORT) for rows of C elements: the fewest threads a row that hold it in a few pieces each
-template <class F> hipError_t with_group(int C, F&& f) {
+// f(NV, TPR, BLOCK, SHORT) for rows of C elements.  Many rows: as few threads a row as hold it in up to three pieces each, so that hardly
+// a thread is idle, and a workgroup for every wavefront (bf16 norms with a residual, us: 25216 x 384 13.6, with four wavefronts a workgroup
+// 15.2; 25216 x 768 28.3, with 256 threads a row 49.9; 20000 x 1536, activation alone, 30.9 and 36.9); from 1537 to 2048 elements 256 threads
+// have one piece each (10000 x 2048 29.9, with 64 threads 32.0; 5003 x 2049 10.9 with 128 threads, 11.5 with 256).  Few rows, where a launch
+// is a chain of latencies: 256 threads from 513 elements on (197 x 1536, activation alone, 2.9 and 3.6).
+template <class F> hipError_t with_group(int64_t rows, int C, F&& f) {
     const int pieces = (C + 7) / 8;
 #define IVIT_GROUP(nv, tpr, block, s) f(std::integral_constant<int, nv>(), std::integral_constant<int, tpr>(), std::integral_constant<int, block>(), std::integral_constant<bool, s>())
-    if (C < 8) return IVIT_GROUP(1, 8, 256, true);
-    if (pieces <= 8) return IVIT_GROUP(1, 8, 256, false);
-    if (pieces <= 16) return IVIT_GROUP(1, 16, 256, false);
-    if (pieces <= 32) return IVIT_GROUP(1, 32, 256, false);
-    if (pieces <= 64) return IVIT_GROUP(1, 64, 256, false);
+    if (C < 8) return IVIT_GROUP(1, 8, 64, true);
+    if (pieces <= 8) return IVIT_GROUP(1, 8, 64, false);
+    if (pieces <= 16) return IVIT_GROUP(1, 16, 64, false);
+    if (pieces <= 32) return IVIT_GROUP(1, 32, 64, false);
+    if (pieces <= 64) return IVIT_GROUP(1, 64, 64, false);
+    if (pieces <= 192 && rows > 2 * num_cus()) {
+        if (pieces <= 128) return IVIT_GROUP(2, 64, 64, false);
+        return IVIT_GROUP(3, 64, 64, false);
+    }
     if (pieces <= 256) return IVIT_GROUP(1, 256, 256, false);
+    if (pieces <= 320) return IVIT_GROUP(3, 128, 128, false);
     if (pieces <= 512) return IVIT_GROUP(2, 256, 256, false);
     if (pieces <= 1024) return IVIT_GROUP(4, 256, 256, false);
     if (pieces <= 2048) return IVIT_GROUP(2, 1024, 1024, false);
@@ -209,27 +218,46 @@ template <class F> hipError_t with_group(int C, F&& f) {
 #undef IVIT_GROUP
 }
 
+// Rows of one launch: a grid may have 2^32 threads.
+constexpr int64_t kThreads = (int64_t)1 << 31;
+
 template <class T> hipError_t norm_of(hipStream_t s, const RmsNormArgs& a) {
-    return with_group(a.C, [&](auto nv, auto tpr, auto block, auto few) {
+    return with_group(a.rows, a.C, [&](auto nv, auto tpr, auto block, auto few) {
         constexpr int NV = nv, TPR = tpr, BLOCK = block, ROWS = BLOCK / TPR;
         constexpr bool SHORT = few;
-        const NormParams P{a.x, a.residual, a.gamma, a.sum, a.y, a.y_scale, a.ldx, a.ld_res, a.ld_sum, a.ldy, a.rows, a.C, a.eps};
-        const dim3 grid((unsigned)((a.rows + ROWS - 1) / ROWS));
-        if (a.y_scale) hipLaunchKernelGGL((rmsnorm_kernel<T, NV, TPR, BLOCK, true, SHORT>), grid, dim3(BLOCK), 0, s, P);
-        else hipLaunchKernelGGL((rmsnorm_kernel<T, NV, TPR, BLOCK, false, SHORT>), grid, dim3(BLOCK), 0, s, P);
-        return hipGetLastError();
+        constexpr int64_t MOST = kThreads / BLOCK * ROWS;
+        for (int64_t r = 0; r < a.rows; r += MOST) {
+            auto at = [&](const void* p, int64_t ld) { return p ? static_cast<const T*>(p) + r * ld : nullptr; };
+            const int64_t rows = min64(a.rows - r, MOST), grid = (rows + ROWS - 1) / ROWS;
+            NormParams P{at(a.x, a.ldx), at(a.residual, a.ld_res), a.gamma, const_cast<T*>(at(a.sum, a.ld_sum)), nullptr, nullptr,
+                         a.ldx, a.ld_res, a.ld_sum, a.ldy, rows, a.C, a.eps};
+            if (a.y_scale) {
+                P.y = static_cast<int8_t*>(a.y) + r * a.ldy;
+                P.scale = a.y_scale + r;
+                hipLaunchKernelGGL((rmsnorm_kernel<T, NV, TPR, BLOCK, true, SHORT>), dim3((unsigned)grid), dim3(BLOCK), 0, s, P);
+            } else {
+                P.y = const_cast<T*>(at(a.y, a.ldy));
+                hipLaunchKernelGGL((rmsnorm_kernel<T, NV, TPR, BLOCK, false, SHORT>), dim3((unsigned)grid), dim3(BLOCK), 0, s, P);
+            }
+            if (hipError_t e = hipGetLastError()) return e;
+        }
+        return hipSuccess;
     });
 }
 
 template <class T> hipError_t gate_of(hipStream_t s, const GatedArgs& a) {
-    return with_group(a.C, [&](auto nv, auto tpr, auto block, auto few) {
+    return with_group(a.rows, a.C, [&](auto nv, auto tpr, auto block, auto few) {
         constexpr int NV = nv, TPR = tpr, BLOCK = block, ROWS = BLOCK / TPR;
         constexpr bool SHORT = few;
-        const GateParams P{a.x, a.y, a.y_scale, a.ldx, a.ldy, a.rows, a.C, a.act};
-        const dim3 grid((unsigned)((a.rows + ROWS - 1) / ROWS));
-        if (a.gated) hipLaunchKernelGGL((gated_kernel<T, NV, TPR, BLOCK, true, SHORT>), grid, dim3(BLOCK), 0, s, P);
-        else hipLaunchKernelGGL((gated_kernel<T, NV, TPR, BLOCK, false, SHORT>), grid, dim3(BLOCK), 0, s, P);
-        return hipGetLastError();
+        constexpr int64_t MOST = kThreads / BLOCK * ROWS;
+        for (int64_t r = 0; r < a.rows; r += MOST) {
+            const int64_t rows = min64(a.rows - r, MOST), grid = (rows + ROWS - 1) / ROWS;
+            const GateParams P{static_cast<const T*>(a.x) + r * a.ldx, a.y + r * a.ldy, a.y_scale + r, a.ldx, a.ldy, rows, a.C, a.act};
+            if (a.gated) hipLaunchKernelGGL((gated_kernel<T, NV, TPR, BLOCK, true, SHORT>), dim3((unsigned)grid), dim3(BLOCK), 0, s, P);
+            else hipLaunchKernelGGL((gated_kernel<T, NV, TPR, BLOCK, false, SHORT>), dim3((unsigned)grid), dim3(BLOCK), 0, s, P);
+            if (hipError_t e = hipGetLastError()) return e;
+        }
+        return hipSuccess;
     });
 }
 

@@ -439,6 +439,34 @@ def test_offsets_beyond_32_bits(ivit):
     check_dense(d, run_dense(ivit, d, "f32", "none"), "f32", "none", None, "x far apart")
 
 
+def test_rows_of_more_than_one_launch(ivit):
+    """More rows than one grid has threads for: 2^31 threads are 2^23 rows of 256 threads, 2^28 rows of x in tiles of 64 rows and 256 threads."""
+    import torch
+    rows, C = (1 << 23) + 9, 2048
+    at = torch.tensor([0, 1, (1 << 23) - 1, 1 << 23, rows - 1], device="cuda")
+    x = torch.zeros((rows, C), dtype=torch.bfloat16, device="cuda")
+    x[at] = rand(gen(1), at.numel(), C).to(x.dtype)
+    q, s = torch.full((rows, C), 77, dtype=torch.int8, device="cuda"), torch.full((rows,), 7.0, device="cuda")
+    ivit.ivit_rmsnorm_quant(x, None, q, s, 1e-6)
+    check_norm(x[at], None, None, 1e-6, "bf16", None, q[at], s[at], "norm of many rows")
+    assert int((s != 0).sum()) == at.numel() and int(torch.count_nonzero(s)) == at.numel()
+    q.fill_(77); s.fill_(7.0)
+    ivit.ivit_gated_quant(x, q, s, act="silu", gated=False)
+    a = x[at].double()
+    check_q(q[at], s[at], act64(a, "silu"), OPS * U * a.abs() + 2.0 ** -126, "gate of many rows")
+    assert int(torch.count_nonzero(s)) == at.numel()
+    del x, q, s
+    M = (1 << 28) + 100
+    d = dict(x=torch.zeros((M, 16), dtype=torch.int8, device="cuda"), x_scale=torch.rand(M, device="cuda"), bias=rand(gen(2), 16), residual=None,
+             w=torch.randint(-127, 128, (16, 16), device="cuda", dtype=torch.int8), w_scale=torch.rand(16, device="cuda"))
+    at = torch.tensor([0, 63, (1 << 28) - 1, 1 << 28, M - 1], device="cuda")
+    d["x"][at] = torch.randint(-127, 128, (at.numel(), 16), device="cuda", dtype=torch.int8)
+    y = run_dense(ivit, d, "i8", "none", 20.0)
+    check_dense(d, y, "i8", "none", 20.0, "many rows", rows=at)
+    base = (d["bias"] / 20.0).round().to(torch.int8)
+    assert int((y != base).any(1).sum()) <= at.numel()
+
+
 # -------------------------------------------------------------------------------------------------- streams, capture, together
 class Block:
     """One pre-norm encoder block of real scales around the integer attention, every intermediate kept."""

@@ -47,7 +47,7 @@ def test_dense_refusals(lib):
         assert dense(lib, **{k: None}) == E["NULL"], k
     assert dense(lib, M=-1) == E["SHAPE"] and dense(lib, M=1 << 31) == E["SHAPE"] and dense(lib, N=0) == E["SHAPE"]
     assert dense(lib, K=0) == E["SHAPE"] and dense(lib, K=24) == E["SHAPE"] and dense(lib, K=65552, ldx=65552) == E["SHAPE"]
-    assert dense(lib, M=(1 << 31) - 1, N=(1 << 31) - 1, ldy=(1 << 31) - 1) == E["SHAPE"]
+    assert dense(lib, N=(1 << 24) + 1, ldy=(1 << 24) + 1) == E["SHAPE"]
     assert dense(lib, ldx=48) == E["SHAPE"] and dense(lib, ldx=72) == E["SHAPE"] and dense(lib, ldx=(1 << 22) + 16) == E["SHAPE"]
     assert dense(lib, ldy=31) == E["SHAPE"] and dense(lib, ldy=1 << 31) == E["SHAPE"] and dense(lib, r=FAKE, ldr=31) == E["SHAPE"]
     assert dense(lib, act=-1) == E["PARAM"] and dense(lib, act=6) == E["PARAM"] and dense(lib, t=-1) == E["PARAM"] and dense(lib, t=4) == E["PARAM"]
