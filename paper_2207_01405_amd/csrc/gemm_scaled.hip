@@ -23,14 +23,11 @@ typedef float v4f __attribute__((ext_vector_type(4)));
 struct TileOrder {
     FastDiv band, full, last;                  // tiles of a band; its height; that of the last one
     uint32_t tiles, per_xcd, last_band;
-    __device__ __forceinline__ bool tile(uint32_t block, uint32_t& tm, uint32_t& tn) const {
-        const uint32_t t = (block % NXCD) * per_xcd + block / NXCD;
-        if (t >= tiles) return false;
+    __device__ __forceinline__ void tile(uint32_t t, uint32_t& tm, uint32_t& tn) const {
         uint32_t in, row;
         const uint32_t b = band.divide(t, in);
         tn = b == last_band ? last.divide(in, row) : full.divide(in, row);
         tm = b * full.d + row;
-        return true;
     }
     TileOrder() = default;
     TileOrder(uint32_t rows, uint32_t cols, uint32_t height)
@@ -91,7 +88,7 @@ template <int TYPE> struct Chunk {
 template <int MT, int NT, int GM, int GN, int BK> struct GsTile {
     static constexpr int W = GM * GN, TM = 32 * MT * GM, TN = 32 * NT * GN, LR = 1024 / BK;      // LR: rows a load instruction fills
     static_assert(TM % (LR * W) == 0 && TN % (LR * W) == 0, "a load instruction of all wavefronts fills rows of one operand");
-    static_assert(TN % 64 == 0 && TN / 64 <= W, "the constants of 64 channels a wavefront");
+    static_assert(TN % 64 == 0 && TN / 64 <= W && TM % 64 == 0 && TM / 64 <= W, "the constants of 64 channels or rows a wavefront");
 };
 
 template <int TYPE, int MT, int NT, int GM, int GN, int S, int BK>
@@ -100,64 +97,83 @@ __global__ __launch_bounds__((64 * GM * GN), (GM * GN == 4 && MT * NT == 16 ? 1 
     using T = Stored<TYPE>;
     constexpr int W = TL::W, TM = TL::TM, TN = TL::TN, LR = TL::LR, XI = TM / (LR * W), WI = TN / (LR * W), DP = XI + WI, STG = (TM + TN) * BK;
     constexpr int PC = BK / 16;                           // 16-byte pieces of a row of a stage
+    // PIPE: the tiles of four products a k-step and more; PERSIST: a workgroup goes on to its next tile, whose first stage comes in
+    // under the epilogue of the present one
+    constexpr bool PIPE = MT * NT >= 4, PERSIST = PIPE && S == 2;
     __shared__ __align__(16) int8_t lds[S * STG];
-    __shared__ __align__(16) float ws_s[TN], bias_s[TN];
+    __shared__ __align__(16) float ws_s[PERSIST ? 2 : 1][TN], bias_s[PERSIST ? 2 : 1][TN], xs_s[PERSIST ? 2 : 1][TM];
 
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int li = lane & 31, lg = lane >> 5, wm = wv / GN, wn = wv % GN;
+    const int wm = wv / GN, wn = wv % GN;
 
-    uint32_t tm, tn;
-    if (!P.order.tile(blockIdx.x, tm, tn)) return;
-    const int64_t m0 = (int64_t)tm * TM;
-    const int n0 = (int)tn * TN;
+    // each XCD takes a contiguous range of tiles, each of its workgroups every `slots`th of them
+    const uint32_t slots = gridDim.x / NXCD, end = min((blockIdx.x % NXCD + 1) * P.order.per_xcd, P.order.tiles);
+    uint32_t tile = (blockIdx.x % NXCD) * P.order.per_xcd + blockIdx.x / NXCD;
+    if (tile >= end) return;
     const int K = P.K, N = P.N;
-    const int rows = (int)min64(P.M - m0, TM);
-
-    // this lane's outputs: tokens row0 + 32 tt, channels n0 + cl + 16 ct .. + 15
-    const int row0 = wm * 32 * MT + li, cl = wn * 32 * NT + 16 * NT * lg;
-    if (wv < TN / 64) {                       // the channels' constants, 64 channels a wavefront
-        const uint32_t off = 4u * min(n0 + 64 * wv + lane, N - 1);
-        dma4(uniform_ptr(reinterpret_cast<const int8_t*>(P.w_scale)), off, lds_offset(reinterpret_cast<const int8_t*>(ws_s + 64 * wv)));
-        if (P.bias) dma4(uniform_ptr(reinterpret_cast<const int8_t*>(P.bias)), off, lds_offset(reinterpret_cast<const int8_t*>(bias_s + 64 * wv)));
-        else bias_s[64 * wv + lane] = 0.0f;
-    }
-    float xs[MT];
-#pragma unroll
-    for (int tt = 0; tt < MT; ++tt) xs[tt] = P.x_scale[P.one_scale ? 0 : m0 + min(row0 + 32 * tt, rows - 1)];
+    struct Place { int64_t m0; int n0, rows; };
+    auto place = [&](uint32_t t) __attribute__((always_inline)) {
+        uint32_t tm, tn;
+        P.order.tile(t, tm, tn);
+        const int64_t m0 = (int64_t)tm * TM;
+        return Place{m0, (int)tn * TN, (int)min64(P.M - m0, TM)};
+    };
 
     // (32-bit offsets from the tile's first row: 255 rows of at most 2^22 bytes)
     // Load instruction i of a wavefront fills LDS rows LR (W i + wavefront) + lane / PC, PC lanes a row; the lane lands in physical
     // piece p = lane % PC of row r and fetches piece p ^ mix(r).  Rows past the last token or channel repeat it (never stored),
     // pieces past the end of a row its last piece (never multiplied, see below).
     auto mix = [](int r) __attribute__((always_inline)) { return (r >> 1) & (PC - 1); };
-    const int ld_r = LR * wv + lane / PC, ld_col = 16 * ((lane % PC) ^ mix(ld_r));
-    const int8_t* xg = uniform_ptr(P.x + m0 * P.ldx);
-    const int8_t* wg = uniform_ptr(P.w + (int64_t)n0 * K);
+    // a copy of the lane's number that the compiler takes for another one at every use: what is formed from it anew for every tile would
+    // else be kept in registers all along
+    auto lane_now = [&]() __attribute__((always_inline)) {
+        int l = lane;
+        if (PERSIST) asm volatile("" : "+v"(l));
+        return l;
+    };
+    const int ld_col = 16 * ((lane % PC) ^ mix(LR * wv + lane / PC));
     uint32_t off[DP];
-#pragma unroll
-    for (int i = 0; i < DP; ++i) {
-        if (i < XI) {
-            off[i] = (uint32_t)min(LR * W * i + ld_r, rows - 1) * (uint32_t)P.ldx + ld_col;
-        } else {
-            // row 8 q + 4 g + r of MFMA tile ct holds channel 16 NT g + 16 ct + 4 q + r of the wavefront's 32 NT: that is
-            // accumulator register 4 q + r of lane group g
-            const int R = LR * W * (i - XI) + ld_r, ct = (R >> 5) % NT, rr = R & 31;
-            const int ch = (R / (32 * NT)) * 32 * NT + 16 * NT * ((rr >> 2) & 1) + 16 * ct + 4 * (rr >> 3) + (rr & 3);
-            off[i] = (uint32_t)min(ch, N - 1 - n0) * (uint32_t)K + ld_col;
-        }
-    }
+    v4i x_buf, w_buf;
+    int is = 0;
+    uint32_t k_off = 0;
     auto buffer = [](const int8_t* p) __attribute__((always_inline)) {
-        const uint64_t a = (uint64_t)p;
+        const uint64_t a = (uint64_t)uniform_ptr(p);
         return v4i{(int)(uint32_t)a, (int)(uint32_t)(a >> 32), (int)kTileBytes, 0x00020000};
     };
-    const v4i x_buf = buffer(xg), w_buf = buffer(wg);
+    // where the loads of a tile find their rows; the constants of its channels and rows, 64 a wavefront
+    auto aim = [&](const Place& at, int par) __attribute__((always_inline)) {
+        const int lane = lane_now(), ld_r = LR * wv + lane / PC, ld_col = 16 * ((lane % PC) ^ mix(ld_r));
+        if (wv < TN / 64) {
+            const uint32_t o = 4u * min(at.n0 + 64 * wv + lane, N - 1);
+            dma4(uniform_ptr(reinterpret_cast<const int8_t*>(P.w_scale)), o, lds_offset(reinterpret_cast<const int8_t*>(ws_s[par] + 64 * wv)));
+            if (P.bias) dma4(uniform_ptr(reinterpret_cast<const int8_t*>(P.bias)), o, lds_offset(reinterpret_cast<const int8_t*>(bias_s[par] + 64 * wv)));
+            else bias_s[par][64 * wv + lane] = 0.0f;
+        }
+        if (wv < TM / 64)
+            dma4(uniform_ptr(reinterpret_cast<const int8_t*>(P.x_scale + (P.one_scale ? 0 : at.m0))), P.one_scale ? 0u : 4u * min(64 * wv + lane, at.rows - 1),
+                 lds_offset(reinterpret_cast<const int8_t*>(xs_s[par] + 64 * wv)));
+#pragma unroll
+        for (int i = 0; i < DP; ++i) {
+            if (i < XI) {
+                off[i] = (uint32_t)min(LR * W * i + ld_r, at.rows - 1) * (uint32_t)P.ldx + ld_col;
+            } else {
+                // row 8 q + 4 g + r of MFMA tile ct holds channel 16 NT g + 16 ct + 4 q + r of the wavefront's 32 NT: that is
+                // accumulator register 4 q + r of lane group g
+                const int R = LR * W * (i - XI) + ld_r, ct = (R >> 5) % NT, rr = R & 31;
+                const int ch = (R / (32 * NT)) * 32 * NT + 16 * NT * ((rr >> 2) & 1) + 16 * ct + 4 * (rr >> 3) + (rr & 3);
+                off[i] = (uint32_t)min(ch, N - 1 - at.n0) * (uint32_t)K + ld_col;
+            }
+        }
+        x_buf = buffer(P.x + at.m0 * P.ldx);
+        w_buf = buffer(P.w + (int64_t)at.n0 * K);
+        is = 0;
+        k_off = 0;
+    };
     const int stages = (K + BK - 1) / BK, k_last = K - (stages - 1) * BK;      // bytes of K in the last stage: 16 .. BK
     const uint32_t lds0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)(lds_offset(lds) + wv * 1024));
     // A stage's loads: stage `is` goes to buffer is % S, known where the loads stand.  A lane whose piece lies past the end of
     // the rows moves back to the last one (the last stage only).  One scalar offset serves both operands.
     const int back = max(ld_col - (k_last - 16), 0), moves = k_last < BK ? stages - 1 : -1;
-    int is = 0;
-    uint32_t k_off = 0;
     auto issue = [&](auto buf_c) __attribute__((always_inline)) {
         if (is == moves) {
 #pragma unroll
@@ -170,25 +186,15 @@ __global__ __launch_bounds__((64 * GM * GN), (GM * GN == 4 && MT * NT == 16 ? 1 
         ++is;
         k_off += BK;
     };
-    // PIPE: the tiles of four products a k-step and more (see below)
-    constexpr bool PIPE = MT * NT >= 4;
-    static_for<PIPE ? S : S - 1>([&](auto buf) __attribute__((always_inline)) {
-        if (decltype(buf)::value < stages) issue(buf);
-    });
-
+    Place at = place(tile);
+    aim(at, 0);
+    if constexpr (PERSIST) {
+        issue(std::integral_constant<int, 0>());
+        wait_vm0();
+    }
     v16i acc[NT][MT];
-#pragma unroll
-    for (int ct = 0; ct < NT; ++ct)
-#pragma unroll
-        for (int tt = 0; tt < MT; ++tt) acc[ct][tt] = sums_from(0);
     constexpr int KS = BK / 32, AHEAD = MT * NT == 1 ? KS : 2;      // fragments are read AHEAD - 1 k-steps before their use
     int fx[KS], fw[KS];                                   // where this lane's fragments of k-step kk lie (buffer 0)
-#pragma unroll
-    for (int kk = 0; kk < KS; ++kk) {
-        const int col = 16 * ((2 * kk + lg) ^ mix(li));
-        fx[kk] = row0 * BK + col;
-        fw[kk] = (TM + wn * 32 * NT + li) * BK + col;
-    }
     struct Frag { v4i a[NT], b[MT]; };
     // fragment i of k-step kk, in the order of their use: the first of the weights, those of the tokens, the other ones
     auto read_one = [&](Frag& f, int i, int kk, int buf) __attribute__((always_inline)) {
@@ -206,7 +212,6 @@ __global__ __launch_bounds__((64 * GM * GN), (GM * GN == 4 && MT * NT == 16 ? 1 
             for (int tt = 0; tt < MT; ++tt) acc[ct][tt] = __builtin_amdgcn_mfma_i32_32x32x32_i8(f.a[ct], f.b[tt], acc[ct][tt], 0, 0, 0);
     };
     static_assert(S >= 2 && S <= 4 && (S - 1) * DP + 2 <= 63, "wait counts");
-    int s = 0;
     const int full = k_last == BK ? stages : stages - 1;  // a last stage of less than 128 bytes comes after the loop
     // all loads but those of the `left` stages requested last have arrived, and LDS reads returned, for everybody
     auto arrive_but = [&](int left) __attribute__((always_inline)) {
@@ -214,13 +219,37 @@ __global__ __launch_bounds__((64 * GM * GN), (GM * GN == 4 && MT * NT == 16 ? 1 
         else if (S <= 3 || left == 1) arrive<DP>();
         else arrive<2 * DP>();
     };
+#pragma unroll 1
+    for (int par = 0;; par ^= PERSIST) {
+    if constexpr (PERSIST) {                              // stage 0 has arrived; the other buffer served the last epilogue
+        __syncthreads();
+        if (1 < stages) issue(std::integral_constant<int, 1>());
+    } else {
+        static_for<PIPE ? S : S - 1>([&](auto buf) __attribute__((always_inline)) {
+            if (decltype(buf)::value < stages) issue(buf);
+        });
+    }
+#pragma unroll
+    for (int ct = 0; ct < NT; ++ct)
+#pragma unroll
+        for (int tt = 0; tt < MT; ++tt) acc[ct][tt] = sums_from(0);
+    int s = 0;
+    {
+        const int ln = lane_now(), li = ln & 31, lg = ln >> 5;
+#pragma unroll
+        for (int kk = 0; kk < KS; ++kk) {
+            const int col = 16 * ((2 * kk + lg) ^ mix(li));
+            fx[kk] = (wm * 32 * MT + li) * BK + col;
+            fw[kk] = (TM + wn * 32 * NT + li) * BK + col;
+        }
+    }
     if constexpr (PIPE) {
         // All S buffers are filled to begin with.  In front of the last k-step of stage s, whose fragments are in registers then, stage
         // s + 1 has to have arrived; behind the barrier there nobody reads stage s any more: its buffer takes stage s + S, and the first
         // fragments of stage s + 1 come under the products of that last k-step.  So no stage begins with a wait.  Reads and requests stand
         // one by one between the products: a wavefront issues in order, and eight reads at a stretch hold it for longer than a product takes.
         Frag f[2];
-        arrive_but(min(stages, S) - 1 >= S - 1 ? S - 1 : 0);
+        if constexpr (!PERSIST) arrive_but(stages >= S ? S - 1 : 0);
         read_frag(f[0], 0, 0);
         auto body = [&](auto buf_c, auto more_c) __attribute__((always_inline)) {
             constexpr int buf = decltype(buf_c)::value, nb = (buf + 1) % S;
@@ -292,7 +321,7 @@ __global__ __launch_bounds__((64 * GM * GN), (GM * GN == 4 && MT * NT == 16 ? 1 
             if (32 * kk >= k_last) return;
             Frag f;
             read_frag(f, kk, buf);
-            if (32 * kk + 16 >= k_last && lg) {
+            if (32 * kk + 16 >= k_last && lane >= 32) {
 #pragma unroll
                 for (int ct = 0; ct < NT; ++ct) f.a[ct] = v4i{0, 0, 0, 0};
             }
@@ -306,25 +335,44 @@ __global__ __launch_bounds__((64 * GM * GN), (GM * GN == 4 && MT * NT == 16 ? 1 
     // stands at c ^ swz(row), which spreads rows over the banks.
     using CK = Chunk<TYPE>;
     constexpr int RB = 32 * NT * (int)sizeof(T), CH = RB / 16, MINE = NT * (int)sizeof(T);     // bytes and chunks of a row; a lane's chunks
-    constexpr int REGION = S * STG / W / 1024 * 1024, FIT = REGION / (32 * RB), SLOTS = FIT >= MT && MT * RB <= 512 ? MT : 1;      // (at most 16 chunks of a residual in registers)
+    constexpr int REGION = (PERSIST ? STG : S * STG) / W / 1024 * 1024, FIT = REGION / (32 * RB), SLOTS = FIT >= MT && MT * RB <= 512 ? MT : FIT >= 2 && MT % 2 == 0 && RB <= 256 / 2 ? 2 : 1;      // (at most 16 chunks of a residual in registers)
     constexpr int MOVES = RB / 32;                        // instructions of 64 chunks that move a slot
     static_assert(FIT >= 1 && MT % SLOTS == 0, "room for 32 rows");
     auto swz = [](int r) __attribute__((always_inline)) { return CH >= 8 ? r & (CH - 1) : (r / (8 / CH)) & (CH - 1); };
     __syncthreads();                                      // (nobody reads operands any more)
-    int8_t* const own = lds + wv * REGION;
+    const bool more_tiles = PERSIST && tile + slots < end;
+    Place next = at;
+    if constexpr (PERSIST) {
+        if (more_tiles) {
+            next = place(tile + slots);
+            aim(next, par ^ 1);
+            issue(std::integral_constant<int, 0>());
+        }
+    }
+    const int64_t m0 = at.m0;
+    const int n0 = at.n0, rows = at.rows;
+    int8_t* const own = lds + (PERSIST ? STG : 0) + wv * REGION;
+    // this lane's results: tokens 32 MT wm + 32 tt + li, channels from cl on
+    const int lane_e = lane_now(), li = lane_e & 31, lg = lane_e >> 5, cl = wn * 32 * NT + 16 * NT * lg;
+    float xs[MT];
+#pragma unroll
+    for (int tt = 0; tt < MT; ++tt) xs[tt] = xs_s[par][wm * 32 * MT + li + 32 * tt];
     // chunk i of this lane when rows move: row MV_ROWS i + mv_row of the slots, channels from c_mv on
     constexpr int MV_ROWS = 64 / CH;
-    const int mv_row = lane / CH, c_mv = n0 + wn * 32 * NT + CK::E * (lane % CH);
+    const int mv_row = lane_e / CH, c_mv = n0 + wn * 32 * NT + CK::E * (lane_e % CH);
     const bool whole = n0 + (wn + 1) * 32 * NT <= N;      // (of all lanes) no channel of the wavefront's is past the last
     auto at_mv = [&](int i) __attribute__((always_inline)) {
         const int row = MV_ROWS * i + mv_row;
-        return own + row * RB + 16 * ((lane % CH) ^ swz(row));
+        return own + row * RB + 16 * ((lane_e % CH) ^ swz(row));
     };
 #pragma unroll 1
     for (int t0 = 0; t0 < MT; t0 += SLOTS) {
         const int64_t mw = m0 + wm * 32 * MT + 32 * t0;   // the first token of the slots
         const int left = rows - (wm * 32 * MT + 32 * t0); // tokens from there on
-        if (left <= 0) break;
+        if (left <= 0) {
+            if (PERSIST && t0 == 0) wait_vm0();
+            break;
+        }
         if constexpr (TYPE != TYPE_I8) {
             if (P.residual) {
                 const T* const res = static_cast<const T*>(P.residual) + mw * P.ld_res + c_mv;
@@ -350,7 +398,7 @@ __global__ __launch_bounds__((64 * GM * GN), (GM * GN == 4 && MT * NT == 16 ? 1 
                 typename CK::vf ws, bi;
 #pragma unroll
                 for (int e = 0; e < CK::E; e += 4) {
-                    const v4f a = *reinterpret_cast<const v4f*>(&ws_s[c + e]), b = *reinterpret_cast<const v4f*>(&bias_s[c + e]);
+                    const v4f a = *reinterpret_cast<const v4f*>(&ws_s[par][c + e]), b = *reinterpret_cast<const v4f*>(&bias_s[par][c + e]);
 #pragma unroll
                     for (int k = 0; k < 4; ++k) { ws[e + k] = a[k]; bi[e + k] = b[k]; }
                 }
@@ -374,6 +422,7 @@ __global__ __launch_bounds__((64 * GM * GN), (GM * GN == 4 && MT * NT == 16 ? 1 
         });
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
+        if (PERSIST && t0 == 0) wait_vm0();               // the next tile's first stage, before stores stand in line behind it
         T* const y = static_cast<T*>(P.y) + mw * P.ldy + c_mv;
         if (whole) {
 #pragma unroll
@@ -391,6 +440,10 @@ __global__ __launch_bounds__((64 * GM * GN), (GM * GN == 4 && MT * NT == 16 ? 1 
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
     }
+    if (!more_tiles) break;
+    at = next;
+    tile += slots;
+    }
 }
 
 constexpr int64_t kBand = 4;                   // rows of tiles in a band
@@ -400,8 +453,10 @@ template <int TYPE, int MT, int NT, int GM, int GN, int S, int BK = 128> hipErro
     P.x = a.x; P.x_scale = a.x_scale; P.w = a.w; P.w_scale = a.w_scale; P.bias = a.bias; P.residual = a.residual; P.y = a.y;
     P.ldx = a.ldx; P.ld_res = a.ld_res; P.ldy = a.ldy; P.M = a.M; P.N = a.N; P.K = a.K; P.act = a.act; P.one_scale = a.one_scale;
     P.inv_step = a.inv_step;
-    const int64_t tm = (a.M + TL::TM - 1) / TL::TM, tn = (a.N + TL::TN - 1) / TL::TN, grid = (tm * tn + NXCD - 1) / NXCD * NXCD;
+    const int64_t tm = (a.M + TL::TM - 1) / TL::TM, tn = (a.N + TL::TN - 1) / TL::TN;
+    int64_t grid = (tm * tn + NXCD - 1) / NXCD * NXCD;
     P.order = TileOrder((uint32_t)tm, (uint32_t)tn, (uint32_t)(tm < kBand ? tm : kBand));
+    if (MT * NT >= 4 && S == 2) grid = min64(grid, (int64_t)num_cus() * (TL::W == 4 ? 2 : 1) / NXCD * NXCD);     // (PERSIST)
     hipLaunchKernelGGL((gemm_scaled_kernel<TYPE, MT, NT, GM, GN, S, BK>), dim3((unsigned)grid), dim3(64 * TL::W), 0, s, P);
     return hipGetLastError();
 }
