@@ -67,9 +67,9 @@ template <int TYPE> struct Chunk {
         }
     }
     static __device__ __forceinline__ vf unpack(v4i v) { return __builtin_convertvector(__builtin_bit_cast(vt, v), vf); }
-    // the first n elements at p, which may have the alignment of one
-    static __device__ __forceinline__ v4i load(const T* p, int n) {
-        if (n >= E) return __builtin_bit_cast(v4i, (vt)*reinterpret_cast<const mem*>(p));
+    // the chunk at p, which may have the alignment of one element; of it n elements count, and `there` exist
+    static __device__ __forceinline__ v4i load(const T* p, int n, int64_t there) {
+        if (n >= E || there >= E) return __builtin_bit_cast(v4i, (vt)*reinterpret_cast<const mem*>(p));
         vt v = {};
 #pragma unroll
         for (int e = 0; e < E - 1; ++e)
@@ -132,7 +132,9 @@ __global__ __launch_bounds__((64 * GM * GN), (GM * GN == 4 && MT * NT == 16 ? 1 
         return l;
     };
     const int ld_col = 16 * ((lane % PC) ^ mix(LR * wv + lane / PC));
+    const int stages = (K + BK - 1) / BK, k_last = K - (stages - 1) * BK;      // bytes of K in the last stage: 16 .. BK
     uint32_t off[DP];
+    bool off_whole = false;
     v4i x_buf, w_buf;
     int is = 0;
     uint32_t k_off = 0;
@@ -152,6 +154,9 @@ __global__ __launch_bounds__((64 * GM * GN), (GM * GN == 4 && MT * NT == 16 ? 1 
         if (wv < TM / 64)
             dma4(uniform_ptr(reinterpret_cast<const int8_t*>(P.x_scale + (P.one_scale ? 0 : at.m0))), P.one_scale ? 0u : 4u * min(64 * wv + lane, at.rows - 1),
                  lds_offset(reinterpret_cast<const int8_t*>(xs_s[par] + 64 * wv)));
+        // (whole tiles have the same offsets from their first rows)
+        const bool whole = at.rows == TM && at.n0 + TN <= N && k_last == BK;
+        if (!(whole && off_whole))
 #pragma unroll
         for (int i = 0; i < DP; ++i) {
             if (i < XI) {
@@ -164,12 +169,12 @@ __global__ __launch_bounds__((64 * GM * GN), (GM * GN == 4 && MT * NT == 16 ? 1 
                 off[i] = (uint32_t)min(ch, N - 1 - at.n0) * (uint32_t)K + ld_col;
             }
         }
+        off_whole = whole;
         x_buf = buffer(P.x + at.m0 * P.ldx);
         w_buf = buffer(P.w + (int64_t)at.n0 * K);
         is = 0;
         k_off = 0;
     };
-    const int stages = (K + BK - 1) / BK, k_last = K - (stages - 1) * BK;      // bytes of K in the last stage: 16 .. BK
     const uint32_t lds0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)(lds_offset(lds) + wv * 1024));
     // A stage's loads: stage `is` goes to buffer is % S, known where the loads stand.  A lane whose piece lies past the end of
     // the rows moves back to the last one (the last stage only).  One scalar offset serves both operands.
@@ -211,16 +216,44 @@ __global__ __launch_bounds__((64 * GM * GN), (GM * GN == 4 && MT * NT == 16 ? 1 
 #pragma unroll
             for (int tt = 0; tt < MT; ++tt) acc[ct][tt] = __builtin_amdgcn_mfma_i32_32x32x32_i8(f.a[ct], f.b[tt], acc[ct][tt], 0, 0, 0);
     };
-    static_assert(S >= 2 && S <= 4 && (S - 1) * DP + 2 <= 63, "wait counts");
+    static_assert(S >= 2 && S <= 6 && (S - 1) * DP + 2 <= 63, "wait counts");
     const int full = k_last == BK ? stages : stages - 1;  // a last stage of less than 128 bytes comes after the loop
     // all loads but those of the `left` stages requested last have arrived, and LDS reads returned, for everybody
     auto arrive_but = [&](int left) __attribute__((always_inline)) {
         if (left <= 0) arrive<0>();
         else if (S <= 3 || left == 1) arrive<DP>();
-        else arrive<2 * DP>();
+        else if (S <= 4 || left == 2) arrive<2 * DP>();
+        else if (S <= 5 || left == 3) arrive<3 * DP>();
+        else arrive<4 * DP>();
     };
+    // The epilogue turns results over in LDS (see there), SLOTS times 32 tokens at once.
+    using CK = Chunk<TYPE>;
+    constexpr int RB = 32 * NT * (int)sizeof(T), CH = RB / 16, MINE = NT * (int)sizeof(T);     // bytes and chunks of a row; a lane's chunks
+    constexpr int REGION = (PERSIST ? STG : S * STG) / W / 1024 * 1024, FIT = REGION / (32 * RB), SLOTS = FIT >= MT && MT * RB <= 512 ? MT : FIT >= 2 && MT % 2 == 0 && RB <= 256 / 2 ? 2 : 1;      // (at most 16 chunks of a residual in registers)
+    constexpr int MOVES = RB / 32;                        // instructions of 64 chunks that move a slot
+    static_assert(FIT >= 1 && MT % SLOTS == 0, "room for 32 rows");
+    // chunk i of a lane when rows move: row MV_ROWS i + lane / CH of the slots, channels from E (lane % CH) on
+    constexpr int MV_ROWS = 64 / CH;
 #pragma unroll 1
     for (int par = 0;; par ^= PERSIST) {
+    constexpr bool EARLY = !PIPE && TYPE != TYPE_I8;      // a residual is requested first: such launches are a chain of latencies
+    v4i early[EARLY ? MT / SLOTS : 1][EARLY ? SLOTS * MOVES : 1];
+    // Where the last channels are not a whole chunk, what follows them, the next row's, is loaded with them; only behind the last row of all
+    // there may be nothing: (rows behind this one) ld + (channels from the chunk on) elements follow.
+    if constexpr (EARLY) {
+        if (P.residual) {
+            const int c = at.n0 + wn * 32 * NT + CK::E * (lane % CH);
+            const T* const res = static_cast<const T*>(P.residual) + at.m0 * P.ld_res + c;
+#pragma unroll
+            for (int p = 0; p < MT / SLOTS; ++p)
+#pragma unroll
+                for (int i = 0; i < SLOTS * MOVES; ++i) {
+                    const int row = min(wm * 32 * MT + 32 * SLOTS * p + MV_ROWS * i + lane / CH, at.rows - 1);
+                    early[p][i] = v4i{0, 0, 0, 0};
+                    if (c < N) early[p][i] = CK::load(res + row * P.ld_res, N - c, (P.M - 1 - at.m0 - row) * P.ld_res + N - c);
+                }
+        }
+    }
     if constexpr (PERSIST) {                              // stage 0 has arrived; the other buffer served the last epilogue
         __syncthreads();
         if (1 < stages) issue(std::integral_constant<int, 1>());
@@ -333,11 +366,6 @@ __global__ __launch_bounds__((64 * GM * GN), (GM * GN == 4 && MT * NT == 16 ? 1 
     // instruction would touch 64 lines and fill none.  So a wavefront turns its results over in LDS that it has for itself
     // (REGION bytes), SLOTS times 32 tokens at once, and lines leave whole; a residual comes in the same way.  Chunk c of a row
     // stands at c ^ swz(row), which spreads rows over the banks.
-    using CK = Chunk<TYPE>;
-    constexpr int RB = 32 * NT * (int)sizeof(T), CH = RB / 16, MINE = NT * (int)sizeof(T);     // bytes and chunks of a row; a lane's chunks
-    constexpr int REGION = (PERSIST ? STG : S * STG) / W / 1024 * 1024, FIT = REGION / (32 * RB), SLOTS = FIT >= MT && MT * RB <= 512 ? MT : FIT >= 2 && MT % 2 == 0 && RB <= 256 / 2 ? 2 : 1;      // (at most 16 chunks of a residual in registers)
-    constexpr int MOVES = RB / 32;                        // instructions of 64 chunks that move a slot
-    static_assert(FIT >= 1 && MT % SLOTS == 0, "room for 32 rows");
     auto swz = [](int r) __attribute__((always_inline)) { return CH >= 8 ? r & (CH - 1) : (r / (8 / CH)) & (CH - 1); };
     __syncthreads();                                      // (nobody reads operands any more)
     const bool more_tiles = PERSIST && tile + slots < end;
@@ -357,35 +385,40 @@ __global__ __launch_bounds__((64 * GM * GN), (GM * GN == 4 && MT * NT == 16 ? 1 
     float xs[MT];
 #pragma unroll
     for (int tt = 0; tt < MT; ++tt) xs[tt] = xs_s[par][wm * 32 * MT + li + 32 * tt];
-    // chunk i of this lane when rows move: row MV_ROWS i + mv_row of the slots, channels from c_mv on
-    constexpr int MV_ROWS = 64 / CH;
     const int mv_row = lane_e / CH, c_mv = n0 + wn * 32 * NT + CK::E * (lane_e % CH);
     const bool whole = n0 + (wn + 1) * 32 * NT <= N;      // (of all lanes) no channel of the wavefront's is past the last
     auto at_mv = [&](int i) __attribute__((always_inline)) {
         const int row = MV_ROWS * i + mv_row;
         return own + row * RB + 16 * ((lane_e % CH) ^ swz(row));
     };
-#pragma unroll 1
-    for (int t0 = 0; t0 < MT; t0 += SLOTS) {
+    auto pass = [&](auto t0_c) __attribute__((always_inline)) -> bool {      // false: no tokens from there on
+        constexpr int t0 = decltype(t0_c)::value;
         const int64_t mw = m0 + wm * 32 * MT + 32 * t0;   // the first token of the slots
         const int left = rows - (wm * 32 * MT + 32 * t0); // tokens from there on
         if (left <= 0) {
             if (PERSIST && t0 == 0) wait_vm0();
-            break;
+            return false;
         }
         if constexpr (TYPE != TYPE_I8) {
             if (P.residual) {
-                const T* const res = static_cast<const T*>(P.residual) + mw * P.ld_res + c_mv;
-                if (whole) {
-                    v4i r[SLOTS * MOVES];
+                if constexpr (EARLY) {
 #pragma unroll
-                    for (int i = 0; i < SLOTS * MOVES; ++i) r[i] = CK::load(res + min(MV_ROWS * i + mv_row, left - 1) * P.ld_res, CK::E);
-#pragma unroll
-                    for (int i = 0; i < SLOTS * MOVES; ++i) *reinterpret_cast<v4i*>(at_mv(i)) = r[i];
+                    for (int i = 0; i < SLOTS * MOVES; ++i) *reinterpret_cast<v4i*>(at_mv(i)) = early[EARLY ? t0 / SLOTS : 0][EARLY ? i : 0];
                 } else {
+                    const T* const res = static_cast<const T*>(P.residual) + mw * P.ld_res + c_mv;
+                    if (whole) {
+                        v4i r[SLOTS * MOVES];
+#pragma unroll
+                        for (int i = 0; i < SLOTS * MOVES; ++i) r[i] = CK::load(res + min(MV_ROWS * i + mv_row, left - 1) * P.ld_res, CK::E, CK::E);
+#pragma unroll
+                        for (int i = 0; i < SLOTS * MOVES; ++i) *reinterpret_cast<v4i*>(at_mv(i)) = r[i];
+                    } else if (c_mv < N) {
 #pragma unroll 1
-                    for (int i = 0; i < SLOTS * MOVES; ++i)
-                        *reinterpret_cast<v4i*>(at_mv(i)) = CK::load(res + min(MV_ROWS * i + mv_row, left - 1) * P.ld_res, N - c_mv);
+                        for (int i = 0; i < SLOTS * MOVES; ++i) {
+                            const int row = min(MV_ROWS * i + mv_row, left - 1);
+                            *reinterpret_cast<v4i*>(at_mv(i)) = CK::load(res + row * P.ld_res, N - c_mv, (P.M - 1 - mw - row) * P.ld_res + N - c_mv);
+                        }
+                    }
                 }
                 __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
                 __builtin_amdgcn_wave_barrier();
@@ -402,9 +435,8 @@ __global__ __launch_bounds__((64 * GM * GN), (GM * GN == 4 && MT * NT == 16 ? 1 
 #pragma unroll
                     for (int k = 0; k < 4; ++k) { ws[e + k] = a[k]; bi[e + k] = b[k]; }
                 }
-                static_for<MT>([&](auto tt_c) __attribute__((always_inline)) {
-                    constexpr int tt = decltype(tt_c)::value;
-                    if (tt < t0 || tt >= t0 + SLOTS) return;
+                static_for<SLOTS>([&](auto tt_c) __attribute__((always_inline)) {
+                    constexpr int tt = t0 + decltype(tt_c)::value;
                     int8_t* const at = own + (32 * (tt % SLOTS) + li) * RB + 16 * ((MINE * lg + j) ^ swz(li));
                     typename CK::vf v;
 #pragma unroll
@@ -439,7 +471,10 @@ __global__ __launch_bounds__((64 * GM * GN), (GM * GN == 4 && MT * NT == 16 ? 1 
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
-    }
+        return true;
+    };
+    bool on = true;
+    static_for<MT / SLOTS>([&](auto p) __attribute__((always_inline)) { if (on) on = pass(std::integral_constant<int, decltype(p)::value * SLOTS>()); });
     if (!more_tiles) break;
     at = next;
     tile += slots;
