@@ -422,7 +422,7 @@ int ivit_forward_swin(void* stream, const int8_t* patches, int8_t* logits, const
  *  - An int8 row q with scale s stands for s q.  s = max |v| / 127 and q = round(v / s) over the row's values v; a row of
  *    zeros has s = 0 and zeros, a row that holds a NaN or an infinite value (or whose largest leaves the range of
  *    float32) has s = NaN and zeros.
- *  - Results do not depend on the grid or the order in which anything ran: equal calls give equal bits. */
+ *  - Equal calls give equal bits; a row of ivit_linear_scaled comes out the same whatever rows are beside it. */
 typedef enum { IVIT_F32 = 0, IVIT_F16 = 1, IVIT_BF16 = 2, IVIT_I8 = 3 } ivit_type;
 
 /* Activations: x, max(x, 0), x sigma(x), x Phi(x), the tanh form of the former
@@ -436,7 +436,8 @@ typedef enum { IVIT_ACT_NONE = 0, IVIT_ACT_RELU = 1, IVIT_ACT_SILU = 2, IVIT_ACT
  * x, residual (nullable), sum (nullable) [rows, C] of `type`; gamma float32 [C], nullable (ones).  n is formed from h
  * before its rounding to `type`.  Result: y_scale != NULL: int8 rows y [rows, C] and their scales y_scale [rows]; y_scale
  * == NULL: n itself, of `type`.  A mean square beyond the range of float32 counts as infinite (n = 0 where h is finite).
- * sum may be x or residual themselves, and so may a y of `type` (the same pointer and leading dimension); no other overlap.
+ * sum may be x or residual themselves, and so may a y of `type` (the same pointer and leading dimension; not both the same one);
+ * no other overlap.
  * Requirements: 0 <= rows < 2^31, 1 <= C <= 32768, eps > 0 and finite.
  * Errors: NULL, SHAPE, PARAM (type, eps), ALIGN, HIP. */
 int ivit_rmsnorm_quant(void* stream, const void* x, int64_t ldx, const void* residual, int64_t ld_residual,

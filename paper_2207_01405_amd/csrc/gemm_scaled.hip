@@ -1,11 +1,17 @@
 // int8 x int8 -> int32 Dense on the gfx950 matrix cores with real scales and the epilogue of a float layer:
 //   y[m][n] = act(s_x[m] s_w[n] sum_k x[m][k] w[n][k] + bias[n]) + r[m][n]
 //
-// A workgroup of GM x GN wavefronts computes one tile of 32 MT GM tokens x 32 NT GN channels.  Both operands stream through S LDS
-// stages of 128 bytes of K, filled by LDS-direct loads S - 1 stages ahead (no register pass, one barrier per stage); the 16-byte
-// pieces of a row are permuted by an XOR with bits of the row number, so that the fragment reads are spread over the banks.  The
-// weights are the MFMA "A" operand and the loads put the channel rows in such an order that a lane ends up with 16 NT consecutive
-// channels of one token.
+// A workgroup of GM x GN wavefronts computes tiles of 32 MT GM tokens x 32 NT GN channels.  Both operands stream through S LDS
+// stages of 128 bytes of K, filled by LDS-direct loads (no register pass, one barrier per stage); the 16-byte pieces of a row are
+// permuted by an XOR with bits of the row number, so that the fragment reads are spread over the banks.  The weights are the MFMA "A"
+// operand and the loads put the channel rows in such an order that a lane ends up with 16 NT consecutive channels of one token.
+//
+// What bounds the tiles is LDS, 128 bytes a cycle and CU for fragment reads and arriving loads alike: a stage of two 128 x 128 tiles a CU is
+// 1536 cycles of it for 1024 of products and takes 0.99 us, one of 256 x 256 (eight wavefronts of 128 x 64) 2048 for 2048 and 1.57 us at the
+// 1.7 GHz that this card keeps up then.  8192 x 8192 x 4096 with bf16 results 245 us, 2.24 POP/s (a product alone from registers runs at 3.2
+// to 3.3 on random data), 8192 x 8192 x 8192 2.47; with the residual 277 us.  Tried for 256 x 256 and taken back: four wavefronts of 128 x 128,
+// a quarter less LDS (497 against 465 us at K = 8192, then 461 against 451); stages of 64 bytes, four of them (473 against 451: half lines);
+// the residual's lines requested into L2 during the last stages (286 against 281) or a pass ahead (290 against 286); wave priorities (no change).
 #include "linear_rows.hpp"
 #include "regst_common.hpp"
 #include "scaled_common.hpp"
@@ -17,6 +23,8 @@ using namespace regst;
 using namespace scaled;
 
 typedef float v4f __attribute__((ext_vector_type(4)));
+
+constexpr int BK = 128, LR = 1024 / BK, PC = BK / 16;      // bytes of K per stage; rows a load instruction fills; 16-byte pieces of a row
 
 // Tiles in bands of `height` rows of tiles, column by column within a band; each XCD takes a contiguous range of that order.  What
 // an XCD works on at one time is then a patch of the result about as high as wide, and its L2 takes in the fewest rows of either operand.
@@ -85,18 +93,17 @@ template <int TYPE> struct Chunk {
     }
 };
 
-template <int MT, int NT, int GM, int GN, int BK> struct GsTile {
-    static constexpr int W = GM * GN, TM = 32 * MT * GM, TN = 32 * NT * GN, LR = 1024 / BK;      // LR: rows a load instruction fills
+template <int MT, int NT, int GM, int GN> struct GsTile {
+    static constexpr int W = GM * GN, TM = 32 * MT * GM, TN = 32 * NT * GN;
     static_assert(TM % (LR * W) == 0 && TN % (LR * W) == 0, "a load instruction of all wavefronts fills rows of one operand");
     static_assert(TN % 64 == 0 && TN / 64 <= W && TM % 64 == 0 && TM / 64 <= W, "the constants of 64 channels or rows a wavefront");
 };
 
-template <int TYPE, int MT, int NT, int GM, int GN, int S, int BK>
-__global__ __launch_bounds__((64 * GM * GN), (GM * GN == 4 && MT * NT == 16 ? 1 : 2)) void gemm_scaled_kernel(GsParams P) {
-    using TL = GsTile<MT, NT, GM, GN, BK>;
+template <int TYPE, int MT, int NT, int GM, int GN, int S>
+__global__ __launch_bounds__((64 * GM * GN), 2) void gemm_scaled_kernel(GsParams P) {
+    using TL = GsTile<MT, NT, GM, GN>;
     using T = Stored<TYPE>;
-    constexpr int W = TL::W, TM = TL::TM, TN = TL::TN, LR = TL::LR, XI = TM / (LR * W), WI = TN / (LR * W), DP = XI + WI, STG = (TM + TN) * BK;
-    constexpr int PC = BK / 16;                           // 16-byte pieces of a row of a stage
+    constexpr int W = TL::W, TM = TL::TM, TN = TL::TN, XI = TM / (LR * W), WI = TN / (LR * W), DP = XI + WI, STG = (TM + TN) * BK;
     // PIPE: the tiles of four products a k-step and more; PERSIST: a workgroup goes on to its next tile, whose first stage comes in
     // under the epilogue of the present one
     constexpr bool PIPE = MT * NT >= 4, PERSIST = PIPE && S == 2;
@@ -216,274 +223,273 @@ __global__ __launch_bounds__((64 * GM * GN), (GM * GN == 4 && MT * NT == 16 ? 1 
 #pragma unroll
             for (int tt = 0; tt < MT; ++tt) acc[ct][tt] = __builtin_amdgcn_mfma_i32_32x32x32_i8(f.a[ct], f.b[tt], acc[ct][tt], 0, 0, 0);
     };
-    static_assert(S >= 2 && S <= 6 && (S - 1) * DP + 2 <= 63, "wait counts");
+    static_assert(S >= 2 && S <= 4 && (S - 1) * DP + 2 <= 63, "wait counts");
     const int full = k_last == BK ? stages : stages - 1;  // a last stage of less than 128 bytes comes after the loop
     // all loads but those of the `left` stages requested last have arrived, and LDS reads returned, for everybody
     auto arrive_but = [&](int left) __attribute__((always_inline)) {
         if (left <= 0) arrive<0>();
         else if (S <= 3 || left == 1) arrive<DP>();
-        else if (S <= 4 || left == 2) arrive<2 * DP>();
-        else if (S <= 5 || left == 3) arrive<3 * DP>();
-        else arrive<4 * DP>();
+        else arrive<2 * DP>();
     };
     // The epilogue turns results over in LDS (see there), SLOTS times 32 tokens at once.
     using CK = Chunk<TYPE>;
     constexpr int RB = 32 * NT * (int)sizeof(T), CH = RB / 16, MINE = NT * (int)sizeof(T);     // bytes and chunks of a row; a lane's chunks
-    constexpr int REGION = (PERSIST ? STG : S * STG) / W / 1024 * 1024, FIT = REGION / (32 * RB), SLOTS = FIT >= MT && MT * RB <= 512 ? MT : FIT >= 2 && MT % 2 == 0 && RB <= 256 / 2 ? 2 : 1;      // (at most 16 chunks of a residual in registers)
+    constexpr int REGION = (PERSIST ? STG : S * STG) / W / 1024 * 1024, FIT = REGION / (32 * RB);
+    constexpr int SLOTS = FIT >= MT && MT * RB <= 512 ? MT : FIT >= 2 && MT % 2 == 0 && RB <= 128 ? 2 : 1;     // (registers for a residual's chunks)
     constexpr int MOVES = RB / 32;                        // instructions of 64 chunks that move a slot
     static_assert(FIT >= 1 && MT % SLOTS == 0, "room for 32 rows");
     // chunk i of a lane when rows move: row MV_ROWS i + lane / CH of the slots, channels from E (lane % CH) on
     constexpr int MV_ROWS = 64 / CH;
 #pragma unroll 1
     for (int par = 0;; par ^= PERSIST) {
-    constexpr bool EARLY = !PIPE && TYPE != TYPE_I8;      // a residual is requested first: such launches are a chain of latencies
-    v4i early[EARLY ? MT / SLOTS : 1][EARLY ? SLOTS * MOVES : 1];
-    // Where the last channels are not a whole chunk, what follows them, the next row's, is loaded with them; only behind the last row of all
-    // there may be nothing: (rows behind this one) ld + (channels from the chunk on) elements follow.
-    if constexpr (EARLY) {
-        if (P.residual) {
-            const int c = at.n0 + wn * 32 * NT + CK::E * (lane % CH);
-            const T* const res = static_cast<const T*>(P.residual) + at.m0 * P.ld_res + c;
+        constexpr bool EARLY = !PIPE && TYPE != TYPE_I8;      // a residual is requested first: such launches are a chain of latencies
+        v4i early[EARLY ? MT / SLOTS : 1][EARLY ? SLOTS * MOVES : 1];
+        // Where the last channels are not a whole chunk, what follows them, the next row's, is loaded with them; only behind the last row of all
+        // there may be nothing: (rows behind this one) ld + (channels from the chunk on) elements follow.
+        if constexpr (EARLY) {
+            if (P.residual) {
+                const int c = at.n0 + wn * 32 * NT + CK::E * (lane % CH);
+                const T* const res = static_cast<const T*>(P.residual) + at.m0 * P.ld_res + c;
 #pragma unroll
-            for (int p = 0; p < MT / SLOTS; ++p)
+                for (int p = 0; p < MT / SLOTS; ++p)
+#pragma unroll
+                    for (int i = 0; i < SLOTS * MOVES; ++i) {
+                        const int row = min(wm * 32 * MT + 32 * SLOTS * p + MV_ROWS * i + lane / CH, at.rows - 1);
+                        early[p][i] = v4i{0, 0, 0, 0};
+                        if (c < N) early[p][i] = CK::load(res + row * P.ld_res, N - c, (P.M - 1 - at.m0 - row) * P.ld_res + N - c);
+                    }
+            }
+        }
+        if constexpr (PERSIST) {                              // stage 0 has arrived; the other buffer served the last epilogue
+            __syncthreads();
+            if (1 < stages) issue(std::integral_constant<int, 1>());
+        } else {
+            static_for<PIPE ? S : S - 1>([&](auto buf) __attribute__((always_inline)) {
+                if (decltype(buf)::value < stages) issue(buf);
+            });
+        }
+#pragma unroll
+        for (int ct = 0; ct < NT; ++ct)
+#pragma unroll
+            for (int tt = 0; tt < MT; ++tt) acc[ct][tt] = sums_from(0);
+        int s = 0;
+        {
+            const int ln = lane_now(), li = ln & 31, lg = ln >> 5;
+#pragma unroll
+            for (int kk = 0; kk < KS; ++kk) {
+                const int col = 16 * ((2 * kk + lg) ^ mix(li));
+                fx[kk] = (wm * 32 * MT + li) * BK + col;
+                fw[kk] = (TM + wn * 32 * NT + li) * BK + col;
+            }
+        }
+        if constexpr (PIPE) {
+            // All S buffers are filled to begin with.  In front of the last k-step of stage s, whose fragments are in registers then, stage
+            // s + 1 has to have arrived; behind the barrier there nobody reads stage s any more: its buffer takes stage s + S, and the first
+            // fragments of stage s + 1 come under the products of that last k-step.  So no stage begins with a wait.  Reads and requests stand
+            // one by one between the products: a wavefront issues in order, and eight reads at a stretch hold it for longer than a product takes.
+            Frag f[2];
+            if constexpr (!PERSIST) arrive_but(stages >= S ? S - 1 : 0);
+            read_frag(f[0], 0, 0);
+            auto body = [&](auto buf_c, auto more_c) __attribute__((always_inline)) {
+                constexpr int buf = decltype(buf_c)::value, nb = (buf + 1) % S;
+                constexpr bool MORE = decltype(more_c)::value;            // there is a stage s + S (false: maybe)
+                static_for<KS>([&](auto kk_c) __attribute__((always_inline)) {
+                    constexpr int kk = decltype(kk_c)::value;
+                    constexpr bool last = kk == KS - 1;
+                    if constexpr (last) {
+                        if constexpr (MORE) {
+                            arrive<(S - 2) * DP>();
+                            if (is == moves) {
+#pragma unroll
+                                for (int i = 0; i < DP; ++i) off[i] -= back;
+                            }
+                        } else if (s + 1 < stages) {
+                            arrive_but(min(stages - 2 - s, S - 2));
+                            if (is < stages) issue(buf_c);
+                        }
+                    }
+                    constexpr int READS = NT + MT, DO = READS + (last && MORE ? DP : 0), N_MUL = NT * MT;
+                    static_for<N_MUL>([&](auto i_c) __attribute__((always_inline)) {
+                        constexpr int i = decltype(i_c)::value, ct = i / MT, tt = i % MT;
+                        acc[ct][tt] = __builtin_amdgcn_mfma_i32_32x32x32_i8(f[kk & 1].a[ct], f[kk & 1].b[tt], acc[ct][tt], 0, 0, 0);
+                        constexpr int from = i * DO / N_MUL, to = (i + 1) * DO / N_MUL;
+                        static_for<to - from>([&](auto d_c) __attribute__((always_inline)) {
+                            constexpr int d = from + decltype(d_c)::value;
+                            if constexpr (d < READS) read_one(f[(kk + 1) & 1], d, last ? 0 : kk + 1, last ? nb : buf);
+                            else load_lds<buf * STG + (d - READS) * W * 1024>(d - READS < XI ? x_buf : w_buf, off[d - READS], k_off, lds0);
+                        });
+                        __builtin_amdgcn_sched_barrier(0);
+                    });
+                    if constexpr (last && MORE) { ++is; k_off += BK; }
+                });
+                ++s;
+            };
+            static_assert(KS % 2 == 0, "the first fragments of every stage go to the same registers");
+#pragma unroll 1
+            while (s + 2 * S <= stages)
+                static_for<S>([&](auto buf) __attribute__((always_inline)) { body(buf, std::true_type()); });
+#pragma unroll 1
+            while (s < full)
+                static_for<S>([&](auto buf) __attribute__((always_inline)) { if (s < full) body(buf, std::false_type()); });
+        } else {
+            // Stage s: its loads have arrived when at most those of the later stages requested so far (S - 2, fewer at the end)
+            // are outstanding; behind the barrier nobody reads stage s - 1 any more and its buffer takes stage s + S - 1.  Those
+            // loads go out behind the first fragment reads.
+            auto body = [&](auto buf_c) __attribute__((always_inline)) {
+                constexpr int buf = decltype(buf_c)::value;
+                arrive_but(min(stages - 1 - s, S - 2));
+                Frag f[AHEAD];
+                static_for<AHEAD - 1>([&](auto kk) __attribute__((always_inline)) { read_frag(f[decltype(kk)::value], decltype(kk)::value, buf); });
+                if (is < stages) issue(std::integral_constant<int, (buf + S - 1) % S>());
+                static_for<KS>([&](auto kk_c) __attribute__((always_inline)) {
+                    constexpr int kk = decltype(kk_c)::value;
+                    if constexpr (kk + AHEAD - 1 < KS) read_frag(f[(kk + AHEAD - 1) % AHEAD], kk + AHEAD - 1, buf);
+                    multiply(f[kk % AHEAD]);
+                });
+                ++s;
+            };
+#pragma unroll 1
+            while (s < full)
+                static_for<S>([&](auto buf) __attribute__((always_inline)) { if (s < full) body(buf); });
+        }
+        if (full < stages) {                                  // what is left of K; of its last 32 bytes maybe the first half only
+            arrive<0>();
+            const int buf = s % S;
+            static_for<KS>([&](auto kk_c) __attribute__((always_inline)) {
+                constexpr int kk = decltype(kk_c)::value;
+                if (32 * kk >= k_last) return;
+                Frag f;
+                read_frag(f, kk, buf);
+                if (32 * kk + 16 >= k_last && lane >= 32) {
+#pragma unroll
+                    for (int ct = 0; ct < NT; ++ct) f.a[ct] = v4i{0, 0, 0, 0};
+                }
+                multiply(f);
+            });
+        }
+
+        // ---- epilogue.  A lane has 16 NT consecutive channels of a token, and its neighbour those of the next one: stored from there, every
+        // instruction would touch 64 lines and fill none.  So a wavefront turns its results over in LDS that it has for itself
+        // (REGION bytes), SLOTS times 32 tokens at once, and lines leave whole; a residual comes in the same way.  Chunk c of a row
+        // stands at c ^ swz(row), which spreads rows over the banks.
+        auto swz = [](int r) __attribute__((always_inline)) { return CH >= 8 ? r & (CH - 1) : (r / (8 / CH)) & (CH - 1); };
+        __syncthreads();                                      // (nobody reads operands any more)
+        const bool more_tiles = PERSIST && tile + slots < end;
+        Place next = at;
+        if constexpr (PERSIST) {
+            if (more_tiles) {
+                next = place(tile + slots);
+                aim(next, par ^ 1);
+                issue(std::integral_constant<int, 0>());
+            }
+        }
+        const int64_t m0 = at.m0;
+        const int n0 = at.n0, rows = at.rows;
+        int8_t* const own = lds + (PERSIST ? STG : 0) + wv * REGION;
+        // this lane's results: tokens 32 MT wm + 32 tt + li, channels from cl on
+        const int lane_e = lane_now(), li = lane_e & 31, lg = lane_e >> 5, cl = wn * 32 * NT + 16 * NT * lg;
+        float xs[MT];
+#pragma unroll
+        for (int tt = 0; tt < MT; ++tt) xs[tt] = xs_s[par][wm * 32 * MT + li + 32 * tt];
+        const int mv_row = lane_e / CH, c_mv = n0 + wn * 32 * NT + CK::E * (lane_e % CH);
+        const bool whole = n0 + (wn + 1) * 32 * NT <= N;      // (of all lanes) no channel of the wavefront's is past the last
+        auto at_mv = [&](int i) __attribute__((always_inline)) {
+            const int row = MV_ROWS * i + mv_row;
+            return own + row * RB + 16 * ((lane_e % CH) ^ swz(row));
+        };
+        auto pass = [&](auto t0_c) __attribute__((always_inline)) -> bool {      // false: no tokens from there on
+            constexpr int t0 = decltype(t0_c)::value;
+            const int64_t mw = m0 + wm * 32 * MT + 32 * t0;   // the first token of the slots
+            const int left = rows - (wm * 32 * MT + 32 * t0); // tokens from there on
+            if (left <= 0) {
+                if (PERSIST && t0 == 0) wait_vm0();
+                return false;
+            }
+            if constexpr (TYPE != TYPE_I8) {
+                if (P.residual) {
+                    if constexpr (EARLY) {
+#pragma unroll
+                        for (int i = 0; i < SLOTS * MOVES; ++i) *reinterpret_cast<v4i*>(at_mv(i)) = early[EARLY ? t0 / SLOTS : 0][EARLY ? i : 0];
+                    } else {
+                        const T* const res = static_cast<const T*>(P.residual) + mw * P.ld_res + c_mv;
+                        if (whole) {
+                            v4i r[SLOTS * MOVES];
+#pragma unroll
+                            for (int i = 0; i < SLOTS * MOVES; ++i) r[i] = CK::load(res + min(MV_ROWS * i + mv_row, left - 1) * P.ld_res, CK::E, CK::E);
+#pragma unroll
+                            for (int i = 0; i < SLOTS * MOVES; ++i) *reinterpret_cast<v4i*>(at_mv(i)) = r[i];
+                        } else if (c_mv < N) {
+#pragma unroll 1
+                            for (int i = 0; i < SLOTS * MOVES; ++i) {
+                                const int row = min(MV_ROWS * i + mv_row, left - 1);
+                                *reinterpret_cast<v4i*>(at_mv(i)) = CK::load(res + row * P.ld_res, N - c_mv, (P.M - 1 - mw - row) * P.ld_res + N - c_mv);
+                            }
+                        }
+                    }
+                    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                    __builtin_amdgcn_wave_barrier();
+                }
+            }
+            with_activation(P.act, [&](auto act) __attribute__((always_inline)) {
+#pragma unroll
+                for (int j = 0; j < MINE; ++j) {
+                    const int c = cl + CK::E * j;             // first channel of the chunk in the tile
+                    typename CK::vf ws, bi;
+#pragma unroll
+                    for (int e = 0; e < CK::E; e += 4) {
+                        const v4f a = *reinterpret_cast<const v4f*>(&ws_s[par][c + e]), b = *reinterpret_cast<const v4f*>(&bias_s[par][c + e]);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) { ws[e + k] = a[k]; bi[e + k] = b[k]; }
+                    }
+                    static_for<SLOTS>([&](auto tt_c) __attribute__((always_inline)) {
+                        constexpr int tt = t0 + decltype(tt_c)::value;
+                        int8_t* const at = own + (32 * (tt % SLOTS) + li) * RB + 16 * ((MINE * lg + j) ^ swz(li));
+                        typename CK::vf v;
+#pragma unroll
+                        for (int e = 0; e < CK::E; ++e) {
+                            constexpr int PER = 16 / CK::E;   // chunks of the 16 results of an MFMA tile
+                            v[e] = activation<decltype(act)::value>(__builtin_fmaf((float)acc[j / PER][tt][CK::E * (j % PER) + e] * ws[e], xs[tt], bi[e]));
+                        }
+                        if constexpr (TYPE != TYPE_I8) {
+                            if (P.residual) v += CK::unpack(*reinterpret_cast<const v4i*>(at));
+                        }
+                        *reinterpret_cast<v4i*>(at) = CK::pack(v, P.inv_step);
+                    });
+                    __builtin_amdgcn_sched_barrier(0);        // keep the register footprint of the epilogue small
+                }
+            });
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            if (PERSIST && t0 == 0) wait_vm0();               // the next tile's first stage, before stores stand in line behind it
+            T* const y = static_cast<T*>(P.y) + mw * P.ldy + c_mv;
+            if (whole) {
 #pragma unroll
                 for (int i = 0; i < SLOTS * MOVES; ++i) {
-                    const int row = min(wm * 32 * MT + 32 * SLOTS * p + MV_ROWS * i + lane / CH, at.rows - 1);
-                    early[p][i] = v4i{0, 0, 0, 0};
-                    if (c < N) early[p][i] = CK::load(res + row * P.ld_res, N - c, (P.M - 1 - at.m0 - row) * P.ld_res + N - c);
+                    const v4i v = *reinterpret_cast<const v4i*>(at_mv(i));
+                    if (MV_ROWS * i + mv_row < left) CK::store(y + (MV_ROWS * i + mv_row) * P.ldy, v, CK::E);
                 }
-        }
-    }
-    if constexpr (PERSIST) {                              // stage 0 has arrived; the other buffer served the last epilogue
-        __syncthreads();
-        if (1 < stages) issue(std::integral_constant<int, 1>());
-    } else {
-        static_for<PIPE ? S : S - 1>([&](auto buf) __attribute__((always_inline)) {
-            if (decltype(buf)::value < stages) issue(buf);
-        });
-    }
-#pragma unroll
-    for (int ct = 0; ct < NT; ++ct)
-#pragma unroll
-        for (int tt = 0; tt < MT; ++tt) acc[ct][tt] = sums_from(0);
-    int s = 0;
-    {
-        const int ln = lane_now(), li = ln & 31, lg = ln >> 5;
-#pragma unroll
-        for (int kk = 0; kk < KS; ++kk) {
-            const int col = 16 * ((2 * kk + lg) ^ mix(li));
-            fx[kk] = (wm * 32 * MT + li) * BK + col;
-            fw[kk] = (TM + wn * 32 * NT + li) * BK + col;
-        }
-    }
-    if constexpr (PIPE) {
-        // All S buffers are filled to begin with.  In front of the last k-step of stage s, whose fragments are in registers then, stage
-        // s + 1 has to have arrived; behind the barrier there nobody reads stage s any more: its buffer takes stage s + S, and the first
-        // fragments of stage s + 1 come under the products of that last k-step.  So no stage begins with a wait.  Reads and requests stand
-        // one by one between the products: a wavefront issues in order, and eight reads at a stretch hold it for longer than a product takes.
-        Frag f[2];
-        if constexpr (!PERSIST) arrive_but(stages >= S ? S - 1 : 0);
-        read_frag(f[0], 0, 0);
-        auto body = [&](auto buf_c, auto more_c) __attribute__((always_inline)) {
-            constexpr int buf = decltype(buf_c)::value, nb = (buf + 1) % S;
-            constexpr bool MORE = decltype(more_c)::value;            // there is a stage s + S (false: maybe)
-            static_for<KS>([&](auto kk_c) __attribute__((always_inline)) {
-                constexpr int kk = decltype(kk_c)::value;
-                constexpr bool last = kk == KS - 1;
-                if constexpr (last) {
-                    if constexpr (MORE) {
-                        arrive<(S - 2) * DP>();
-                        if (is == moves) {
-#pragma unroll
-                            for (int i = 0; i < DP; ++i) off[i] -= back;
-                        }
-                    } else if (s + 1 < stages) {
-                        arrive_but(min(stages - 2 - s, S - 2));
-                        if (is < stages) issue(buf_c);
-                    }
+            } else {
+#pragma unroll 1
+                for (int i = 0; i < SLOTS * MOVES; ++i) {
+                    const v4i v = *reinterpret_cast<const v4i*>(at_mv(i));
+                    if (MV_ROWS * i + mv_row < left) CK::store(y + (MV_ROWS * i + mv_row) * P.ldy, v, N - c_mv);
                 }
-                constexpr int READS = NT + MT, DO = READS + (last && MORE ? DP : 0), N_MUL = NT * MT;
-                static_for<N_MUL>([&](auto i_c) __attribute__((always_inline)) {
-                    constexpr int i = decltype(i_c)::value, ct = i / MT, tt = i % MT;
-                    acc[ct][tt] = __builtin_amdgcn_mfma_i32_32x32x32_i8(f[kk & 1].a[ct], f[kk & 1].b[tt], acc[ct][tt], 0, 0, 0);
-                    constexpr int from = i * DO / N_MUL, to = (i + 1) * DO / N_MUL;
-                    static_for<to - from>([&](auto d_c) __attribute__((always_inline)) {
-                        constexpr int d = from + decltype(d_c)::value;
-                        if constexpr (d < READS) read_one(f[(kk + 1) & 1], d, last ? 0 : kk + 1, last ? nb : buf);
-                        else load_lds<buf * STG + (d - READS) * W * 1024>(d - READS < XI ? x_buf : w_buf, off[d - READS], k_off, lds0);
-                    });
-                    __builtin_amdgcn_sched_barrier(0);
-                });
-                if constexpr (last && MORE) { ++is; k_off += BK; }
-            });
-            ++s;
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            return true;
         };
-        static_assert(KS % 2 == 0, "the first fragments of every stage go to the same registers");
-#pragma unroll 1
-        while (s + 2 * S <= stages)
-            static_for<S>([&](auto buf) __attribute__((always_inline)) { body(buf, std::true_type()); });
-#pragma unroll 1
-        while (s < full)
-            static_for<S>([&](auto buf) __attribute__((always_inline)) { if (s < full) body(buf, std::false_type()); });
-    } else {
-        // Stage s: its loads have arrived when at most those of the later stages requested so far (S - 2, fewer at the end)
-        // are outstanding; behind the barrier nobody reads stage s - 1 any more and its buffer takes stage s + S - 1.  Those
-        // loads go out behind the first fragment reads.
-        auto body = [&](auto buf_c) __attribute__((always_inline)) {
-            constexpr int buf = decltype(buf_c)::value;
-            arrive_but(min(stages - 1 - s, S - 2));
-            Frag f[AHEAD];
-            static_for<AHEAD - 1>([&](auto kk) __attribute__((always_inline)) { read_frag(f[decltype(kk)::value], decltype(kk)::value, buf); });
-            if (is < stages) issue(std::integral_constant<int, (buf + S - 1) % S>());
-            static_for<KS>([&](auto kk_c) __attribute__((always_inline)) {
-                constexpr int kk = decltype(kk_c)::value;
-                if constexpr (kk + AHEAD - 1 < KS) read_frag(f[(kk + AHEAD - 1) % AHEAD], kk + AHEAD - 1, buf);
-                multiply(f[kk % AHEAD]);
-            });
-            ++s;
-        };
-#pragma unroll 1
-        while (s < full)
-            static_for<S>([&](auto buf) __attribute__((always_inline)) { if (s < full) body(buf); });
-    }
-    if (full < stages) {                                  // what is left of K; of its last 32 bytes maybe the first half only
-        arrive<0>();
-        const int buf = s % S;
-        static_for<KS>([&](auto kk_c) __attribute__((always_inline)) {
-            constexpr int kk = decltype(kk_c)::value;
-            if (32 * kk >= k_last) return;
-            Frag f;
-            read_frag(f, kk, buf);
-            if (32 * kk + 16 >= k_last && lane >= 32) {
-#pragma unroll
-                for (int ct = 0; ct < NT; ++ct) f.a[ct] = v4i{0, 0, 0, 0};
-            }
-            multiply(f);
-        });
-    }
-
-    // ---- epilogue.  A lane has 16 NT consecutive channels of a token, and its neighbour those of the next one: stored from there, every
-    // instruction would touch 64 lines and fill none.  So a wavefront turns its results over in LDS that it has for itself
-    // (REGION bytes), SLOTS times 32 tokens at once, and lines leave whole; a residual comes in the same way.  Chunk c of a row
-    // stands at c ^ swz(row), which spreads rows over the banks.
-    auto swz = [](int r) __attribute__((always_inline)) { return CH >= 8 ? r & (CH - 1) : (r / (8 / CH)) & (CH - 1); };
-    __syncthreads();                                      // (nobody reads operands any more)
-    const bool more_tiles = PERSIST && tile + slots < end;
-    Place next = at;
-    if constexpr (PERSIST) {
-        if (more_tiles) {
-            next = place(tile + slots);
-            aim(next, par ^ 1);
-            issue(std::integral_constant<int, 0>());
-        }
-    }
-    const int64_t m0 = at.m0;
-    const int n0 = at.n0, rows = at.rows;
-    int8_t* const own = lds + (PERSIST ? STG : 0) + wv * REGION;
-    // this lane's results: tokens 32 MT wm + 32 tt + li, channels from cl on
-    const int lane_e = lane_now(), li = lane_e & 31, lg = lane_e >> 5, cl = wn * 32 * NT + 16 * NT * lg;
-    float xs[MT];
-#pragma unroll
-    for (int tt = 0; tt < MT; ++tt) xs[tt] = xs_s[par][wm * 32 * MT + li + 32 * tt];
-    const int mv_row = lane_e / CH, c_mv = n0 + wn * 32 * NT + CK::E * (lane_e % CH);
-    const bool whole = n0 + (wn + 1) * 32 * NT <= N;      // (of all lanes) no channel of the wavefront's is past the last
-    auto at_mv = [&](int i) __attribute__((always_inline)) {
-        const int row = MV_ROWS * i + mv_row;
-        return own + row * RB + 16 * ((lane_e % CH) ^ swz(row));
-    };
-    auto pass = [&](auto t0_c) __attribute__((always_inline)) -> bool {      // false: no tokens from there on
-        constexpr int t0 = decltype(t0_c)::value;
-        const int64_t mw = m0 + wm * 32 * MT + 32 * t0;   // the first token of the slots
-        const int left = rows - (wm * 32 * MT + 32 * t0); // tokens from there on
-        if (left <= 0) {
-            if (PERSIST && t0 == 0) wait_vm0();
-            return false;
-        }
-        if constexpr (TYPE != TYPE_I8) {
-            if (P.residual) {
-                if constexpr (EARLY) {
-#pragma unroll
-                    for (int i = 0; i < SLOTS * MOVES; ++i) *reinterpret_cast<v4i*>(at_mv(i)) = early[EARLY ? t0 / SLOTS : 0][EARLY ? i : 0];
-                } else {
-                    const T* const res = static_cast<const T*>(P.residual) + mw * P.ld_res + c_mv;
-                    if (whole) {
-                        v4i r[SLOTS * MOVES];
-#pragma unroll
-                        for (int i = 0; i < SLOTS * MOVES; ++i) r[i] = CK::load(res + min(MV_ROWS * i + mv_row, left - 1) * P.ld_res, CK::E, CK::E);
-#pragma unroll
-                        for (int i = 0; i < SLOTS * MOVES; ++i) *reinterpret_cast<v4i*>(at_mv(i)) = r[i];
-                    } else if (c_mv < N) {
-#pragma unroll 1
-                        for (int i = 0; i < SLOTS * MOVES; ++i) {
-                            const int row = min(MV_ROWS * i + mv_row, left - 1);
-                            *reinterpret_cast<v4i*>(at_mv(i)) = CK::load(res + row * P.ld_res, N - c_mv, (P.M - 1 - mw - row) * P.ld_res + N - c_mv);
-                        }
-                    }
-                }
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                __builtin_amdgcn_wave_barrier();
-            }
-        }
-        with_activation(P.act, [&](auto act) __attribute__((always_inline)) {
-#pragma unroll
-            for (int j = 0; j < MINE; ++j) {
-                const int c = cl + CK::E * j;             // first channel of the chunk in the tile
-                typename CK::vf ws, bi;
-#pragma unroll
-                for (int e = 0; e < CK::E; e += 4) {
-                    const v4f a = *reinterpret_cast<const v4f*>(&ws_s[par][c + e]), b = *reinterpret_cast<const v4f*>(&bias_s[par][c + e]);
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) { ws[e + k] = a[k]; bi[e + k] = b[k]; }
-                }
-                static_for<SLOTS>([&](auto tt_c) __attribute__((always_inline)) {
-                    constexpr int tt = t0 + decltype(tt_c)::value;
-                    int8_t* const at = own + (32 * (tt % SLOTS) + li) * RB + 16 * ((MINE * lg + j) ^ swz(li));
-                    typename CK::vf v;
-#pragma unroll
-                    for (int e = 0; e < CK::E; ++e) {
-                        constexpr int PER = 16 / CK::E;   // chunks of the 16 results of an MFMA tile
-                        v[e] = activation<decltype(act)::value>(__builtin_fmaf((float)acc[j / PER][tt][CK::E * (j % PER) + e] * ws[e], xs[tt], bi[e]));
-                    }
-                    if constexpr (TYPE != TYPE_I8) {
-                        if (P.residual) v += CK::unpack(*reinterpret_cast<const v4i*>(at));
-                    }
-                    *reinterpret_cast<v4i*>(at) = CK::pack(v, P.inv_step);
-                });
-                __builtin_amdgcn_sched_barrier(0);        // keep the register footprint of the epilogue small
-            }
-        });
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        if (PERSIST && t0 == 0) wait_vm0();               // the next tile's first stage, before stores stand in line behind it
-        T* const y = static_cast<T*>(P.y) + mw * P.ldy + c_mv;
-        if (whole) {
-#pragma unroll
-            for (int i = 0; i < SLOTS * MOVES; ++i) {
-                const v4i v = *reinterpret_cast<const v4i*>(at_mv(i));
-                if (MV_ROWS * i + mv_row < left) CK::store(y + (MV_ROWS * i + mv_row) * P.ldy, v, CK::E);
-            }
-        } else {
-#pragma unroll 1
-            for (int i = 0; i < SLOTS * MOVES; ++i) {
-                const v4i v = *reinterpret_cast<const v4i*>(at_mv(i));
-                if (MV_ROWS * i + mv_row < left) CK::store(y + (MV_ROWS * i + mv_row) * P.ldy, v, N - c_mv);
-            }
-        }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        return true;
-    };
-    bool on = true;
-    static_for<MT / SLOTS>([&](auto p) __attribute__((always_inline)) { if (on) on = pass(std::integral_constant<int, decltype(p)::value * SLOTS>()); });
-    if (!more_tiles) break;
-    at = next;
-    tile += slots;
+        bool on = true;
+        static_for<MT / SLOTS>([&](auto p) __attribute__((always_inline)) { if (on) on = pass(std::integral_constant<int, decltype(p)::value * SLOTS>()); });
+        if (!more_tiles) break;
+        at = next;
+        tile += slots;
     }
 }
 
 constexpr int64_t kBand = 4;                   // rows of tiles in a band
-template <int TYPE, int MT, int NT, int GM, int GN, int S, int BK = 128> hipError_t launch_tile(hipStream_t s, const ScaledArgs& a) {
-    using TL = GsTile<MT, NT, GM, GN, BK>;
+template <int TYPE, int MT, int NT, int GM, int GN, int S> hipError_t launch_tile(hipStream_t s, const ScaledArgs& a) {
+    using TL = GsTile<MT, NT, GM, GN>;
     GsParams P;
     P.x = a.x; P.x_scale = a.x_scale; P.w = a.w; P.w_scale = a.w_scale; P.bias = a.bias; P.residual = a.residual; P.y = a.y;
     P.ldx = a.ldx; P.ld_res = a.ld_res; P.ldy = a.ldy; P.M = a.M; P.N = a.N; P.K = a.K; P.act = a.act; P.one_scale = a.one_scale;
@@ -492,7 +498,7 @@ template <int TYPE, int MT, int NT, int GM, int GN, int S, int BK = 128> hipErro
     int64_t grid = (tm * tn + NXCD - 1) / NXCD * NXCD;
     P.order = TileOrder((uint32_t)tm, (uint32_t)tn, (uint32_t)(tm < kBand ? tm : kBand));
     if (MT * NT >= 4 && S == 2) grid = min64(grid, (int64_t)num_cus() * (TL::W == 4 ? 2 : 1) / NXCD * NXCD);     // (PERSIST)
-    hipLaunchKernelGGL((gemm_scaled_kernel<TYPE, MT, NT, GM, GN, S, BK>), dim3((unsigned)grid), dim3(64 * TL::W), 0, s, P);
+    hipLaunchKernelGGL((gemm_scaled_kernel<TYPE, MT, NT, GM, GN, S>), dim3((unsigned)grid), dim3(64 * TL::W), 0, s, P);
     return hipGetLastError();
 }
 

@@ -1,5 +1,5 @@
 // Pieces shared by the operators around int8 Dense layers whose scales are real numbers taken at run time (rows_scaled.hip,
-// gemm_scaled.hip): element types, activations, rounding.
+// gemm_scaled.hip, gemm_scaled_rows.hip): element types, activations, rounding.
 //
 // Arithmetic is in 32-bit floating point throughout; int8 products are summed exactly in 32-bit integers.  A value is rounded to
 // fewer bits once, where it is stored (round to nearest, ties to even).

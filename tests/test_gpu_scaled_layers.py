@@ -167,6 +167,20 @@ def test_norm_in_place(ivit, t, C):
     assert torch.equal(a, y)
 
 
+@pytest.mark.parametrize("C", [5, 300, 1001, 5000])
+def test_norm_writes_over_both_its_inputs(ivit, C):
+    """The sum over the residual, the result over x, and the other way round."""
+    import torch
+    g, rows = gen(C + 2), 700
+    x, r, gamma = rand(g, rows, C).half(), rand(g, rows, C).half(), rand(g, C)
+    y, total = torch.empty_like(x), torch.empty_like(x)
+    ivit.ivit_rmsnorm_quant(x, gamma, y, None, 1e-6, residual=r, sum_out=total)
+    for swap in (False, True):
+        a, b = x.clone(), r.clone()
+        ivit.ivit_rmsnorm_quant(a, gamma, b if swap else a, None, 1e-6, residual=b, sum_out=a if swap else b)
+        assert torch.equal(b if swap else a, y) and torch.equal(a if swap else b, total)
+
+
 def test_norm_of_odd_rows(ivit):
     """Zeros, NaN, infinities, the smallest and largest numbers: each row by itself, its neighbours untouched by it."""
     import torch
@@ -331,6 +345,22 @@ def test_dense(ivit, M, N, K):
     for i, t in enumerate(("f32", "f16", "bf16", "i8")):
         act, res, bias, one = rng.choice(ACTS), t != "i8" and rng.random() < 0.6, rng.random() < 0.7, rng.random() < 0.3
         d = dense_case(i, M, N, K, t, res, bias, one)
+        step = 0.037 if t == "i8" else None
+        check_dense(d, run_dense(ivit, d, t, act, step), t, act, step, "%d x %d x %d %s %s" % (M, N, K, t, act))
+
+
+# one tile of 64 x 64, 128 x 64, 128 x 128, 256 x 128, 256 x 256 a CU at most (of 256 CUs); several of 256 x 256, and of 128 x 128, one after
+# the other in a workgroup; K that ends inside a stage, rows and channels that end inside a tile
+DENSE_TILES = [(1001, 999, 1008), (1500, 1000, 800), (2990, 770, 784), (4001, 1099, 848), (4000, 3999, 1040), (8001, 6099, 784), (9000, 5003, 896), (20000, 1031, 80),
+               (12000, 2051, 384)]
+
+
+@pytest.mark.parametrize("M,N,K", DENSE_TILES)
+@pytest.mark.parametrize("t", ("f32", "f16", "bf16", "i8"))
+def test_dense_tiles(ivit, M, N, K, t):
+    rng = random.Random(M + N + K)
+    for act, res in (("none", t != "i8"), (rng.choice(ACTS), False)):
+        d = dense_case(9, M, N, K, t, res, rng.random() < 0.7, rng.random() < 0.3)
         step = 0.037 if t == "i8" else None
         check_dense(d, run_dense(ivit, d, t, act, step), t, act, step, "%d x %d x %d %s %s" % (M, N, K, t, act))
 

@@ -111,3 +111,11 @@ def test_the_binding_refuses_tensors_that_are_not_as_stated(lib):
         with pytest.raises(ValueError):
             call()
             pytest.fail("call %d was not refused" % i)
+
+
+def test_no_vector_register_is_spilled(lib):
+    """Loads of the Dense kernels are counted by hand (s_waitcnt): a reload from scratch memory between them would wait for all."""
+    import re
+    from test_spilled_registers import _spills
+    of = {name: n for name, n in _spills().items() if re.search(r"\d(gemm_scaled(_rows)?|rmsnorm|gated)_kernel", name)}
+    assert len(of) > 40 and not [(name, n) for name, n in of.items() if n]
