@@ -6,6 +6,8 @@
  * Vision Transformer Inference" (arXiv 2207.01405): int8 x int8 -> int32
  * Dense / MatMul with dyadic requantisation (Sec. 3.2), Shiftmax (Sec. 3.3,
  * Algorithm 1), ShiftGELU (Sec. 3.4, Algorithm 2) and I-LayerNorm (Sec. 3.5).
+ * Beside it stand three layers with real scales and a floating-point residual
+ * stream (last section but one), for models quantised per token at run time.
  *
  * General rules
  *  - Every tensor pointer is a DEVICE pointer owned by the caller; the library

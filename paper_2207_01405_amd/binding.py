@@ -583,8 +583,9 @@ _FLOAT32 = _INT8 = _current_device = _raw_stream = None
 def _setup():
     global _TYPES, _FLOAT32, _INT8, _current_device, _raw_stream
     import torch
-    _FLOAT32, _INT8, _current_device = torch.float32, torch.int8, torch.cuda.current_device
-    # the handle alone, where torch has it: making a Stream object for it costs more than a launch
+    _FLOAT32, _INT8 = torch.float32, torch.int8
+    # numbers alone, where torch has them: making a Stream object costs about as much as a launch
+    _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
     _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
     _TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2, torch.int8: 3}
 
@@ -644,7 +645,7 @@ def ivit_rmsnorm_quant(x, gamma, y, y_scale, eps, residual=None, sum_out=None, s
     where = "ivit_rmsnorm_quant"
     kind, shape, dtype, dev = _type(x, where), x.shape, x.dtype, x.get_device()
     rows, Cc = shape
-    st = load().ivit_rmsnorm_quant(
+    st = (_lib or load()).ivit_rmsnorm_quant(
         _launch_stream(stream, dev, where), x.data_ptr(), _rows(x, shape, dtype, dev, where),
         None if residual is None else residual.data_ptr(), 0 if residual is None else _rows(residual, shape, dtype, dev, where),
         _vector(gamma, Cc, dev, where), eps,
@@ -669,7 +670,7 @@ def ivit_linear_scaled(x, x_scale, w, w_scale, y, bias=None, act="none", residua
         raise ValueError("%s: an int8 result needs y_step" % where)
     one = M != 1 and x_scale.numel() == 1
     out = (M, N)
-    st = load().ivit_linear_scaled(
+    st = (_lib or load()).ivit_linear_scaled(
         _launch_stream(stream, dev, where), x.data_ptr(), _rows(x, (M, K), _INT8, dev, where), _vector(x_scale, 1 if one else M, dev, where), one,
         w.data_ptr(), _vector(w_scale, N, dev, where), _vector(bias, N, dev, where), _activation(act, where),
         None if residual is None else residual.data_ptr(), 0 if residual is None else _rows(residual, out, dtype, dev, where),
@@ -684,7 +685,7 @@ def ivit_gated_quant(x, y, y_scale, act="silu", gated=True, stream=None):
     where = "ivit_gated_quant"
     kind, dev, shape = _type(x, where), x.get_device(), y.shape
     rows, Cc = shape
-    st = load().ivit_gated_quant(
+    st = (_lib or load()).ivit_gated_quant(
         _launch_stream(stream, dev, where), x.data_ptr(), _rows(x, (rows, 2 * Cc) if gated else shape, x.dtype, dev, where),
         y.data_ptr(), _rows(y, shape, _INT8, dev, where), _vector(y_scale, rows, dev, where), rows, Cc, kind, _activation(act, where), bool(gated))
     if st:
