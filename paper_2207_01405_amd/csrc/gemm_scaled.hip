@@ -546,18 +546,23 @@ template <int TYPE> hipError_t launch_type(hipStream_t s, const ScaledArgs& a, F
 
 hipError_t launch_linear_scaled(hipStream_t s, const ScaledArgs& a) {
     if (a.M == 0) return hipSuccess;
-    TraceScope trace(s, KIND_GEMM_SCALED, 2 * a.M * a.N * a.K,
-                     a.M * a.K + (int64_t)a.N * a.K + a.M * a.N * element_bytes(a.y_type) * (a.residual ? 2 : 1));
     const Form form = form_of(a);
-    if (form == ROWS) return launch_linear_scaled_rows(s, a);
+    const int64_t e = element_bytes(a.y_type);
+    auto ops = [&](int64_t M) { return 2 * M * a.N * a.K; };
+    auto bytes = [&](int64_t M) { return M * a.K + (int64_t)a.N * a.K + M * a.N * e * (a.residual ? 2 : 1); };
+    if (form == ROWS) {
+        TraceScope trace(s, KIND_GEMM_SCALED, ops(a.M), bytes(a.M));
+        return launch_linear_scaled_rows(s, a);
+    }
     // (a grid may have 2^32 threads; N is at most 2^24)
-    const int64_t most = 64 * (((int64_t)1 << 22) / ((a.N + 63) / 64)), e = element_bytes(a.y_type);
+    const int64_t most = 64 * (((int64_t)1 << 22) / ((a.N + 63) / 64));
     for (int64_t m = 0; m < a.M; m += most) {
         ScaledArgs b = a;
         b.x += m * a.ldx; b.M = min64(a.M - m, most);
         if (!a.one_scale) b.x_scale += m;
         if (a.residual) b.residual = static_cast<const int8_t*>(a.residual) + m * a.ld_res * e;
         b.y = static_cast<int8_t*>(a.y) + m * a.ldy * e;
+        TraceScope trace(s, KIND_GEMM_SCALED, ops(b.M), bytes(b.M));
         hipError_t st;
         switch (a.y_type) {
             case TYPE_F16: st = launch_type<TYPE_F16>(s, b, form); break;

@@ -1,11 +1,11 @@
 // The Dense layer with real scales (see gemm_scaled.hip) for few rows: single tokens, batches of them, one image.
 //
 // Hardly a weight is used twice, so what bounds it is how fast the weights come in (16.8 MB of them, N = K = 4096, are 3.3 us at a
-// copy's rate) and, below that, the latencies of a launch.  A workgroup of four wavefronts has 16 CT channels and 8 XT tokens; the
+// copy's rate) and, below that, the latencies of a launch.  A workgroup of W wavefronts has 16 CT channels and 8 XT tokens; the
 // wavefronts split K.  Each has D steps of 128 bytes of K in flight, direct loads of whole lines into LDS that no other wavefront reads, so
 // nobody waits for anybody before the end; there the partial sums, integers, meet in LDS.  What the epilogue reads is requested first.
 // Loads straight into the registers of the matrix instruction ask for 64 bytes of a row at a time and were slower (1 x 4096 x 4096 5.7
-// against 5.1 us, 16 x 11008 x 4096 13.9 and 9.4), as were eight wavefronts and more steps in flight.
+// against 5.1 us, 16 x 11008 x 4096 13.9 and 9.4).
 #include "regst_common.hpp"
 #include "scaled_common.hpp"
 
@@ -14,8 +14,6 @@ namespace {
 
 using namespace scaled;
 using namespace regst;
-
-constexpr int W = 4;                           // wavefronts
 
 // four consecutive results of a row at element `at`, the first n of them
 template <class T> __device__ __forceinline__ void store4(void* y, int64_t at, const float* v, int n) {
@@ -57,7 +55,7 @@ __device__ __forceinline__ float value_of(v4i v, int e, int type) {
 }
 
 // XT: 8-row pieces of x (tokens / 8); a step is 128 bytes of K
-template <int CT, int XT, int D>
+template <int CT, int XT, int W, int D>
 __global__ __launch_bounds__(64 * W) void gemm_scaled_rows_kernel(ScaledArgs P, int steps, int count, FastDiv cols) {
     constexpr int MT = (XT + 1) / 2, PER = 2 * CT + XT, STEP = PER * 1024, RING = D * STEP;
     __shared__ __align__(1024) int8_t lds[RING > CT * MT * 1024 ? W * RING : W * CT * MT * 1024];
@@ -79,7 +77,7 @@ __global__ __launch_bounds__(64 * W) void gemm_scaled_rows_kernel(ScaledArgs P, 
 #pragma unroll
     for (int i = 0; i < XT; ++i) xo[i] = (uint32_t)min(8 * i + lr, rows - 1) * (uint32_t)P.ldx;
     // the 16 x 16 results that this wavefront finishes: channels n .. n + 3 of token m0 + row
-    static_assert(CT * MT <= W, "one a wavefront");
+    static_assert(CT * MT <= W && D <= 3, "a result a wavefront; the waits below");
     const int n = n0 + 16 * (wv / MT) + 4 * lg, row = 16 * (wv % MT) + li, left = wv < CT * MT && row < rows ? N - n : 0;
     v4i res = {}, ws = {}, bi = {};
     float xs = 0.0f;
@@ -141,8 +139,7 @@ __global__ __launch_bounds__(64 * W) void gemm_scaled_rows_kernel(ScaledArgs P, 
             switch (d) {
                 case 0: asm volatile("s_waitcnt vmcnt(%0)" : : "n"(0) : "memory"); break;
                 case 1: asm volatile("s_waitcnt vmcnt(%0)" : : "n"(PER) : "memory"); break;
-                case 2: asm volatile("s_waitcnt vmcnt(%0)" : : "n"(2 * PER) : "memory"); break;
-                default: asm volatile("s_waitcnt vmcnt(%0)" : : "n"(3 * PER) : "memory"); break;
+                default: asm volatile("s_waitcnt vmcnt(%0)" : : "n"(2 * PER) : "memory"); break;
             }
             multiply(i, i % D);
             ++i;
@@ -181,23 +178,28 @@ __global__ __launch_bounds__(64 * W) void gemm_scaled_rows_kernel(ScaledArgs P, 
     else store4<float>(P.y, at, v, left);
 }
 
-template <int CT, int XT, int D> hipError_t launch(hipStream_t s, const ScaledArgs& a) {
+template <int CT, int XT, int W, int D> hipError_t launch(hipStream_t s, const ScaledArgs& a) {
     const int steps = (a.K + 127) / 128, count = (steps + W - 1) / W;
     const int64_t tn = (a.N + 16 * CT - 1) / (16 * CT), tiles = (a.M + 8 * XT - 1) / (8 * XT) * tn;
-    hipLaunchKernelGGL((gemm_scaled_rows_kernel<CT, XT, D>), dim3((unsigned)tiles), dim3(64 * W), 0, s, a, steps, count, FastDiv((uint32_t)tn));
+    hipLaunchKernelGGL((gemm_scaled_rows_kernel<CT, XT, W, D>), dim3((unsigned)tiles), dim3(64 * W), 0, s, a, steps, count, FastDiv((uint32_t)tn));
     return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_linear_scaled_rows(hipStream_t s, const ScaledArgs& a) {
-    if (a.M <= 8) return launch<1, 1, 3>(s, a);
-    if (a.M <= 16) return launch<1, 2, 3>(s, a);
+    // Eight wavefronts with two steps each in flight where half of the CUs have no tile: 1 x 1000 x 4096 3.6 -> 3.1 us, 8 x 1000 x 8192
+    // 5.2 -> 4.7, 48 x 768 x 4096 4.2 -> 3.9; with a tile a CU nothing is gained (16 x 4096 x 4096 5.1 and 5.0), with several
+    // they lose (1 x 11008 x 4096, 688 tiles, 9.0 and 9.4).
+    const int64_t tn = ((int64_t)a.N + 15) / 16, tiles = (a.M + 31) / 32 * tn;
+    const bool few = 2 * tiles <= num_cus();
+    if (a.M <= 8) return few ? launch<1, 1, 8, 2>(s, a) : launch<1, 1, 4, 3>(s, a);
+    if (a.M <= 16) return few ? launch<1, 2, 8, 2>(s, a) : launch<1, 2, 4, 3>(s, a);
+    if (few) return launch<1, 4, 8, 2>(s, a);
     // 16 channels for 32 rows while one such tile a CU takes the shape, 32 channels beyond (197 x 384 x 1536, 168 tiles: 3.4 and 3.6 us;
     // 48 x 4096 x 4096, 512: 7.4 and 6.3)
-    const int64_t tiles = (a.M + 31) / 32 * (((int64_t)a.N + 15) / 16);
-    if (a.M <= 32 || tiles <= num_cus()) return launch<1, 4, 3>(s, a);
-    return launch<2, 4, 2>(s, a);
+    if (a.M <= 32 || tiles <= num_cus()) return launch<1, 4, 4, 3>(s, a);
+    return launch<2, 4, 4, 2>(s, a);
 }
 
 }  // namespace ivit

@@ -231,6 +231,8 @@ template <class T> hipError_t norm_of(hipStream_t s, const RmsNormArgs& a) {
             const int64_t rows = min64(a.rows - r, MOST), grid = (rows + ROWS - 1) / ROWS;
             NormParams P{at(a.x, a.ldx), at(a.residual, a.ld_res), a.gamma, const_cast<T*>(at(a.sum, a.ld_sum)), nullptr, nullptr,
                          a.ldx, a.ld_res, a.ld_sum, a.ldy, rows, a.C, a.eps};
+            const int64_t e = sizeof(T), n = rows * a.C;
+            TraceScope trace(s, KIND_RMSNORM, 0, n * e * (1 + (a.residual != nullptr) + (a.sum != nullptr)) + n * (a.y_scale ? 1 : e));
             if (a.y_scale) {
                 P.y = static_cast<int8_t*>(a.y) + r * a.ldy;
                 P.scale = a.y_scale + r;
@@ -253,6 +255,7 @@ template <class T> hipError_t gate_of(hipStream_t s, const GatedArgs& a) {
         for (int64_t r = 0; r < a.rows; r += MOST) {
             const int64_t rows = min64(a.rows - r, MOST), grid = (rows + ROWS - 1) / ROWS;
             const GateParams P{static_cast<const T*>(a.x) + r * a.ldx, a.y + r * a.ldy, a.y_scale + r, a.ldx, a.ldy, rows, a.C, a.act};
+            TraceScope trace(s, KIND_GATED, 0, rows * a.C * ((int64_t)sizeof(T) * (a.gated ? 2 : 1) + 1));
             if (a.gated) hipLaunchKernelGGL((gated_kernel<T, NV, TPR, BLOCK, true, SHORT>), dim3((unsigned)grid), dim3(BLOCK), 0, s, P);
             else hipLaunchKernelGGL((gated_kernel<T, NV, TPR, BLOCK, false, SHORT>), dim3((unsigned)grid), dim3(BLOCK), 0, s, P);
             if (hipError_t e = hipGetLastError()) return e;
@@ -265,8 +268,6 @@ template <class T> hipError_t gate_of(hipStream_t s, const GatedArgs& a) {
 
 hipError_t launch_rmsnorm(hipStream_t s, const RmsNormArgs& a) {
     if (a.rows == 0) return hipSuccess;
-    const int64_t e = element_bytes(a.type), n = a.rows * a.C;
-    TraceScope trace(s, KIND_RMSNORM, 0, n * e * (1 + (a.residual != nullptr) + (a.sum != nullptr)) + n * (a.y_scale ? 1 : e));
     if (a.type == TYPE_F16) return norm_of<_Float16>(s, a);
     if (a.type == TYPE_BF16) return norm_of<__bf16>(s, a);
     return norm_of<float>(s, a);
@@ -274,8 +275,6 @@ hipError_t launch_rmsnorm(hipStream_t s, const RmsNormArgs& a) {
 
 hipError_t launch_gated(hipStream_t s, const GatedArgs& a) {
     if (a.rows == 0) return hipSuccess;
-    const int64_t e = element_bytes(a.type), n = a.rows * a.C;
-    TraceScope trace(s, KIND_GATED, 0, n * e * (a.gated ? 2 : 1) + n);
     if (a.type == TYPE_F16) return gate_of<_Float16>(s, a);
     if (a.type == TYPE_BF16) return gate_of<__bf16>(s, a);
     return gate_of<float>(s, a);
