@@ -77,7 +77,7 @@ template <int TYPE> struct Chunk {
     static __device__ __forceinline__ vf unpack(v4i v) { return __builtin_convertvector(__builtin_bit_cast(vt, v), vf); }
     // the chunk at p, which may have the alignment of one element; of it n elements count, and `there` exist
     static __device__ __forceinline__ v4i load(const T* p, int n, int64_t there) {
-        if (n >= E || there >= E) return __builtin_bit_cast(v4i, (vt)*reinterpret_cast<const mem*>(p));
+        if (n >= E || there >= E) return __builtin_bit_cast(v4i, (vt)__builtin_nontemporal_load(reinterpret_cast<const mem*>(p)));
         vt v = {};
 #pragma unroll
         for (int e = 0; e < E - 1; ++e)
@@ -86,7 +86,7 @@ template <int TYPE> struct Chunk {
     }
     static __device__ __forceinline__ void store(T* p, v4i w, int n) {
         const vt v = __builtin_bit_cast(vt, w);
-        if (n >= E) { *reinterpret_cast<mem*>(p) = v; return; }
+        if (n >= E) { __builtin_nontemporal_store(v, reinterpret_cast<mem*>(p)); return; }
 #pragma unroll
         for (int e = 0; e < E - 1; ++e)
             if (e < n) p[e] = v[e];

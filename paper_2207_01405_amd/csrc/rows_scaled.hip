@@ -56,7 +56,7 @@ __device__ __forceinline__ void store_q(int8_t* p, const v8f& v, const Quant& q,
     for (int e = 0; e < 8; ++e) w[e] = q.inv == 0.0f ? 0u : round_bits(v[e] * q.up, q.inv);
     typedef uint32_t v2u __attribute__((ext_vector_type(2), aligned(1)));
     const v2u out = {pack4(w[0], w[1], w[2], w[3]), pack4(w[4], w[5], w[6], w[7])};
-    if (n >= 8) { *reinterpret_cast<v2u*>(p) = out; return; }
+    if (n >= 8) { __builtin_nontemporal_store(out, reinterpret_cast<v2u*>(p)); return; }
 #pragma unroll
     for (int e = 0; e < 7; ++e)
         if (e < n) p[e] = (int8_t)(out[e >> 2] >> (8 * (e & 3)));
