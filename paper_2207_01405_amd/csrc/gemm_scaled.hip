@@ -45,7 +45,7 @@ struct TileOrder {
 
 struct GsParams {
     const int8_t* x; const float* x_scale; const int8_t* w; const float* w_scale; const float* bias; const void* residual; void* y;
-    int64_t ldx, ld_res, ldy, M; int N, K, act, one_scale; float inv_step;
+    int64_t ldx, ld_res, ldy, M; int N, K, act, one_scale, res_once; float inv_step;
     TileOrder order;
 };
 
@@ -75,9 +75,11 @@ template <int TYPE> struct Chunk {
         }
     }
     static __device__ __forceinline__ vf unpack(v4i v) { return __builtin_convertvector(__builtin_bit_cast(vt, v), vf); }
+    // a chunk past the L2
+    static __device__ __forceinline__ v4i load_once(const T* p) { return __builtin_bit_cast(v4i, (vt)__builtin_nontemporal_load(reinterpret_cast<const mem*>(p))); }
     // the chunk at p, which may have the alignment of one element; of it n elements count, and `there` exist
     static __device__ __forceinline__ v4i load(const T* p, int n, int64_t there) {
-        if (n >= E || there >= E) return __builtin_bit_cast(v4i, (vt)__builtin_nontemporal_load(reinterpret_cast<const mem*>(p)));
+        if (n >= E || there >= E) return __builtin_bit_cast(v4i, (vt)*reinterpret_cast<const mem*>(p));
         vt v = {};
 #pragma unroll
         for (int e = 0; e < E - 1; ++e)
@@ -414,8 +416,15 @@ __global__ __launch_bounds__((64 * GM * GN), 2) void gemm_scaled_kernel(GsParams
                         const T* const res = static_cast<const T*>(P.residual) + mw * P.ld_res + c_mv;
                         if (whole) {
                             v4i r[SLOTS * MOVES];
+                            if (P.res_once) {
+                                keep_apart();
 #pragma unroll
-                            for (int i = 0; i < SLOTS * MOVES; ++i) r[i] = CK::load(res + min(MV_ROWS * i + mv_row, left - 1) * P.ld_res, CK::E, CK::E);
+                                for (int i = 0; i < SLOTS * MOVES; ++i) r[i] = CK::load_once(res + min(MV_ROWS * i + mv_row, left - 1) * P.ld_res);
+                                keep_apart();
+                            } else {
+#pragma unroll
+                                for (int i = 0; i < SLOTS * MOVES; ++i) r[i] = CK::load(res + min(MV_ROWS * i + mv_row, left - 1) * P.ld_res, CK::E, CK::E);
+                            }
 #pragma unroll
                             for (int i = 0; i < SLOTS * MOVES; ++i) *reinterpret_cast<v4i*>(at_mv(i)) = r[i];
                         } else if (c_mv < N) {
@@ -494,6 +503,10 @@ template <int TYPE, int MT, int NT, int GM, int GN, int S> hipError_t launch_til
     P.x = a.x; P.x_scale = a.x_scale; P.w = a.w; P.w_scale = a.w_scale; P.bias = a.bias; P.residual = a.residual; P.y = a.y;
     P.ldx = a.ldx; P.ld_res = a.ld_res; P.ldy = a.ldy; P.M = a.M; P.N = a.N; P.K = a.K; P.act = a.act; P.one_scale = a.one_scale;
     P.inv_step = a.inv_step;
+    // Results are stored past the L2, which has the operands to keep and would write them back at the launch's end (8192 x 8192 x 4096 246 -> 230 us,
+    // 50432 x 768 x 768 54 -> 47).  A residual of 64 MB and more is loaded past it, and past the last-level cache, too (bf16, 8192 x 8192 x 4096, 134 MB, 284 and
+    // 258 us; 50432 x 768 x 768, 77 MB, 67 and 64.6); smaller ones may still be in that cache (4096 x 4096 x 4096, 34 MB, 67 and 70; 25216 x 384 x 1536 28.0 and 30.0).
+    P.res_once = a.M * a.N * (int64_t)sizeof(Stored<TYPE>) >= (int64_t)1 << 26;
     const int64_t tm = (a.M + TL::TM - 1) / TL::TM, tn = (a.N + TL::TN - 1) / TL::TN;
     int64_t grid = (tm * tn + NXCD - 1) / NXCD * NXCD;
     P.order = TileOrder((uint32_t)tm, (uint32_t)tn, (uint32_t)(tm < kBand ? tm : kBand));

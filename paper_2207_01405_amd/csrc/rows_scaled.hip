@@ -4,7 +4,8 @@
 //   norm:  h = x + r,  n = h / sqrt(mean(h^2) + eps) gamma        gate:  v = act(g) u  or  act(g)
 //   s = max |v| / 127,  q = round(v / s)
 //
-// Both are bound by memory: an element is 10 to 20 operations for 3 to 7 bytes.  A group of TPR threads holds a row in
+// Both are bound by memory: an element is 10 to 20 operations for 3 to 7 bytes.  Results are stored past the L2 (norms of 25216 x 768 29.2 -> 23.2 us,
+// 16384 x 4096 85.7 -> 81.8).  A group of TPR threads holds a row in
 // registers, NV pieces of eight elements a thread, so that x is read once; one reduction over the group gives the norm its sum of
 // squares and its largest |h gamma| together: the factor 1 / sqrt(..) is the same for a row's elements, so q needs h gamma only
 // and s takes the factor once.
@@ -143,7 +144,7 @@ __global__ __launch_bounds__(BLOCK) void rmsnorm_kernel(NormParams P) {
     }
 }
 
-struct GateParams { const void* x; int8_t* y; float* scale; int64_t ldx, ldy, rows; int C, act; };
+struct GateParams { const void* x; int8_t* y; float* scale; int64_t ldx, ldy, rows; int C, act, once; };
 
 template <class T, int NV, int TPR, int BLOCK, bool GATED, bool SHORT>
 __global__ __launch_bounds__(BLOCK) void gated_kernel(GateParams P) {
@@ -156,12 +157,21 @@ __global__ __launch_bounds__(BLOCK) void gated_kernel(GateParams P) {
     Raw a[NV], b[NV];
     Piece p[NV];
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-        p[v] = SHORT ? Piece{0, t ? 8 : 0} : piece_of(t + TPR * v, C);
-        if (SHORT) {
-            a[v] = __builtin_convertvector(load_some(x, C), Raw);
-            if (GATED) b[v] = __builtin_convertvector(load_some(x + C, C), Raw);
-        } else {
+    for (int v = 0; v < NV; ++v) p[v] = SHORT ? Piece{0, t ? 8 : 0} : piece_of(t + TPR * v, C);
+    if (SHORT) {
+        a[0] = __builtin_convertvector(load_some(x, C), Raw);
+        if (GATED) b[0] = __builtin_convertvector(load_some(x + C, C), Raw);
+    } else if (P.once) {
+        keep_apart();
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            a[v] = __builtin_nontemporal_load(reinterpret_cast<const Mem*>(x + p[v].at));
+            if (GATED) b[v] = __builtin_nontemporal_load(reinterpret_cast<const Mem*>(x + C + p[v].at));
+        }
+        keep_apart();
+    } else {
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
             a[v] = *reinterpret_cast<const Mem*>(x + p[v].at);
             if (GATED) b[v] = *reinterpret_cast<const Mem*>(x + C + p[v].at);
         }
@@ -193,8 +203,8 @@ __global__ __launch_bounds__(BLOCK) void gated_kernel(GateParams P) {
 }
 
 // f(NV, TPR, BLOCK, SHORT) for rows of C elements.  Many rows: as few threads a row as hold it in up to three pieces each, so that hardly
-// a thread is idle, and a workgroup for every wavefront (bf16 norms with a residual, us: 25216 x 384 13.6, with four wavefronts a workgroup
-// 15.2; 25216 x 768 28.3, with 256 threads a row 49.9; 20000 x 1536, activation alone, 30.9 and 36.9); from 1537 to 2048 elements 256 threads
+// a thread is idle, and a workgroup for every wavefront (bf16 norms with a residual, us, with ordinary stores: 25216 x 384 13.6, with four wavefronts a
+// workgroup 15.2; 25216 x 768 28.3, with 256 threads a row 49.9; 20000 x 1536, activation alone, 30.9 and 36.9); from 1537 to 2048 elements 256 threads
 // have one piece each (10000 x 2048 29.9, with 64 threads 32.0; 5003 x 2049 10.9 with 128 threads, 11.5 with 256).  Few rows, where a launch
 // is a chain of latencies: 256 threads from 513 elements on (197 x 1536, activation alone, 2.9 and 3.6).
 template <class F> hipError_t with_group(int64_t rows, int C, F&& f) {
@@ -248,13 +258,16 @@ template <class T> hipError_t norm_of(hipStream_t s, const RmsNormArgs& a) {
 }
 
 template <class T> hipError_t gate_of(hipStream_t s, const GatedArgs& a) {
+    // x past the caches from 32 MB on (8192 x 14336 gated 100 and 96 us, 20000 x 1536, 61 MB, 29.4 and 27.5; 1000 x 4096 gated, 16 MB, 6.1 and 6.1; 197 x 1536 2.95
+    // and 3.3).  The norm's inputs, residual and all, are better left alone (25216 x 384 13.7 and 16.6, 16384 x 4096 82 and 79.5).
+    const int once = a.rows * a.C * (int64_t)sizeof(T) * (a.gated ? 2 : 1) >= (int64_t)1 << 25;
     return with_group(a.rows, a.C, [&](auto nv, auto tpr, auto block, auto few) {
         constexpr int NV = nv, TPR = tpr, BLOCK = block, ROWS = BLOCK / TPR;
         constexpr bool SHORT = few;
         constexpr int64_t MOST = kThreads / BLOCK * ROWS;
         for (int64_t r = 0; r < a.rows; r += MOST) {
             const int64_t rows = min64(a.rows - r, MOST), grid = (rows + ROWS - 1) / ROWS;
-            const GateParams P{static_cast<const T*>(a.x) + r * a.ldx, a.y + r * a.ldy, a.y_scale + r, a.ldx, a.ldy, rows, a.C, a.act};
+            const GateParams P{static_cast<const T*>(a.x) + r * a.ldx, a.y + r * a.ldy, a.y_scale + r, a.ldx, a.ldy, rows, a.C, a.act, once};
             TraceScope trace(s, KIND_GATED, 0, rows * a.C * ((int64_t)sizeof(T) * (a.gated ? 2 : 1) + 1));
             if (a.gated) hipLaunchKernelGGL((gated_kernel<T, NV, TPR, BLOCK, true, SHORT>), dim3((unsigned)grid), dim3(BLOCK), 0, s, P);
             else hipLaunchKernelGGL((gated_kernel<T, NV, TPR, BLOCK, false, SHORT>), dim3((unsigned)grid), dim3(BLOCK), 0, s, P);

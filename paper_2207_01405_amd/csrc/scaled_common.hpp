@@ -84,6 +84,10 @@ template <class T> __device__ __forceinline__ void store_some(T* p, v8f v, int n
         if (e < n) p[e] = (T)v[e];
 }
 
+// Ahead of and behind the loads of one of two branches that differ in the kind of load alone: the compiler would make one of them, of the
+// ordinary kind.
+__device__ __forceinline__ void keep_apart() { asm volatile("" ::: "memory"); }
+
 // The nearest whole number (ties to even) of a b, |a b| < 2^22, in the low bits of the result: the sum with 1.5 2^23 has a unit
 // of 1 in its last place, and the multiply-add rounds once.
 __device__ __forceinline__ uint32_t round_bits(float a, float b) { return __float_as_uint(__builtin_fmaf(a, b, 12582912.0f)); }
