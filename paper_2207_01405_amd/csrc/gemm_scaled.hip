@@ -8,8 +8,8 @@
 //
 // What bounds the tiles is LDS, 128 bytes a cycle and CU for fragment reads and arriving loads alike: a stage of two 128 x 128 tiles a CU is
 // 1536 cycles of it for 1024 of products and takes 0.99 us, one of 256 x 256 (eight wavefronts of 128 x 64) 2048 for 2048 and 1.57 us at the
-// 1.7 GHz that this card keeps up then.  8192 x 8192 x 4096 with bf16 results 245 us, 2.24 POP/s (a product alone from registers runs at 3.2
-// to 3.3 on random data), 8192 x 8192 x 8192 2.47; with the residual 277 us.  Tried for 256 x 256 and taken back: four wavefronts of 128 x 128,
+// 1.7 GHz that this card keeps up then.  8192 x 8192 x 4096 with bf16 results 224 us, 2.45 POP/s (a product alone from registers runs at 3.2
+// to 3.3 on random data), 8192 x 8192 x 8192 2.47; with the residual 250 us.  Tried for 256 x 256 and taken back: four wavefronts of 128 x 128,
 // a quarter less LDS (497 against 465 us at K = 8192, then 461 against 451); stages of 64 bytes, four of them (473 against 451: half lines);
 // the residual's lines requested into L2 during the last stages (286 against 281) or a pass ahead (290 against 286); wave priorities (no change).
 #include "linear_rows.hpp"
@@ -45,7 +45,7 @@ struct TileOrder {
 
 struct GsParams {
     const int8_t* x; const float* x_scale; const int8_t* w; const float* w_scale; const float* bias; const void* residual; void* y;
-    int64_t ldx, ld_res, ldy, M; int N, K, act, one_scale, res_once; float inv_step;
+    int64_t ldx, ld_res, ldy, M; int N, K, act, one_scale, once; float inv_step;
     TileOrder order;
 };
 
@@ -75,7 +75,7 @@ template <int TYPE> struct Chunk {
         }
     }
     static __device__ __forceinline__ vf unpack(v4i v) { return __builtin_convertvector(__builtin_bit_cast(vt, v), vf); }
-    // a chunk past the L2
+    // a chunk past the L2, and one stored there
     static __device__ __forceinline__ v4i load_once(const T* p) { return __builtin_bit_cast(v4i, (vt)__builtin_nontemporal_load(reinterpret_cast<const mem*>(p))); }
     // the chunk at p, which may have the alignment of one element; of it n elements count, and `there` exist
     static __device__ __forceinline__ v4i load(const T* p, int n, int64_t there) {
@@ -86,9 +86,10 @@ template <int TYPE> struct Chunk {
             if (e < n) v[e] = p[e];
         return __builtin_bit_cast(v4i, v);
     }
+    static __device__ __forceinline__ void store_once(T* p, v4i w) { __builtin_nontemporal_store(__builtin_bit_cast(vt, w), reinterpret_cast<mem*>(p)); }
     static __device__ __forceinline__ void store(T* p, v4i w, int n) {
         const vt v = __builtin_bit_cast(vt, w);
-        if (n >= E) { __builtin_nontemporal_store(v, reinterpret_cast<mem*>(p)); return; }
+        if (n >= E) { *reinterpret_cast<mem*>(p) = v; return; }
 #pragma unroll
         for (int e = 0; e < E - 1; ++e)
             if (e < n) p[e] = v[e];
@@ -416,7 +417,7 @@ __global__ __launch_bounds__((64 * GM * GN), 2) void gemm_scaled_kernel(GsParams
                         const T* const res = static_cast<const T*>(P.residual) + mw * P.ld_res + c_mv;
                         if (whole) {
                             v4i r[SLOTS * MOVES];
-                            if (P.res_once) {
+                            if (P.once) {
                                 keep_apart();
 #pragma unroll
                                 for (int i = 0; i < SLOTS * MOVES; ++i) r[i] = CK::load_once(res + min(MV_ROWS * i + mv_row, left - 1) * P.ld_res);
@@ -471,7 +472,15 @@ __global__ __launch_bounds__((64 * GM * GN), 2) void gemm_scaled_kernel(GsParams
             __builtin_amdgcn_wave_barrier();
             if (PERSIST && t0 == 0) wait_vm0();               // the next tile's first stage, before stores stand in line behind it
             T* const y = static_cast<T*>(P.y) + mw * P.ldy + c_mv;
-            if (whole) {
+            if (whole && P.once) {
+                keep_apart();
+#pragma unroll
+                for (int i = 0; i < SLOTS * MOVES; ++i) {
+                    const v4i v = *reinterpret_cast<const v4i*>(at_mv(i));
+                    if (MV_ROWS * i + mv_row < left) CK::store_once(y + (MV_ROWS * i + mv_row) * P.ldy, v);
+                }
+                keep_apart();
+            } else if (whole) {
 #pragma unroll
                 for (int i = 0; i < SLOTS * MOVES; ++i) {
                     const v4i v = *reinterpret_cast<const v4i*>(at_mv(i));
@@ -503,10 +512,11 @@ template <int TYPE, int MT, int NT, int GM, int GN, int S> hipError_t launch_til
     P.x = a.x; P.x_scale = a.x_scale; P.w = a.w; P.w_scale = a.w_scale; P.bias = a.bias; P.residual = a.residual; P.y = a.y;
     P.ldx = a.ldx; P.ld_res = a.ld_res; P.ldy = a.ldy; P.M = a.M; P.N = a.N; P.K = a.K; P.act = a.act; P.one_scale = a.one_scale;
     P.inv_step = a.inv_step;
-    // Results are stored past the L2, which has the operands to keep and would write them back at the launch's end (8192 x 8192 x 4096 246 -> 230 us,
-    // 50432 x 768 x 768 54 -> 47).  A residual of 64 MB and more is loaded past it, and past the last-level cache, too (bf16, 8192 x 8192 x 4096, 134 MB, 284 and
-    // 258 us; 50432 x 768 x 768, 77 MB, 67 and 64.6); smaller ones may still be in that cache (4096 x 4096 x 4096, 34 MB, 67 and 70; 25216 x 384 x 1536 28.0 and 30.0).
-    P.res_once = a.M * a.N * (int64_t)sizeof(Stored<TYPE>) >= (int64_t)1 << 26;
+    // From 64 MB on, results are stored past the L2, which has the operands to keep and would write them back at the launch's end
+    // (8192 x 8192 x 4096 246 -> 224 us, 50432 x 768 x 768 54 -> 46), and a residual is loaded past it (8192 x 8192 x 4096, 284 and 258 us;
+    // 50432 x 768 x 768 67 and 64.6).  Smaller ones stay in the caches for whoever reads them next (25216 x 1152 x 384 with int8
+    // results and a pass over them 70 us for 81; residuals: 4096 x 4096 x 4096, 34 MB, 67 and 70; 25216 x 384 x 1536 28.0 and 30.0).
+    P.once = a.M * a.N * (int64_t)sizeof(Stored<TYPE>) >= (int64_t)1 << 26;
     const int64_t tm = (a.M + TL::TM - 1) / TL::TM, tn = (a.N + TL::TN - 1) / TL::TN;
     int64_t grid = (tm * tn + NXCD - 1) / NXCD * NXCD;
     P.order = TileOrder((uint32_t)tm, (uint32_t)tn, (uint32_t)(tm < kBand ? tm : kBand));

@@ -4,11 +4,13 @@
 //   norm:  h = x + r,  n = h / sqrt(mean(h^2) + eps) gamma        gate:  v = act(g) u  or  act(g)
 //   s = max |v| / 127,  q = round(v / s)
 //
-// Both are bound by memory: an element is 10 to 20 operations for 3 to 7 bytes.  Results are stored past the L2 (norms of 25216 x 768 29.2 -> 23.2 us,
-// 16384 x 4096 85.7 -> 81.8).  A group of TPR threads holds a row in
+// Both are bound by memory: an element is 10 to 20 operations for 3 to 7 bytes.  A group of TPR threads holds a row in
 // registers, NV pieces of eight elements a thread, so that x is read once; one reduction over the group gives the norm its sum of
 // squares and its largest |h gamma| together: the factor 1 / sqrt(..) is the same for a row's elements, so q needs h gamma only
-// and s takes the factor once.
+// and s takes the factor once.  Norms of 16384 x 4096 bf16 with a residual take 85 us (5.5 TB/s), 25216 x 384 14.4 (4.7), the gated
+// activation of 8192 x 14336 bf16 101 (5.8).  Results go through the caches, since the product after them reads them: stored past
+// the L2 the norm gets faster (16384 x 4096 82 us, 25216 x 768 23.5 for 28.6) and what follows slower by more (norm, Dense 768 -> 2048,
+// activation and Dense 2048 -> 768 of 50432 rows 355 for 338).
 #include "scaled_common.hpp"
 
 namespace ivit {
@@ -57,7 +59,7 @@ __device__ __forceinline__ void store_q(int8_t* p, const v8f& v, const Quant& q,
     for (int e = 0; e < 8; ++e) w[e] = q.inv == 0.0f ? 0u : round_bits(v[e] * q.up, q.inv);
     typedef uint32_t v2u __attribute__((ext_vector_type(2), aligned(1)));
     const v2u out = {pack4(w[0], w[1], w[2], w[3]), pack4(w[4], w[5], w[6], w[7])};
-    if (n >= 8) { __builtin_nontemporal_store(out, reinterpret_cast<v2u*>(p)); return; }
+    if (n >= 8) { *reinterpret_cast<v2u*>(p) = out; return; }
 #pragma unroll
     for (int e = 0; e < 7; ++e)
         if (e < n) p[e] = (int8_t)(out[e >> 2] >> (8 * (e & 3)));

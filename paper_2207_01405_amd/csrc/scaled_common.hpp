@@ -68,7 +68,7 @@ template <class T> __device__ __forceinline__ v8f load8(const T* p) {
     return __builtin_convertvector(v, v8f);
 }
 template <class T> __device__ __forceinline__ void store8(T* p, v8f v) {
-    __builtin_nontemporal_store((typename Eight<T>::mem)__builtin_convertvector(v, typename Eight<T>::at), reinterpret_cast<typename Eight<T>::mem*>(p));
+    *reinterpret_cast<typename Eight<T>::mem*>(p) = __builtin_convertvector(v, typename Eight<T>::at);
 }
 // ... the first n < 8 of them; the others are 0
 template <class T> __device__ __forceinline__ v8f load_some(const T* p, int n) {
