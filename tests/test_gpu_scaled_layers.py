@@ -443,6 +443,39 @@ def test_dense_equal_calls_give_equal_bits(ivit):
         assert torch.equal(a[:1], run_dense(ivit, one, "f32", "gelu"))
 
 
+@pytest.mark.parametrize("M,N,K,t", [(16411, 1091, 64, "f32"), (16411, 2053, 784, "bf16"), (33333, 1031, 784, "f16"), (33333, 2053, 64, "i8")])
+def test_dense_large_results_equal_those_of_their_parts(ivit, M, N, K, t):
+    """Results of 64 MB and more, which are stored another way, against calls for a part of the rows: the same bits; a residual in place."""
+    import torch
+    d = dense_case(8, M, N, K, t, t != "i8", True, False)
+    step = 0.05 if t == "i8" else None
+    y, buf, outside = guarded(M, N, N + 5, dtype(t), 77, shift=1)
+    rows = [(0, 300), (M // 2 - 7, M // 2 + 450), (M - 301, M)]
+    part = lambda a, b: dict(d, x=d["x"][a:b], x_scale=d["x_scale"][a:b], residual=None if t == "i8" else d["residual"][a:b])
+    want = [run_dense(ivit, part(a, b), t, "silu", step) for a, b in rows]
+    run_dense(ivit, d, t, "silu", step, y=y)
+    assert all(torch.equal(y[a:b], w) for (a, b), w in zip(rows, want))
+    assert bool((buf[outside] == 77).all())
+    if t != "i8":
+        whole = y.clone()
+        y.copy_(d["residual"])
+        run_dense(ivit, dict(d, residual=y), t, "silu", y=y)
+        assert torch.equal(y, whole) and bool((buf[outside] == 77).all())
+
+
+@pytest.mark.parametrize("rows,C,t,gated", [(5003, 2049, "bf16", True), (9001, 1023, "f32", False), (2100, 4099, "f16", True)])
+def test_gate_of_many_rows_equals_that_of_its_parts(ivit, rows, C, t, gated):
+    """32 MB and more, which are loaded another way (16-bit rows of the last case: 34 MB), against calls for a part of the rows."""
+    import torch
+    x = rand(gen(rows), rows, C * (1 + gated)).to(dtype(t))
+    q = torch.empty(rows, C, dtype=torch.int8, device="cuda"); s = torch.empty(rows, device="cuda")
+    ivit.ivit_gated_quant(x, q, s, act="gelu", gated=gated)
+    for a, b in ((0, 700), (rows // 2 + 3, rows // 2 + 900), (rows - 517, rows)):
+        p = torch.empty(b - a, C, dtype=torch.int8, device="cuda"); ps = torch.empty(b - a, device="cuda")
+        ivit.ivit_gated_quant(x[a:b], p, ps, act="gelu", gated=gated)
+        assert torch.equal(q[a:b], p) and torch.equal(s[a:b], ps)
+
+
 def test_offsets_beyond_32_bits(ivit):
     """Results and rows more than 2^32 bytes from the first one."""
     import torch
