@@ -421,7 +421,8 @@ int ivit_forward_swin(void* stream, const int8_t* patches, int8_t* logits, const
  *    alignment of one element only.
  *  - Sums, norms and the epilogue are held in 32 bits; int8 products are summed exactly.  A value is rounded once,
  *    where it is stored, to nearest, ties to even.  A float result beyond the range of its type becomes infinite.
- *  - An int8 row q with scale s stands for s q.  s = max |v| / 127 and q = round(v / s) over the row's values v; a row of
+ *  - An int8 row q with scale s stands for s q.  Over the row's values v, held in 32 bits, s = max |v| / 127 (rounded to 32 bits) and
+ *    q = round(127 v / max |v|), the exact quotient's nearest whole number, ties to even; a row of
  *    zeros has s = 0 and zeros, a row that holds a NaN or an infinite value (or whose largest leaves the range of
  *    float32) has s = NaN and zeros.
  *  - Equal calls give equal bits; a row of ivit_linear_scaled comes out the same whatever rows are beside it. */

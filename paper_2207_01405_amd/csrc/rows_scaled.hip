@@ -20,15 +20,15 @@ using namespace scaled;
 
 constexpr uint32_t kInf = 0x7f800000u;         // the bits of |v|, as unsigned numbers, are in the order of |v|; NaN comes last
 
-// What a row's int8 form needs: the factors of v, and the scale of a row whose v still lack `factor`.  A row of zeros (or whose
-// factor leaves nothing of it) has the scale 0; a row with a NaN or an infinite value NaN, and zeros.
-struct Quant { float up, inv, scale; };
+// What a row's int8 form needs: the largest |v|, 127 / it in 32 bits, and the scale of a row whose v still lack `factor`.  A row of zeros (or
+// whose factor leaves nothing of it) has the scale 0; a row with a NaN or an infinite value NaN; both count as rows with a largest of 0: zeros.
+struct Quant { float top, inv, scale; };
 __device__ __forceinline__ Quant quant_of(uint32_t top_bits, float factor) {
     const float top = __uint_as_float(top_bits);
     if (top_bits >= kInf) return Quant{0.0f, 0.0f, __uint_as_float(0x7fc00000u)};
-    const float scale = top * factor / 127.0f, up = top < 0x1p-90f ? 0x1p64f : 1.0f;      // (127 / top has to be finite)
+    const float scale = top * factor / 127.0f;
     if (scale == 0.0f) return Quant{0.0f, 0.0f, 0.0f};
-    return Quant{up, 127.0f / (top * up), scale};
+    return Quant{top, 127.0f / top, scale};
 }
 
 template <int TPR, int BLOCK> struct Group {
@@ -53,10 +53,26 @@ template <int TPR, int BLOCK> struct Group {
     }
 };
 
+// q = round(127 v / top), ties to even, of the exact quotient.  v inv is within 127 units of 2^-24 of it, so a value whose v inv is not that near a
+// tie is rounded as it stands, by one multiply-add.  Next to ties (half of the largest is one: 63.5) 64 bits decide: there the quotient is
+// within 2^-45, a quotient of two 24-bit numbers that is no tie is 2^-32 from one at least, and adding and taking away 1.5 2^12 leaves it at a
+// multiple of 2^-40, ties as they are.  Tiny rows, whose inv may not be finite, go the same way.
 __device__ __forceinline__ void store_q(int8_t* p, const v8f& v, const Quant& q, int n) {
     uint32_t w[8];
+    float far = 0.0f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) w[e] = q.inv == 0.0f ? 0u : round_bits(v[e] * q.up, q.inv);
+    for (int e = 0; e < 8; ++e) {
+        w[e] = round_bits(v[e], q.inv);
+        far = __builtin_fmaxf(far, __builtin_fabsf(__builtin_fmaf(v[e], q.inv, kRound - __uint_as_float(w[e]))));
+    }
+    if (far >= 0.5f - 0x1p-16f || q.top < 0x1p-100f) {
+        const double up = q.top > 0.0f ? 127.0 / (double)q.top : 0.0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const double d = __builtin_fma((double)v[e], up, 6144.0) - 6144.0;
+            w[e] = q.top > 0.0f ? (uint32_t)(int32_t)__builtin_rint(d) : 0u;
+        }
+    }
     typedef uint32_t v2u __attribute__((ext_vector_type(2), aligned(1)));
     const v2u out = {pack4(w[0], w[1], w[2], w[3]), pack4(w[4], w[5], w[6], w[7])};
     if (n >= 8) { *reinterpret_cast<v2u*>(p) = out; return; }

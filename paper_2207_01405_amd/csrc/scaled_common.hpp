@@ -90,7 +90,8 @@ __device__ __forceinline__ void keep_apart() { asm volatile("" ::: "memory"); }
 
 // The nearest whole number (ties to even) of a b, |a b| < 2^22, in the low bits of the result: the sum with 1.5 2^23 has a unit
 // of 1 in its last place, and the multiply-add rounds once.
-__device__ __forceinline__ uint32_t round_bits(float a, float b) { return __float_as_uint(__builtin_fmaf(a, b, 12582912.0f)); }
+constexpr float kRound = 12582912.0f;
+__device__ __forceinline__ uint32_t round_bits(float a, float b) { return __float_as_uint(__builtin_fmaf(a, b, kRound)); }
 // the low bytes of four words
 __device__ __forceinline__ uint32_t pack4(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     return __builtin_amdgcn_perm(b, a, 0x0c0c0400u) | __builtin_amdgcn_perm(d, c, 0x04000c0cu);
