@@ -33,7 +33,8 @@ __device__ __forceinline__ float gelu_erf(float x) {
     p = __builtin_fmaf(p, z, -0.4591396450996399f);
     p = __builtin_fmaf(p, z, -1.1511139869689941f);
     p = __builtin_fmaf(p, z, -0.9999998211860657f);
-    return __builtin_fmaxf(x, 0.0f) - __builtin_fminf(z, 0x1p100f) * __builtin_amdgcn_exp2f(p);      // (an infinite x: 0)
+    // (+inf: the second term is 0; -inf: NaN, as x Phi(x) and the other forms here give, so that an overflow does not pass for a 0)
+    return __builtin_fmaxf(x, 0.0f) - __builtin_fabsf(__builtin_fminf(x, 0x1p100f)) * __builtin_amdgcn_exp2f(p);
 }
 
 template <int ACT> __device__ __forceinline__ float activation(float x) {
