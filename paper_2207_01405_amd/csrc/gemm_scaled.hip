@@ -458,7 +458,7 @@ __global__ __launch_bounds__((64 * GM * GN), 2) void gemm_scaled_kernel(GsParams
 #pragma unroll
                         for (int e = 0; e < CK::E; ++e) {
                             constexpr int PER = 16 / CK::E;   // chunks of the 16 results of an MFMA tile
-                            v[e] = activation<decltype(act)::value>(__builtin_fmaf((float)acc[j / PER][tt][CK::E * (j % PER) + e] * ws[e], xs[tt], bi[e]));
+                            v[e] = activation<decltype(act)::value, TYPE == TYPE_F32>(__builtin_fmaf((float)acc[j / PER][tt][CK::E * (j % PER) + e] * ws[e], xs[tt], bi[e]));
                         }
                         if constexpr (TYPE != TYPE_I8) {
                             if (P.residual) v += CK::unpack(*reinterpret_cast<const v4i*>(at));

@@ -159,8 +159,10 @@ __global__ __launch_bounds__(64 * W) void gemm_scaled_rows_kernel(ScaledArgs P, 
     float v[4];
     with_activation(P.act, [&](auto act) __attribute__((always_inline)) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            v[e] = activation<decltype(act)::value>(__builtin_fmaf((float)sum[e] * value_of(ws, e, TYPE_F32), xs, value_of(bi, e, TYPE_F32)));
+        for (int e = 0; e < 4; ++e) {
+            v[e] = __builtin_fmaf((float)sum[e] * value_of(ws, e, TYPE_F32), xs, value_of(bi, e, TYPE_F32));
+            v[e] = P.y_type == TYPE_F32 ? activation<decltype(act)::value, true>(v[e]) : activation<decltype(act)::value, false>(v[e]);
+        }
     });
     const int64_t at = (m0 + row) * P.ldy + n;
     if (P.y_type == TYPE_I8) {

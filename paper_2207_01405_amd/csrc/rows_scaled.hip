@@ -33,23 +33,44 @@ __device__ __forceinline__ Quant quant_of(uint32_t top_bits, float factor) {
 
 template <int TPR, int BLOCK> struct Group {
     static constexpr int ROWS = BLOCK / TPR, WAVES = TPR > 64 ? TPR / 64 : 1;
-    // the sum and the largest of the bits over the threads of a row, every one of them getting both
-    static __device__ __forceinline__ void reduce(float& sum, uint32_t& top) {
+    static_assert(TPR <= 64 || TPR == BLOCK, "a row of several wavefronts is the workgroup's");
+    // one(a, b) of a value and the largest of the bits over the threads of a row, every one of them getting both.  AGAIN: a call for the same
+    // rows was before it.
+    template <bool AGAIN, class One> static __device__ __forceinline__ void reduce(float& value, uint32_t& top, One&& one) {
 #pragma unroll
         for (int m = (TPR < 64 ? TPR : 64) / 2; m > 0; m >>= 1) {
-            sum += __shfl_xor(sum, m);
+            value = one(value, __shfl_xor(value, m));
             top = max(top, (uint32_t)__shfl_xor((int)top, m));
         }
         if constexpr (TPR > 64) {
-            static_assert(TPR == BLOCK, "a row of several wavefronts is the workgroup's");
             __shared__ float s[WAVES];
             __shared__ uint32_t t[WAVES];
-            if ((threadIdx.x & 63) == 0) { s[threadIdx.x >> 6] = sum; t[threadIdx.x >> 6] = top; }
+            if (AGAIN) __syncthreads();
+            if ((threadIdx.x & 63) == 0) { s[threadIdx.x >> 6] = value; t[threadIdx.x >> 6] = top; }
             __syncthreads();
-            sum = 0.0f; top = 0;
+            value = s[0]; top = t[0];
 #pragma unroll
-            for (int w = 0; w < WAVES; ++w) { sum += s[w]; top = max(top, t[w]); }
+            for (int w = 1; w < WAVES; ++w) { value = one(value, s[w]); top = max(top, t[w]); }
         }
+    }
+    // The largest of the bits alone; and whether a wavefront of the row (for short rows: the row) had a thread whose `wide` is more than eight
+    // times the largest there.  If the row's largest is that small against a `wide` of the row, it is so.
+    static __device__ __forceinline__ bool largest(uint32_t& top, float wide) {
+#pragma unroll
+        for (int m = (TPR < 64 ? TPR : 64) / 2; m > 0; m >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, m));
+        uint64_t small = __ballot(8.0f * __uint_as_float(top) < wide);
+        if constexpr (TPR < 64) small &= ((1ull << TPR) - 1) << (threadIdx.x & 63 & ~(TPR - 1));
+        if constexpr (TPR > 64) {
+            __shared__ uint32_t t[WAVES], any[WAVES];
+            if ((threadIdx.x & 63) == 0) { t[threadIdx.x >> 6] = top; any[threadIdx.x >> 6] = small != 0; }
+            __syncthreads();
+            top = t[0];
+            uint32_t a = any[0];
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w) { top = max(top, t[w]); a |= any[w]; }
+            return a != 0;
+        }
+        return small != 0;
     }
 };
 
@@ -139,7 +160,7 @@ __global__ __launch_bounds__(BLOCK) void rmsnorm_kernel(NormParams P) {
             for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(h[v][e] * g[v][e]) & 0x7fffffffu);
         }
     }
-    G::reduce(sum, top);
+    G::template reduce<false>(sum, top, [](float a, float b) __attribute__((always_inline)) { return a + b; });
     const float factor = 1.0f / __builtin_sqrtf(sum / (float)C + P.eps);
     const Quant q = quant_of(top, factor);
     if (mine >= P.rows) return;
@@ -160,6 +181,18 @@ __global__ __launch_bounds__(BLOCK) void rmsnorm_kernel(NormParams P) {
             if (SHORT) store_some(y, h[v] * factor, n); else store8(y, h[v] * factor);
         }
     }
+}
+
+// (one instruction; of __builtin_fminf and __builtin_fmaxf on values that come from memory the compiler makes two for each)
+__device__ __forceinline__ float min3(float a, float b, float c) {
+    float m;
+    asm("v_min3_f32 %0, %1, %2, %3" : "=v"(m) : "v"(a), "v"(b), "v"(c));
+    return m;
+}
+__device__ __forceinline__ float max3_abs(float a, float b, float c) {
+    float m;
+    asm("v_max3_f32 %0, %1, |%2|, |%3|" : "=v"(m) : "v"(a), "v"(b), "v"(c));
+    return m;
 }
 
 struct GateParams { const void* x; int8_t* y; float* scale; int64_t ldx, ldy, rows; int C, act, once; };
@@ -195,23 +228,53 @@ __global__ __launch_bounds__(BLOCK) void gated_kernel(GateParams P) {
         }
     }
     v8f h[NV];
-    float none = 0.0f;
+    // GELU falls so fast below 0 that a row's largest value can be far smaller than what goes into it.  gelu_erf is within 2^-23 |x|: where the largest
+    // is below an eighth of `wide`, the most that |x| |u| with x < 0 can be, the row is formed again by gelu_tail, from x anew (the
+    // registers that would hold it until then are worth more).  In all others the values are within 2^-20 of the largest.
+    float wide = 0.0f;
     uint32_t top = 0;
-    auto form = [&](auto act) __attribute__((always_inline)) {
+    auto form = [&](auto act, auto tail_c) __attribute__((always_inline)) {
+        constexpr bool TAIL = decltype(tail_c)::value, WIDE = !TAIL && decltype(act)::value == ACT_GELU;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const v8f f = __builtin_convertvector(a[v], v8f);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) h[v][e] = activation<decltype(act)::value>(f[e]);
-            if (GATED) h[v] *= __builtin_convertvector(b[v], v8f);
+            for (int e = 0; e < 8; ++e) h[v][e] = activation<decltype(act)::value, TAIL>(f[e]);
+            float low = 0.0f, by = GATED ? 0.0f : 1.0f;
+            if (WIDE) {
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) low = min3(low, f[e], f[e + 1]);
+            }
+            if (GATED) {
+                const v8f u = __builtin_convertvector(b[v], v8f);
+                h[v] *= u;
+                if (WIDE) {
+#pragma unroll
+                    for (int e = 0; e < 8; e += 2) by = max3_abs(by, u[e], u[e + 1]);
+                }
+            }
+            if (WIDE) wide = __builtin_fmaxf(wide, -low * by);
         }
+        top = 0;
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(h[v][e]) & 0x7fffffffu);
     };
-    with_activation(P.act, form);
+    with_activation(P.act, [&](auto act) __attribute__((always_inline)) { form(act, std::false_type()); });
+    if (G::largest(top, wide)) {
+        auto more = [](float a, float b) __attribute__((always_inline)) { return __builtin_fmaxf(a, b); };
+        G::template reduce<false>(wide, top, more);
+        if (8.0f * __uint_as_float(top) < wide) {
 #pragma unroll
-    for (int v = 0; v < NV; ++v)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(h[v][e]) & 0x7fffffffu);
-    G::reduce(none, top);
+            for (int v = 0; v < NV; ++v) {
+                a[v] = SHORT ? __builtin_convertvector(load_some(x, C), Raw) : *reinterpret_cast<const Mem*>(x + p[v].at);
+                if (GATED) b[v] = SHORT ? __builtin_convertvector(load_some(x + C, C), Raw) : *reinterpret_cast<const Mem*>(x + C + p[v].at);
+            }
+            form(std::integral_constant<int, ACT_GELU>(), std::true_type());
+            G::template reduce<true>(wide, top, more);
+        }
+    }
     const Quant q = quant_of(top, 1.0f);
     if (mine >= P.rows) return;
     if (t == 0) P.scale[row] = q.scale;

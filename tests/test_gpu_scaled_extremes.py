@@ -69,3 +69,98 @@ def test_infinite_sums_of_the_dense(ivit, act):
                 assert bool((torch.isnan(y[:, 3]) if math.isnan(low) else y[:, 3] == low).all())
                 rest = torch.ones(N, dtype=torch.bool, device="cuda"); rest[3] = rest[N - 1] = False
                 assert bool(torch.isfinite(y[:, rest]).all())
+
+
+# -------------------------------------------------------------------------------------------------- tails of activations
+def exactly(x, act):
+    """In 64 bits, the tails to their last places."""
+    import torch
+    x = x.double()
+    if act == "gelu":
+        return 0.5 * x * torch.special.erfc(-x / math.sqrt(2.0))
+    slope = {"silu": x, "gelu_sigmoid": 1.702 * x, "gelu_tanh": 2.0 * math.sqrt(2.0 / math.pi) * (x + 0.044715 * x ** 3)}[act]
+    return x / (1.0 + torch.exp(-slope))
+
+
+def share(x):
+    """The stated error of an activation, relative to its value."""
+    x = x.double().abs()
+    return (12 + 10 * x + x ** 3) * U
+
+
+TAILS = [("gelu", -9, -4), ("gelu", -12, -8), ("gelu", -4, -1), ("gelu", -1e-3, 0), ("silu", -80, -20), ("gelu_tanh", -8, -4), ("gelu_sigmoid", -45, -10)]
+
+
+def between(lo, hi, shape, t, seed):
+    import torch
+    return (lo + (hi - lo) * torch.rand(shape, generator=gen(seed), device="cuda")).to(dtype(t))
+
+
+def check_rows(q, s, v, rel, more):
+    """int8 rows of values known to within rel |v| + more; the quotient's 3 U"""
+    import torch
+    top, at = v.abs().max(1)
+    rel_top = rel.gather(1, at[:, None])[:, 0]
+    err_top = rel_top * top + more
+    # another element may have come out as the largest, if it is within both errors: its own error counts then
+    err_top = torch.maximum(err_top, (rel * v.abs()).amax(1) + more)
+    assert bool(((s.double() - top / 127).abs() <= err_top / 127 + 3 * U * top / 127).all()), "scale"
+    off, step = (q.double() * (top / 127)[:, None] - v).abs(), (top / 127)[:, None]
+    assert bool((off <= 0.5 * step * (1 + 8 * U) + rel * v.abs() + more[:, None] + err_top[:, None] / top[:, None] * v.abs()).all()), "rows"
+
+
+@pytest.mark.parametrize("act,lo,hi", TAILS)
+@pytest.mark.parametrize("gated", [True, False])
+def test_rows_that_lie_in_the_tail_have_scales_of_their_own(ivit, act, lo, hi, gated):
+    import torch
+    for t in TYPES:
+        if t == "f16" and act == "gelu" and lo == -1e-3:
+            continue                                    # (below its normal numbers)
+        for C in (3, 64, 200, 1000, 2049, 5001, 20000):
+            rows = 37
+            g = between(lo, hi, (rows, C), t, C)
+            x = torch.cat([g, torch.randn((rows, C), generator=gen(C + 1), device="cuda").to(dtype(t))], 1) if gated else g
+            q, s = torch.full((rows, C), 99, dtype=torch.int8, device="cuda"), torch.empty(rows, device="cuda")
+            ivit.ivit_gated_quant(x, q, s, act=act, gated=gated)
+            v = exactly(g, act) * (x[:, C:].double() if gated else 1.0)
+            more = torch.zeros(rows, dtype=torch.float64, device="cuda")
+            if act == "gelu":                           # (rows whose largest is no less than an eighth of what goes into it)
+                wide = (x[:, C:].double().abs().amax(1) if gated else 1.0) * g.double().abs().amax(1)
+                more = torch.where(8 * v.abs().amax(1) >= 0.5 * wide, v.abs().amax(1) * 2.0 ** -20, more)
+            check_rows(q, s, v, share(g) + U, more)
+
+
+@pytest.mark.parametrize("gated", [True, False])
+def test_rows_with_some_values_in_the_tail(ivit, gated):
+    import torch
+    for C in (7, 100, 1536, 5001):
+        rows = 70
+        g = between(-9, -3, (rows, C), "f32", C)
+        g[::2, C // 2] = 10.0 ** torch.linspace(-5, 1, 35, device="cuda")       # (largest values from the tail's size to ordinary ones, by turns)
+        x = torch.cat([g, torch.ones_like(g)], 1) if gated else g
+        q, s = torch.full((rows, C), 99, dtype=torch.int8, device="cuda"), torch.empty(rows, device="cuda")
+        ivit.ivit_gated_quant(x, q, s, act="gelu", gated=gated)
+        v = exactly(g, "gelu")
+        check_rows(q, s, v, share(g) + U, v.abs().amax(1) * 2.0 ** -20)
+        # a row's values do not depend on its neighbours
+        one, s1 = torch.empty((1, C), dtype=torch.int8, device="cuda"), torch.empty(1, device="cuda")
+        for r in (0, 1, 34, 68, 69):
+            ivit.ivit_gated_quant(x[r:r + 1], one, s1, act="gelu", gated=gated)
+            assert torch.equal(one[0], q[r]) and float(s1) == float(s[r])
+
+
+@pytest.mark.parametrize("act,lo,hi", TAILS)
+@pytest.mark.parametrize("t", TYPES)
+def test_tails_in_the_epilogue_of_the_dense(ivit, act, lo, hi, t):
+    """Sums of 0, so that the bias alone, known exactly, goes into the activation."""
+    import torch
+    half = torch.finfo(dtype(t)).eps / 2
+    least = {"f32": 2.0 ** -118, "f16": 2.0 ** -25, "bf16": 2.0 ** -118}[t]
+    for M, N, K in ((1, 200, 64), (16, 2000, 512), (40, 515, 128), (300, 270, 256), (1200, 1300, 96), (4000, 2100, 1024), (20000, 1031, 80)):
+        bias = between(lo, hi, (N,), "f32", N)
+        y = torch.full((M, N), 99, dtype=dtype(t), device="cuda")
+        ivit.ivit_linear_scaled(torch.zeros((M, K), dtype=torch.int8, device="cuda"), torch.ones(M, device="cuda"), torch.ones((N, K), dtype=torch.int8, device="cuda"),
+                                torch.ones(N, device="cuda"), y, bias=bias, act=act)
+        v = exactly(bias, act)
+        err = share(bias) * v.abs() if t == "f32" or act != "gelu" else 2.0 ** -23 * bias.double().abs()
+        assert bool(((y.double() - v).abs() <= err + half * (v.abs() + err) + least).all()), (M, N, K)
