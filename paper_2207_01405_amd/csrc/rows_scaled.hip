@@ -21,12 +21,14 @@ using namespace scaled;
 constexpr uint32_t kInf = 0x7f800000u;         // the bits of |v|, as unsigned numbers, are in the order of |v|; NaN comes last
 
 // What a row's int8 form needs: the largest |v|, 127 / it in 32 bits, and the scale of a row whose v still lack `factor`.  A row of zeros (or
-// whose factor leaves nothing of it) has the scale 0; a row with a NaN or an infinite value NaN; both count as rows with a largest of 0: zeros.
+// whose factor leaves nothing of it) has the scale 0; a row with a NaN or an infinite value, or with one that the factor takes beyond the range,
+// NaN; both count as rows with a largest of 0: zeros.
 struct Quant { float top, inv, scale; };
 __device__ __forceinline__ Quant quant_of(uint32_t top_bits, float factor) {
     const float top = __uint_as_float(top_bits);
     if (top_bits >= kInf) return Quant{0.0f, 0.0f, __uint_as_float(0x7fc00000u)};
-    const float scale = top * factor / 127.0f;
+    const float most = top * factor, scale = most / 127.0f;
+    if (most > 0x1.fffffep127f) return Quant{0.0f, 0.0f, __uint_as_float(0x7fc00000u)};
     if (scale == 0.0f) return Quant{0.0f, 0.0f, 0.0f};
     return Quant{top, 127.0f / top, scale};
 }

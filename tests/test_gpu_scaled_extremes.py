@@ -164,3 +164,35 @@ def test_tails_in_the_epilogue_of_the_dense(ivit, act, lo, hi, t):
         v = exactly(bias, act)
         err = share(bias) * v.abs() if t == "f32" or act != "gelu" else 2.0 ** -23 * bias.double().abs()
         assert bool(((y.double() - v).abs() <= err + half * (v.abs() + err) + least).all()), (M, N, K)
+
+
+# ------------------------------------------------------------------------------------------- the norm's sums and products
+WIDTHS = [5, 64, 100, 500, 1000, 1536, 2049, 4096, 6000, 12000, 32768]
+
+
+def norm_of(ivit, x, gamma, eps, i8):
+    import torch
+    y = torch.full(x.shape, 99, dtype=torch.int8 if i8 else x.dtype, device="cuda")
+    s = torch.empty(x.shape[0], device="cuda") if i8 else None
+    total = torch.empty_like(x)
+    ivit.ivit_rmsnorm_quant(x, gamma, y, s, eps, residual=torch.zeros_like(x), sum_out=total)
+    assert torch.equal(total, x)
+    return y, s
+
+
+@pytest.mark.parametrize("C", [5, 64, 1000, 2049, 6000, 32768])
+def test_results_beyond_the_range_of_32_bits(ivit, C):
+    """The row's largest n beyond the range: NaN as its scale and zeros, and infinite where the result is of the stream's type."""
+    import torch
+    x = torch.ones((4, C), device="cuda")
+    x[2] = 0.0                                              # n of one element: sqrt(C), of the others 0
+    x[2, C // 2] = 1.0
+    x[3] = 0.0
+    gamma = torch.full((C,), 3e38, device="cuda")
+    gamma[0], x[:, 0] = 1.0, torch.tensor([1.0, 1e-30, 0.0, 0.0], device="cuda")
+    for scale in (1.0,):
+        y, s = norm_of(ivit, x * scale, gamma, 1e-12, True)
+        assert bool(torch.isnan(s[2])) and not bool(y[2].any()) and float(s[3]) == 0.0 and not bool(y[3].any())
+        assert bool(torch.isfinite(s[:2]).all())
+        y, _ = norm_of(ivit, x * scale, gamma, 1e-12, False)
+        assert float(y[2, C // 2]) == math.inf and not bool(y[3].any())
