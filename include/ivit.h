@@ -441,7 +441,8 @@ typedef enum { IVIT_ACT_NONE = 0, IVIT_ACT_RELU = 1, IVIT_ACT_SILU = 2, IVIT_ACT
  *   h = x + residual;   sum = h;   n = h / sqrt(mean(h^2) + eps) * gamma
  * x, residual (nullable), sum (nullable) [rows, C] of `type`; gamma float32 [C], nullable (ones).  n is formed from h
  * before its rounding to `type`.  Result: y_scale != NULL: int8 rows y [rows, C] and their scales y_scale [rows]; y_scale
- * == NULL: n itself, of `type`.  A mean square beyond the range of float32 counts as infinite (n = 0 where h is finite).
+ * == NULL: n itself, of `type`.  A mean square beyond the range of float32 counts as infinite (n = 0 where h is finite); an int8 row with
+ * |h| < 2^-75 and |h gamma| < 2^-150 throughout as zeros.
  * sum may be x or residual themselves, and so may a y of `type` (the same pointer and leading dimension; not both the same one);
  * no other overlap.
  * Requirements: 0 <= rows < 2^31, 1 <= C <= 32768, eps > 0 and finite.

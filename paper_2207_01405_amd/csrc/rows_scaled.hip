@@ -18,7 +18,7 @@ namespace {
 
 using namespace scaled;
 
-constexpr uint32_t kInf = 0x7f800000u;         // the bits of |v|, as unsigned numbers, are in the order of |v|; NaN comes last
+constexpr uint32_t kNormal = 0x00800000u, kInf = 0x7f800000u;      // the bits of |v|, as unsigned numbers, are in the order of |v|; NaN comes last
 
 // What a row's int8 form needs: the largest |v|, 127 / it in 32 bits, and the scale of a row whose v still lack `factor`.  A row of zeros (or
 // whose factor leaves nothing of it) has the scale 0; a row with a NaN or an infinite value, or with one that the factor takes beyond the range,
@@ -36,6 +36,9 @@ __device__ __forceinline__ Quant quant_of(uint32_t top_bits, float factor) {
 template <int TPR, int BLOCK> struct Group {
     static constexpr int ROWS = BLOCK / TPR, WAVES = TPR > 64 ? TPR / 64 : 1;
     static_assert(TPR <= 64 || TPR == BLOCK, "a row of several wavefronts is the workgroup's");
+    // what all threads of a row agree on and is hardly ever true, as a branch of the wavefront where it has one row only: what is live on the way
+    // not taken needs no registers then
+    static __device__ __forceinline__ bool agreed(bool b) { return __builtin_expect(TPR >= 64 ? __builtin_amdgcn_readfirstlane(b) : b, 0); }
     // one(a, b) of a value and the largest of the bits over the threads of a row, every one of them getting both.  AGAIN: a call for the same
     // rows was before it.
     template <bool AGAIN, class One> static __device__ __forceinline__ void reduce(float& value, uint32_t& top, One&& one) {
@@ -52,7 +55,10 @@ template <int TPR, int BLOCK> struct Group {
             __syncthreads();
             value = s[0]; top = t[0];
 #pragma unroll
-            for (int w = 1; w < WAVES; ++w) { value = one(value, s[w]); top = max(top, t[w]); }
+            for (int w = 1; w < WAVES; ++w) {
+                value = one(value, s[w]); top = max(top, t[w]);
+                if (w % 8 == 7) __builtin_amdgcn_sched_barrier(0);      // (sixteen wavefronts' at once would be 32 registers)
+            }
         }
     }
     // The largest of the bits alone; and whether a wavefront of the row (for short rows: the row) had a thread whose `wide` is more than eight
@@ -80,6 +86,7 @@ template <int TPR, int BLOCK> struct Group {
 // tie is rounded as it stands, by one multiply-add.  Next to ties (half of the largest is one: 63.5) 64 bits decide: there the quotient is
 // within 2^-45, a quotient of two 24-bit numbers that is no tie is 2^-32 from one at least, and adding and taking away 1.5 2^12 leaves it at a
 // multiple of 2^-40, ties as they are.  Tiny rows, whose inv may not be finite, go the same way.
+__device__ __forceinline__ int32_t nearest(float v, double up) { return (int32_t)__builtin_rint(__builtin_fma((double)v, up, 6144.0) - 6144.0); }
 __device__ __forceinline__ void store_q(int8_t* p, const v8f& v, const Quant& q, int n) {
     uint32_t w[8];
     float far = 0.0f;
@@ -88,13 +95,10 @@ __device__ __forceinline__ void store_q(int8_t* p, const v8f& v, const Quant& q,
         w[e] = round_bits(v[e], q.inv);
         far = __builtin_fmaxf(far, __builtin_fabsf(__builtin_fmaf(v[e], q.inv, kRound - __uint_as_float(w[e]))));
     }
-    if (far >= 0.5f - 0x1p-16f || q.top < 0x1p-100f) {
+    if (__builtin_expect(far >= 0.5f - 0x1p-16f || q.top < 0x1p-100f, 0)) {
         const double up = q.top > 0.0f ? 127.0 / (double)q.top : 0.0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const double d = __builtin_fma((double)v[e], up, 6144.0) - 6144.0;
-            w[e] = q.top > 0.0f ? (uint32_t)(int32_t)__builtin_rint(d) : 0u;
-        }
+        for (int e = 0; e < 8; ++e) w[e] = q.top > 0.0f ? (uint32_t)nearest(v[e], up) : 0u;
     }
     typedef uint32_t v2u __attribute__((ext_vector_type(2), aligned(1)));
     const v2u out = {pack4(w[0], w[1], w[2], w[3]), pack4(w[4], w[5], w[6], w[7])};
@@ -118,6 +122,51 @@ struct NormParams {
     const void* x; const void* r; const float* gamma; void* sum; void* y; float* scale;
     int64_t ldx, ldr, ld_sum, ldy, rows; int C; float eps;
 };
+
+// A row whose sum of squares, or whose largest |h gamma|, is beyond the range of 32 bits or below the normal numbers, while its n need not be: the
+// sum again of h 2^-64, if it is infinite, and products of h factor, which is at most sqrt(C), with gamma.  All threads of the row come here, with the
+// same sum, and read it anew, element by element, each its own ones: hardly a row is like this, and the kernel needs no register for it.
+template <class T, int TPR, int BLOCK, bool I8>
+__device__ __forceinline__ void far_row(const NormParams& P, int64_t row, bool real, float sum) {
+    using G = Group<TPR, BLOCK>;
+    const int t = threadIdx.x % TPR, C = P.C;
+    const T* const x = static_cast<const T*>(P.x) + row * P.ldx;
+    const T* const r = static_cast<const T*>(P.r) + row * P.ldr;
+    auto input = [&](int c) __attribute__((always_inline)) { return P.r ? (float)x[c] + (float)r[c] : (float)x[c]; };
+    auto gamma = [&](int c) __attribute__((always_inline)) { return P.gamma ? P.gamma[c] : 1.0f; };
+    auto add = [](float a, float b) __attribute__((always_inline)) { return a + b; };
+    uint32_t top = 0;
+    float factor = 1.0f / __builtin_sqrtf(sum / (float)C + P.eps);
+    if (G::agreed(sum == __builtin_inff())) {
+        sum = 0.0f;
+#pragma unroll 1
+        for (int c = t; c < C; c += TPR) {
+            const float h = input(c) * 0x1p-64f;
+            sum = __builtin_fmaf(h, h, sum);
+        }
+        G::template reduce<true>(sum, top, add);
+        const float mean = sum / (float)C + P.eps * 0x1p-64f * 0x1p-64f;
+        factor = mean < 1.0f ? 0x1p-64f / __builtin_sqrtf(mean) : 0.0f;        // (a mean square beyond the range counts as infinite)
+    }
+    Quant q = {};
+    if (I8) {
+        top = 0;
+#pragma unroll 1
+        for (int c = t; c < C; c += TPR) top = max(top, __float_as_uint(input(c) * factor * gamma(c)) & 0x7fffffffu);
+        G::template reduce<true>(sum, top, add);
+        q = quant_of(top, 1.0f);
+        if (real && t == 0) P.scale[row] = q.scale;
+    }
+    if (!real) return;
+    const double up = q.top > 0.0f ? 127.0 / (double)q.top : 0.0;
+#pragma unroll 1
+    for (int c = t; c < C; c += TPR) {
+        const float h = input(c), n = h * factor * gamma(c);
+        if (P.sum) static_cast<T*>(P.sum)[row * P.ld_sum + c] = (T)h;
+        if (I8) static_cast<int8_t*>(P.y)[row * P.ldy + c] = q.top > 0.0f ? (int8_t)nearest(n, up) : (int8_t)0;
+        else static_cast<T*>(P.y)[row * P.ldy + c] = (T)n;
+    }
+}
 
 // SHORT: fewer than eight elements a row (TPR = 8, NV = 1): the first thread takes them one by one
 template <class T, int NV, int TPR, int BLOCK, bool I8, bool SHORT>
@@ -163,6 +212,9 @@ __global__ __launch_bounds__(BLOCK) void rmsnorm_kernel(NormParams P) {
         }
     }
     G::template reduce<false>(sum, top, [](float a, float b) __attribute__((always_inline)) { return a + b; });
+    // (rows of zeros go on, and with them rows whose squares and products with gamma are all 0 in 32 bits)
+    if (G::agreed(sum == __builtin_inff() || (I8 && top - kNormal >= kInf - kNormal && (top | __float_as_uint(sum)))))
+        return far_row<T, TPR, BLOCK, I8>(P, row, mine < P.rows, sum);
     const float factor = 1.0f / __builtin_sqrtf(sum / (float)C + P.eps);
     const Quant q = quant_of(top, factor);
     if (mine >= P.rows) return;
@@ -175,12 +227,11 @@ __global__ __launch_bounds__(BLOCK) void rmsnorm_kernel(NormParams P) {
             T* s = static_cast<T*>(P.sum) + row * P.ld_sum + p[v].at;
             if (SHORT) store_some(s, h[v], n); else store8(s, h[v]);
         }
-        h[v] *= g[v];
         if (I8) {
-            store_q(static_cast<int8_t*>(P.y) + row * P.ldy + p[v].at, h[v], q, n);
-        } else {
+            store_q(static_cast<int8_t*>(P.y) + row * P.ldy + p[v].at, h[v] * g[v], q, n);
+        } else {                                              // (h factor is at most sqrt(C), a product of h and gamma may be beyond the range)
             T* y = static_cast<T*>(P.y) + row * P.ldy + p[v].at;
-            if (SHORT) store_some(y, h[v] * factor, n); else store8(y, h[v] * factor);
+            if (SHORT) store_some(y, h[v] * factor * g[v], n); else store8(y, h[v] * factor * g[v]);
         }
     }
 }
@@ -264,10 +315,10 @@ __global__ __launch_bounds__(BLOCK) void gated_kernel(GateParams P) {
             for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(h[v][e]) & 0x7fffffffu);
     };
     with_activation(P.act, [&](auto act) __attribute__((always_inline)) { form(act, std::false_type()); });
-    if (G::largest(top, wide)) {
+    if (G::agreed(G::largest(top, wide))) {
         auto more = [](float a, float b) __attribute__((always_inline)) { return __builtin_fmaxf(a, b); };
         G::template reduce<false>(wide, top, more);
-        if (8.0f * __uint_as_float(top) < wide) {
+        if (G::agreed(8.0f * __uint_as_float(top) < wide)) {
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
                 a[v] = SHORT ? __builtin_convertvector(load_some(x, C), Raw) : *reinterpret_cast<const Mem*>(x + p[v].at);

@@ -180,6 +180,65 @@ def norm_of(ivit, x, gamma, eps, i8):
     return y, s
 
 
+def check_normed(y, s, x, gamma, eps, what):
+    """Against 64 bits: half of the error of a sum of squares in chains of 32 and a tree of 10, the root, the quotient, two products; the rounding of the result."""
+    import torch
+    h = x.double()
+    n = h / ((h * h).mean(1, keepdim=True) + eps).sqrt()
+    n = n if gamma is None else n * gamma.double()
+    rel = ((32 + 10 + 3) / 2 + 8) * U
+    if s is None:
+        half = torch.finfo(y.dtype).eps / 2
+        assert bool(((y.double() - n).abs() <= (rel + half + rel * half) * n.abs() + 2.0 ** -133).all()), what
+        return
+    top = n.abs().amax(1)
+    assert bool(((s.double() - top / 127).abs() <= (rel + 2 * U) * top / 127 + 2.0 ** -149).all()), what + ": scale"
+    assert bool(((y.double() * (top / 127)[:, None] - n).abs() <= (top / 127)[:, None] * (0.5 + 127 * 8 * U)).all()), what + ": rows"
+
+
+@pytest.mark.parametrize("C", WIDTHS)
+def test_sums_of_squares_beyond_the_range_of_32_bits(ivit, C):
+    """Rows whose mean square is in the range and whose sum of squares is not, beside ordinary ones; and a mean square beyond it."""
+    import torch
+    for t in ("f32", "bf16"):
+        z = torch.randn((9, C), generator=gen(C), device="cuda").clamp(-8, 8)
+        z[:, 0] = 1.0
+        z *= torch.tensor([1.0, 1e17, 4e17, 1e18, 1.0, 3e18, 8e18, 1e-3, 4e37], device="cuda")[:, None]
+        x, gamma = z.to(dtype(t)), 1.0 + 0.1 * torch.randn(C, generator=gen(C + 1), device="cuda")
+        for g in (None, gamma):
+            for i8 in (True, False):
+                y, s = norm_of(ivit, x, g, 1e-6, i8)
+                check_normed(y[:8], s[:8] if i8 else None, x[:8], g, 1e-6, "%s %s" % (t, i8))
+                assert not bool(y[8].any()) and (not i8 or float(s[8]) == 0.0)      # (counts as infinite)
+
+
+def test_eps_counts_beside_large_sums(ivit):
+    import torch
+    x = torch.full((3, 4096), 4e17, device="cuda")
+    for eps in (1e35, 3e38):
+        for i8 in (True, False):
+            y, s = norm_of(ivit, x, None, eps, i8)
+            eps32 = float(torch.tensor(eps, dtype=torch.float32))
+            check_normed(y, s, x, None, eps32, "eps %g" % eps)
+
+
+@pytest.mark.parametrize("C", WIDTHS)
+def test_products_with_gamma_beyond_the_range_of_32_bits(ivit, C):
+    """h gamma beyond the range, or below the normal numbers, where n = h / rms gamma is not; rows of ordinary size with the same gamma."""
+    import torch
+    z = torch.randn((8, C), generator=gen(C), device="cuda").clamp(-6, 6)
+    z[:, C // 2] = 2.0
+    base = 1.0 + 0.1 * torch.randn(C, generator=gen(C + 1), device="cuda")
+    for by, rows in ((1e30, [1.0, 1e12, 1e18, 1e-15, 0.0, 1e9, 3e18, 1.0]), (1e-30, [1.0, 1e-12, 1e-15, 1e10, 0.0, 3e-14, 1e-8, 1.0])):
+        x = z * torch.tensor(rows, device="cuda")[:, None]
+        gamma, eps = base * by, 1e-37
+        for i8 in (True, False):
+            y, s = norm_of(ivit, x, gamma, eps, i8)
+            fine = [0, 1, 2, 3, 5, 6, 7]
+            check_normed(y[fine], s[fine] if i8 else None, x[fine], gamma, eps, "gamma %g" % by)
+            assert not bool(y[4].any()) and (not i8 or float(s[4]) == 0.0)
+
+
 @pytest.mark.parametrize("C", [5, 64, 1000, 2049, 6000, 32768])
 def test_results_beyond_the_range_of_32_bits(ivit, C):
     """The row's largest n beyond the range: NaN as its scale and zeros, and infinite where the result is of the stream's type."""
@@ -190,7 +249,7 @@ def test_results_beyond_the_range_of_32_bits(ivit, C):
     x[3] = 0.0
     gamma = torch.full((C,), 3e38, device="cuda")
     gamma[0], x[:, 0] = 1.0, torch.tensor([1.0, 1e-30, 0.0, 0.0], device="cuda")
-    for scale in (1.0,):
+    for scale in (1.0, 1e15):
         y, s = norm_of(ivit, x * scale, gamma, 1e-12, True)
         assert bool(torch.isnan(s[2])) and not bool(y[2].any()) and float(s[3]) == 0.0 and not bool(y[3].any())
         assert bool(torch.isfinite(s[:2]).all())
