@@ -455,8 +455,10 @@ int ivit_rmsnorm_quant(void* stream, const void* x, int64_t ldx, const void* res
  *   y[m][n] = act(x_scale[m] * w_scale[n] * sum_k x[m][k] w[n][k] + bias[n]) + residual[m][n]
  * x int8 [M, K] (ldx elements between rows, a multiple of 16, at most 2^22), w int8 [N, K] dense; the full range of int8,
  * -128 included.  x_scale float32 [M], or one value for all rows if one_scale != 0; w_scale float32 [N]; bias float32 [N]
- * or NULL.  y [M, N] of y_type; residual [M, N] of y_type or NULL.  y_type == IVIT_I8: y = clamp8(round(act(..) / y_step)),
- * without a residual (y_step is ignored otherwise; a NaN gives 0).  residual may be y itself (same pointer and leading
+ * or NULL.  y [M, N] of y_type; residual [M, N] of y_type or NULL.  y_type == IVIT_I8: y = clamp8(round(act(..) * f)), f = 1 / y_step,
+ * without a residual (y_step is ignored otherwise; a NaN gives 0): f and the product are rounded to 32 bits, so that act(..) / y_step within
+ * 2^-17 of a tie goes by them, and a tie is exact where y_step is a power of two.  act's argument is formed as
+ * (sum * w_scale[n]) * x_scale[m] + bias[n], the last two operations rounded once.  residual may be y itself (same pointer and leading
  * dimension); no other overlap.
  * Requirements: 0 <= M < 2^31, 1 <= N <= 2^24, 16 <= K <= 65536, K % 16 == 0; x and w 16-byte aligned; y_step a normal number whose
  * reciprocal is one too.

@@ -83,3 +83,22 @@ def test_every_value_of_many_is_the_nearest(ivit, t):
         gamma = 1.0 + 0.1 * torch.randn(C, generator=g, device="cuda")
         ivit.ivit_rmsnorm_quant(x, gamma, y, sy, 1e-6, residual=x, sum_out=h)
         assert torch.equal(y, levels((x.float() + x.float()) * gamma))      # (x + x is exact; the product is rounded to 32 bits once)
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 253, 16), (20, 253, 64), (40, 253, 512), (300, 253, 256), (3000, 506, 96)])
+def test_int8_at_a_fixed_step(ivit, M, N, K):
+    """Values exactly between two steps, by the bias alone: as the header has it, round(v * (1 / step)) in 32 bits; even at a power of two."""
+    import numpy as np
+    import torch
+    k = torch.arange(-126, 127, device="cuda").repeat(N // 253).float()
+    for step in (1.0, 0.25, 2.0 ** -7, 0.75, 7.0, 0.21875, 0.40625, 100.0):
+        bias = (k + 0.5) * step
+        assert torch.equal(bias.double(), (k.double() + 0.5) * step)
+        y = torch.full((M, N), 99, dtype=torch.int8, device="cuda")
+        ivit.ivit_linear_scaled(torch.zeros((M, K), dtype=torch.int8, device="cuda"), torch.ones(M, device="cuda"), torch.ones((N, K), dtype=torch.int8, device="cuda"),
+                                torch.ones(N, device="cuda"), y, bias=bias, y_step=step)
+        f = np.float32(1) / np.float32(step)
+        want = torch.from_numpy(np.clip(np.rint(bias.cpu().numpy() * f), -127, 127).astype(np.int8)).cuda()
+        assert bool((y == want).all()), step
+        if step in (1.0, 0.25, 2.0 ** -7):
+            assert torch.equal(want, torch.round(k + 0.5).to(torch.int8))
