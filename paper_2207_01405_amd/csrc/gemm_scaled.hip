@@ -15,6 +15,7 @@
 #include "linear_rows.hpp"
 #include "regst_common.hpp"
 #include "scaled_common.hpp"
+#include "scaled_form.hpp"
 
 namespace ivit {
 namespace {
@@ -525,35 +526,6 @@ template <int TYPE, int MT, int NT, int GM, int GN, int S> hipError_t launch_til
     return hipGetLastError();
 }
 
-// Which tile.  us measured on 256 CUs, bf16 results, inputs in turn.
-enum Form { ROWS, T64, T128X64, T128X8, T256X128, T256, T128 };
-Form form_of(const ScaledArgs& a) {
-    const int64_t cus = num_cus();
-    auto tiles = [&](int64_t m, int64_t n) { return ((a.M + m - 1) / m) * ((a.N + n - 1) / n); };
-    auto rounds = [&](int64_t m, int64_t n, int64_t per_cu) { return (tiles(m, n) + per_cu * cus - 1) / (per_cu * cus); };
-    // Few rows: the kernel whose wavefronts split K, while two of its 32 x 32 tiles a CU take the shape (that kernel's and 64 x 64:
-    // 64 x 4096 x 4096 6.6 and 11.1, 128 x 4096 x 4096 8.7 and 11.2, 394 x 384 x 384 3.0 and 3.4, 788 x 384 x 1536 5.2 and 5.1; three a CU:
-    // 64 x 11008 x 4096 14.4 and 12.1, 394 x 1536 x 384 4.7 and 3.6), and for up to 32 rows always (16 x 32000 x 4096 28.0 and 33.7).
-    if (a.M <= 32 || rounds(32, 32, 2) <= 1) return ROWS;
-    // Rows of 768 bytes and more: the smallest tile that gives every CU at most one workgroup (64 x 64, 128 x 64, 128 x 128, 256 x 128,
-    // 256 x 256: 1024 x 1024 x 1024 4.6, 5.4, 6.8; 512 x 4096 x 4096 16.1, 14.8, 18.4; 1024 x 4096 x 4096 34, 26, 21.8, 25.7; 512 x 11008 x
-    // 4096 44, 37, 36, 27.7, 41; 1024 x 11008 x 4096 -, -, 56, 54, 46.7).  Shorter rows gain nothing by it (1576 x 1536 x 384 6.1, 9.1, 7.2).
-    if (a.K >= 768) {
-        if (tiles(64, 64) <= cus) return T64;
-        if (tiles(128, 64) <= cus) return T128X64;
-        if (tiles(128, 128) <= cus) return T128X8;
-        if (tiles(256, 128) <= cus) return T256X128;
-        // A round of 256 x 256 (one a CU) against one of 128 x 128 (two a CU, half the work): 62 and 36 at K = 4096; 8192 x 8192 x 4096
-        // 248 and 290, 4096 x 16384 x 4096 247 and 301; with 1024 bytes of K the gain is gone (50432 x 768 x 768 54.4 and 54.6).
-        if (rounds(256, 256, 1) * 10 <= rounds(128, 128, 2) * 6) return T256;
-        return T128;
-    }
-    // up to three 64 x 64 tiles a CU, and where 128 channels would be half padding: 64 x 64 (1576 x 1536 x 384 6.1 and 8.2 with 128 x 128, 3152 x
-    // 1536 x 384, 4.7 tiles a CU, 8.1 and 7.9; 300000 x 64 x 64 16.1 and 22.5)
-    if (rounds(64, 64, 3) <= 1 || a.N <= 64) return T64;
-    return T128;
-}
-
 template <int TYPE> hipError_t launch_type(hipStream_t s, const ScaledArgs& a, Form form) {
     switch (form) {
         case T64: return launch_tile<TYPE, 1, 1, 2, 2, 3>(s, a);
@@ -569,7 +541,7 @@ template <int TYPE> hipError_t launch_type(hipStream_t s, const ScaledArgs& a, F
 
 hipError_t launch_linear_scaled(hipStream_t s, const ScaledArgs& a) {
     if (a.M == 0) return hipSuccess;
-    const Form form = form_of(a);
+    const Form form = form_of(a.M, a.N, a.K, num_cus());
     const int64_t e = element_bytes(a.y_type);
     auto ops = [&](int64_t M) { return 2 * M * a.N * a.K; };
     auto bytes = [&](int64_t M) { return M * a.K + (int64_t)a.N * a.K + M * a.N * e * (a.residual ? 2 : 1); };
