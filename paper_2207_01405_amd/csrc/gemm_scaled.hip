@@ -232,7 +232,7 @@ __global__ __launch_bounds__((64 * GM * GN), 2) void gemm_scaled_kernel(GsParams
     // all loads but those of the `left` stages requested last have arrived, and LDS reads returned, for everybody
     auto arrive_but = [&](int left) __attribute__((always_inline)) {
         if (left <= 0) arrive<0>();
-        else if (S <= 3 || left == 1) arrive<DP>();
+        else if (left == 1) arrive<DP>();
         else arrive<2 * DP>();
     };
     // The epilogue turns results over in LDS (see there), SLOTS times 32 tokens at once.
