@@ -337,10 +337,12 @@ __global__ __launch_bounds__(BLOCK) void gated_kernel(GateParams P) {
 }
 
 // f(NV, TPR, BLOCK, SHORT) for rows of C elements.  Many rows: as few threads a row as hold it in up to three pieces each, so that hardly
-// a thread is idle, and a workgroup for every wavefront (bf16 norms with a residual, us, with ordinary stores: 25216 x 384 13.6, with four wavefronts a
-// workgroup 15.2; 25216 x 768 28.3, with 256 threads a row 49.9; 20000 x 1536, activation alone, 30.9 and 36.9); from 1537 to 2048 elements 256 threads
-// have one piece each (10000 x 2048 29.9, with 64 threads 32.0; 5003 x 2049 10.9 with 128 threads, 11.5 with 256).  Few rows, where a launch
-// is a chain of latencies: 256 threads from 513 elements on (197 x 1536, activation alone, 2.9 and 3.6).
+// a thread is idle, and a workgroup for every wavefront (bf16 norms with a residual, us: 25216 x 384 15.7, with four wavefronts a
+// workgroup 16.5; 25216 x 768 29.3, with 256 threads a row 51.0; 20000 x 1536, activation alone, 24.0 and 34.1); from 1537 to 2048 elements 256 threads
+// have one piece each (10000 x 2048 30.6, with 128 threads of two 33.3); up to three pieces of 128 threads then, against two of 256:
+// activation alone 10000 x 2304 21.7 and 26.9, x 3000 23.5 and 29.2, gated 22.3 and 26.0, 26.9 and 27.3, norms 36.4 and 35.8, 44.9 and 43.7,
+// without a residual, to float16, 5003 x 2049 10.8 and 11.4, 10000 x 3000 26.1 and 26.3.  Few rows, where a launch is a chain of
+// latencies: 256 threads from 513 elements on (197 x 1536, activation alone, 3.2 and 3.5; 300 x 2304 3.9, with 128 threads of three pieces 4.4, norms 4.2 and 4.6).
 template <class F> hipError_t with_group(int64_t rows, int C, F&& f) {
     const int pieces = (C + 7) / 8;
 #define IVIT_GROUP(nv, tpr, block, s) f(std::integral_constant<int, nv>(), std::integral_constant<int, tpr>(), std::integral_constant<int, block>(), std::integral_constant<bool, s>())
@@ -349,12 +351,13 @@ template <class F> hipError_t with_group(int64_t rows, int C, F&& f) {
     if (pieces <= 16) return IVIT_GROUP(1, 16, 64, false);
     if (pieces <= 32) return IVIT_GROUP(1, 32, 64, false);
     if (pieces <= 64) return IVIT_GROUP(1, 64, 64, false);
-    if (pieces <= 192 && rows > 2 * num_cus()) {
+    const bool many = rows > 2 * num_cus();
+    if (pieces <= 192 && many) {
         if (pieces <= 128) return IVIT_GROUP(2, 64, 64, false);
         return IVIT_GROUP(3, 64, 64, false);
     }
     if (pieces <= 256) return IVIT_GROUP(1, 256, 256, false);
-    if (pieces <= 320) return IVIT_GROUP(3, 128, 128, false);
+    if (pieces <= 384 && many) return IVIT_GROUP(3, 128, 128, false);
     if (pieces <= 512) return IVIT_GROUP(2, 256, 256, false);
     if (pieces <= 1024) return IVIT_GROUP(4, 256, 256, false);
     if (pieces <= 2048) return IVIT_GROUP(2, 1024, 1024, false);
