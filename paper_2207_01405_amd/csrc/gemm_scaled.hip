@@ -8,8 +8,8 @@
 //
 // What bounds the tiles is LDS, 128 bytes a cycle and CU for fragment reads and arriving loads alike: a stage of two 128 x 128 tiles a CU is
 // 1536 cycles of it for 1024 of products and takes 0.99 us, one of 256 x 256 (eight wavefronts of 128 x 64) 2048 for 2048 and 1.57 us at the
-// 1.7 GHz that this card keeps up then.  8192 x 8192 x 4096 with bf16 results 224 us, 2.45 POP/s (a product alone from registers runs at 3.2
-// to 3.3 on random data), 8192 x 8192 x 8192 2.47; with the residual 250 us.  Tried for 256 x 256 and taken back: four wavefronts of 128 x 128,
+// 1.7 GHz that this card keeps up then.  8192 x 8192 x 4096 with bf16 results 224 to 229 us, 2.4 POP/s (a product alone from registers runs at 3.2
+// to 3.3 on random data); with the residual 249 to 252.  Tried for 256 x 256 and taken back: four wavefronts of 128 x 128,
 // a quarter less LDS (497 against 465 us at K = 8192, then 461 against 451); stages of 64 bytes, four of them (473 against 451: half lines);
 // the residual's lines requested into L2 during the last stages (286 against 281) or a pass ahead (290 against 286); wave priorities (no change).
 #include "linear_rows.hpp"
@@ -514,9 +514,9 @@ template <int TYPE, int MT, int NT, int GM, int GN, int S> hipError_t launch_til
     P.ldx = a.ldx; P.ld_res = a.ld_res; P.ldy = a.ldy; P.M = a.M; P.N = a.N; P.K = a.K; P.act = a.act; P.one_scale = a.one_scale;
     P.inv_step = a.inv_step;
     // From 64 MB on, results are stored past the L2, which has the operands to keep and would write them back at the launch's end
-    // (8192 x 8192 x 4096 246 -> 224 us, 50432 x 768 x 768 54 -> 46), and a residual is loaded past it (8192 x 8192 x 4096, 284 and 258 us;
-    // 50432 x 768 x 768 67 and 64.6).  Smaller ones stay in the caches for whoever reads them next (25216 x 1152 x 384 with int8
-    // results and a pass over them 70 us for 81; residuals: 4096 x 4096 x 4096, 34 MB, 67 and 70; 25216 x 384 x 1536 28.0 and 30.0).
+    // (8192 x 8192 x 4096 239 and 229 us, 50432 x 768 x 768 53 and 44.5), and a residual is loaded past it (both: 8192 x 8192 x 4096 278 and 252,
+    // 50432 x 768 x 768 64 and 57.5).  Smaller ones stay in the caches for whoever reads them next (25216 x 1152 x 384 with int8 results and a
+    // pass over them 67 us for 76; residuals: 25216 x 384 x 1536 28.2 and 29.4, 4096 x 4096 x 4096, 34 MB, 67.4 and 66.6).
     P.once = a.M * a.N * (int64_t)sizeof(Stored<TYPE>) >= (int64_t)1 << 26;
     const int64_t tm = (a.M + TL::TM - 1) / TL::TM, tn = (a.N + TL::TN - 1) / TL::TN;
     int64_t grid = (tm * tn + NXCD - 1) / NXCD * NXCD;

@@ -4,13 +4,15 @@
 //   norm:  h = x + r,  n = h / sqrt(mean(h^2) + eps) gamma        gate:  v = act(g) u  or  act(g)
 //   s = max |v| / 127,  q = round(v / s)
 //
-// Both are bound by memory: an element is 10 to 20 operations for 3 to 7 bytes.  A group of TPR threads holds a row in
-// registers, NV pieces of eight elements a thread, so that x is read once; one reduction over the group gives the norm its sum of
-// squares and its largest |h gamma| together: the factor 1 / sqrt(..) is the same for a row's elements, so q needs h gamma only
-// and s takes the factor once.  Norms of 16384 x 4096 bf16 with a residual take 85 us (5.5 TB/s), 25216 x 384 14.4 (4.7), the gated
-// activation of 8192 x 14336 bf16 101 (5.8).  Results go through the caches, since the product after them reads them: stored past
-// the L2 the norm gets faster (16384 x 4096 82 us, 25216 x 768 23.5 for 28.6) and what follows slower by more (norm, Dense 768 -> 2048,
-// activation and Dense 2048 -> 768 of 50432 rows 355 for 338).
+// A group of TPR threads holds a row in registers, NV pieces of eight elements a thread, so that x is read once; one reduction over the group
+// gives the norm its sum of squares and its largest |h gamma| together: the factor 1 / sqrt(..) is the same for a row's elements, so q
+// needs h gamma only and s takes the factor once.
+//
+// Norms are bound by memory, 5 to 7 bytes an element for some 14 instruction slots: 16384 x 4096 bf16 with a residual 85 us (5.5 TB/s), 25216 x 384
+// 15.5 (4.4).  Gated by SiLU 8192 x 14336 take 100 (5.9), memory too; GELU alone is bound by vector instructions as well, about 24 slots an element
+// for 3 bytes: 20000 x 1536 bf16 23 us, of which 21 are issue and 18 the bytes; 8192 x 14336 gated by it 117.  Results go through the caches, since
+// the product after them reads them: stored past the L2 the norm gets faster (when chosen: 16384 x 4096 82 us, 25216 x 768 23.5 for 28.6)
+// and what follows slower by more (norm, Dense 768 -> 2048, activation and Dense 2048 -> 768 of 50432 rows 355 for 338).
 #include "scaled_common.hpp"
 
 namespace ivit {
@@ -395,8 +397,8 @@ template <class T> hipError_t norm_of(hipStream_t s, const RmsNormArgs& a) {
 }
 
 template <class T> hipError_t gate_of(hipStream_t s, const GatedArgs& a) {
-    // x past the caches from 32 MB on (8192 x 14336 gated 100 and 96 us, 20000 x 1536, 61 MB, 29.4 and 27.5; 1000 x 4096 gated, 16 MB, 6.1 and 6.1; 197 x 1536 2.95
-    // and 3.3).  The norm's inputs, residual and all, are better left alone (25216 x 384 13.7 and 16.6, 16384 x 4096 82 and 79.5).
+    // x past the caches from 32 MB on (8192 x 14336 gated, 470 MB, 103.6 and 99.7 us, 20000 x 1536, 61 MB, 22.7 and 23.2; 1000 x 4096 gated, 16 MB,
+    // 6.4 and 6.0).  The norm's inputs, residual and all, are better left alone (when chosen: 25216 x 384 13.7 and 16.6, 16384 x 4096 82 and 79.5).
     const int once = a.rows * a.C * (int64_t)sizeof(T) * (a.gated ? 2 : 1) >= (int64_t)1 << 25;
     return with_group(a.rows, a.C, [&](auto nv, auto tpr, auto block, auto few) {
         constexpr int NV = nv, TPR = tpr, BLOCK = block, ROWS = BLOCK / TPR;
