@@ -255,3 +255,84 @@ def test_results_beyond_the_range_of_32_bits(ivit, C):
         assert bool(torch.isfinite(s[:2]).all())
         y, _ = norm_of(ivit, x * scale, gamma, 1e-12, False)
         assert float(y[2, C // 2]) == math.inf and not bool(y[3].any())
+
+
+# ------------------------------------------------------------------- such rows in place, with strides, and replayed from a graph
+def odd_rows(rows, C, t, seed):
+    """Ordinary rows, zeros, rows whose squares and products leave the range, tails, NaN and infinities, by turns."""
+    import torch
+    z = torch.randn((rows, C), generator=gen(seed), device="cuda")
+    by = torch.tensor([1.0, 0.0, 1e18, 1.0, 2e-15, 1e17, 1.0, 30.0], device="cuda").repeat(rows // 8 + 1)[:rows]
+    if t == "f16":
+        by = by.clamp(0.0, 1e3)
+    x = z * by[:, None]
+    x[3::8] = -4.0 - 5.0 * torch.rand((len(range(3, rows, 8)), C), generator=gen(seed + 1), device="cuda")
+    x[6::16, C // 3] = math.nan
+    x[14::16, C // 2] = math.inf
+    return x.to(dtype(t))
+
+
+def same(a, b):
+    import torch
+    return torch.equal(a.nan_to_num(nan=7.0, posinf=8.0, neginf=9.0), b.nan_to_num(nan=7.0, posinf=8.0, neginf=9.0)) if a.is_floating_point() else torch.equal(a, b)
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("C", [5, 60, 130, 500, 1000, 2300, 4099, 9000])
+def test_odd_rows_written_over_their_inputs(ivit, t, C):
+    import torch
+    rows = 67
+    x, r = odd_rows(rows, C, t, C), (0.5 * odd_rows(rows, C, t, C + 9))
+    r[::8] = 0.0
+    for by in (1.0, 1e25, 1e-25):
+        gamma = by * (1.0 + 0.1 * torch.randn(C, generator=gen(C + 3), device="cuda"))
+        q, s, total, n = torch.empty((rows, C), dtype=torch.int8, device="cuda"), torch.empty(rows, device="cuda"), torch.empty_like(x), torch.empty_like(x)
+        ivit.ivit_rmsnorm_quant(x, gamma, q, s, 1e-37, residual=r, sum_out=total)
+        ivit.ivit_rmsnorm_quant(x, gamma, n, None, 1e-37, residual=r)
+        for swap in (False, True):
+            a, b = x.clone(), r.clone()
+            q2, s2 = torch.full_like(q, 99), torch.empty_like(s)
+            ivit.ivit_rmsnorm_quant(a, gamma, q2, s2, 1e-37, residual=b, sum_out=b if swap else a)
+            assert same(b if swap else a, total) and same(q2, q) and same(s2, s)
+            a, b = x.clone(), r.clone()
+            ivit.ivit_rmsnorm_quant(a, gamma, b if swap else a, None, 1e-37, residual=b, sum_out=a if swap else b)
+            assert same(b if swap else a, n) and same(a if swap else b, total)
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("C", [5, 60, 500, 2300, 9000])
+def test_odd_rows_with_strides_and_from_a_graph(ivit, t, C):
+    import torch
+    rows, ld = 67, C + 3
+    x = torch.zeros(1 + rows * 2 * ld, dtype=dtype(t), device="cuda")
+    xn, xg = x[1:1 + rows * 2 * ld].view(rows, 2 * ld)[:, :C], x[1:1 + rows * 2 * ld].view(rows, 2 * ld)[:, :2 * C]
+    xg.copy_(odd_rows(rows, 2 * C, t, C))
+    gamma = 1e25 * (1.0 + 0.1 * torch.randn(C, generator=gen(C + 3), device="cuda"))
+    bufs = [torch.full((rows, ld), 77, dtype=torch.int8, device="cuda") for _ in range(3)]
+    s = [torch.empty(rows, device="cuda") for _ in range(3)]
+
+    def run(y, a, b):
+        ivit.ivit_rmsnorm_quant(a, gamma, y[0][:, :C], s[0], 1e-37)
+        ivit.ivit_gated_quant(b, y[1][:, :C], s[1], act="gelu")
+        ivit.ivit_gated_quant(a, y[2][:, :C], s[2], act="gelu", gated=False)
+
+    run([torch.empty_like(v) for v in bufs], xn.contiguous(), xg.contiguous())
+    torch.cuda.synchronize()
+    want_s = [v.clone() for v in s]
+    dense = [torch.full_like(v, 77) for v in bufs]
+    run(dense, xn.contiguous(), xg.contiguous())
+    run(bufs, xn, xg)
+    assert all(torch.equal(a, b) for a, b in zip(bufs, dense)) and all(same(a, b) for a, b in zip(s, want_s))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run(bufs, xn, xg)
+    for k in range(3):
+        xg.copy_(odd_rows(rows, 2 * C, t, C + 100 + k))
+        run(dense, xn, xg)
+        torch.cuda.synchronize()
+        want_s = [v.clone() for v in s]
+        for v in bufs + s:
+            v.fill_(77)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(bufs, dense)) and all(same(a, b) for a, b in zip(s, want_s))
