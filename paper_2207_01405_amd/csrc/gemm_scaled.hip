@@ -376,7 +376,7 @@ __global__ __launch_bounds__((64 * GM * GN), 2) void gemm_scaled_kernel(GsParams
         // instruction would touch 64 lines and fill none.  So a wavefront turns its results over in LDS that it has for itself
         // (REGION bytes), SLOTS times 32 tokens at once, and lines leave whole; a residual comes in the same way.  Chunk c of a row
         // stands at c ^ swz(row), which spreads rows over the banks.
-        auto swz = [](int r) __attribute__((always_inline)) { return CH >= 8 ? r & (CH - 1) : (r / (8 / CH)) & (CH - 1); };
+        auto swz = [](int r) __attribute__((always_inline)) { return (CH >= 8 ? r : r / (CH < 8 ? 8 / CH : 1)) & (CH - 1); };
         __syncthreads();                                      // (nobody reads operands any more)
         const bool more_tiles = PERSIST && tile + slots < end;
         Place next = at;
