@@ -7,7 +7,8 @@
  * Dense / MatMul with dyadic requantisation (Sec. 3.2), Shiftmax (Sec. 3.3,
  * Algorithm 1), ShiftGELU (Sec. 3.4, Algorithm 2) and I-LayerNorm (Sec. 3.5).
  * Beside it stand three layers with real scales and a floating-point residual
- * stream (last section but one), for models quantised per token at run time.
+ * stream (last section but two), for models quantised per token at run time, and attention
+ * over their rows with a paged cache (last section but one).
  *
  * General rules
  *  - Every tensor pointer is a DEVICE pointer owned by the caller; the library
@@ -293,7 +294,8 @@ int ivit_window_attention_ex(void* stream, const int8_t* qkv, const int8_t* rel_
  * `capacity` entries) with, per launch in launch order: elapsed milliseconds, kind (1 I-LayerNorm, 2 Dense,
  * 3 Dense + residual, 4 Dense + ShiftGELU, 5 attention, 6 Shiftmax, 7 ShiftGELU, 8 token assembly, 9 patch-merging
  * gather, 10 mean pooling, 11 the token-wise layers of a block in one kernel, 12 the constants of such
- * launches prepared, 13 root-mean-square norm, 14 Dense with real scales, 15 gated activation to int8), algorithmic integer operations (2 per int8 multiply-accumulate; 0 for row-wise kernels)
+ * launches prepared, 13 root-mean-square norm, 14 Dense with real scales, 15 gated activation to int8, 16 rotary
+ * positions, 17 rows into the cache, 18 attention over prompts, 19 over the cache, 20 its parts joined), algorithmic integer operations (2 per int8 multiply-accumulate; 0 for row-wise kernels)
  * and algorithmic HBM bytes (each operand read once, each result written once); *count receives the number of
  * launches seen.
  * One trace at a time per process, not thread-safe; launches beyond max_launches make ivit_trace_end
@@ -474,6 +476,96 @@ int ivit_linear_scaled(void* stream, const int8_t* x, int64_t ldx, const float* 
  * Requirements: 0 <= rows < 2^31, 1 <= C <= 32768.  Errors: NULL, SHAPE, PARAM (type, act), ALIGN, HIP. */
 int ivit_gated_quant(void* stream, const void* x, int64_t ldx, int8_t* y, int64_t ldy, float* y_scale, int64_t rows,
                      int32_t C, int32_t type, int32_t act, int32_t gated);
+
+/* ---- Attention over float rows: rotary positions, a paged cache, whole prompts, single tokens behind a shared prefix. --
+ * For the models of the section above whose sequences are longer than ivit_attention takes, causal, or answered token by
+ * token:  linear_scaled (q | k | v rows) -> cache_append (or rotary) -> prompt_attention, then per token cached_attention ->
+ * gated_quant (IVIT_ACT_NONE, not gated) -> linear_scaled.
+ *
+ *  - Heads lie side by side in a row: head h owns elements h d .. (h + 1) d.  H query heads share G key heads, H a multiple of
+ *    G: query head h reads key head h / (H / G).
+ *  - Rows, leading dimensions and alignment as in the section above, unless stated.  Rows and caches of attention are float16
+ *    or bfloat16, its head size d 64 or 128.
+ *  - Scores, the statistics of softmax and sums of values are held in 32 bits.  Weights, at most 256 (float16: 2^15) times the
+ *    largest, are rounded to the rows' type where the matrix cores multiply them, and their sum is that of the rounded ones.
+ *    Results are rounded once.  Equal calls give equal bits.
+ *  - A key left out (behind a query, past the end of its sequence) has no part in a result whatever it holds, NaN included; a
+ *    row without keys is zeros.  Rows of no sequence are left as they were. */
+
+/* Rotary positions: pair i of a head, i < rotary_dim / 2, is turned by  phi = positions[a][row] * freq[i],  a = axis ? axis[i] : 0:
+ *   (x1, x2) -> (x1 cos phi - x2 sin phi, x2 cos phi + x1 sin phi)
+ * (x1, x2) being elements (i, i + rotary_dim / 2) of the head, or (2 i, 2 i + 1) if adjacent != 0; elements from rotary_dim on
+ * are copied.  phi is formed in 64 bits and brought to one turn there, its sine and cosine are within 2^-22 of themselves plus
+ * |phi| 2^-51.  Several axes: images (row, column), video (time, row, column); a value of axis outside 0 .. n_axes - 1 is
+ * taken as the nearest of them. */
+typedef struct {
+    const int32_t* positions;     /* [n_axes, rows], any int32 values                               */
+    int64_t ld_positions;         /* elements between the axes of positions, >= rows                */
+    int32_t n_axes;               /* 1 .. 8                                                         */
+    const double* freq;           /* [rotary_dim / 2], radians a step                               */
+    const int32_t* axis;          /* [rotary_dim / 2], nullable (all 0)                             */
+    int32_t rotary_dim;           /* even, 2 .. d                                                   */
+    int32_t adjacent;
+} ivit_rotary_params;
+
+/* y = x with every head's pairs turned.  x, y [rows, heads * d] of `type` (float32, float16, bfloat16); y may be x itself (same
+ * pointer and leading dimension), no other overlap.  One rounding, of the result (float32: the two products and their sum).
+ * Requirements: 0 <= rows < 2^31, heads >= 1, 2 <= d <= 1024, d even, heads * d <= 2^24.
+ * Errors: NULL, SHAPE, PARAM (type, n_axes), ALIGN, HIP. */
+int ivit_rotary(void* stream, const void* x, int64_t ldx, void* y, int64_t ldy, int64_t rows, int32_t heads, int32_t d,
+                int32_t type, const ivit_rotary_params* r);
+
+/* A paged cache of keys and values.  Page p holds page_size slots of every key head; slot t of it is slot p * page_size + t of the
+ * cache and element e of head g lies at  p * ld_page + (g * page_size + t) * d + e.  type IVIT_I8: int8 rows of d with one scale
+ * each, as in the section above; k_scale, v_scale [n_pages, n_heads, page_size] dense. */
+typedef struct {
+    void *k, *v;                  /* 16-byte aligned                                                */
+    float *k_scale, *v_scale;     /* IVIT_I8 only                                                   */
+    int64_t ld_page;              /* elements between pages, >= n_heads * page_size * d, whole 16 bytes */
+    int32_t n_pages, page_size;   /* >= 1, n_pages * page_size < 2^31; page_size a power of two, 16 .. 1024 */
+    int32_t n_heads, head_dim;    /* G, d                                                           */
+    int32_t type;                 /* IVIT_F16, IVIT_BF16 (that of the rows) or IVIT_I8              */
+} ivit_cache;
+
+/* Row n's key heads, turned by r (NULL: as they are), and its value heads go to slot slots[n] of the cache; its query heads, turned
+ * likewise, to row n of q_out (q and q_out may be NULL, both).  A row whose slot lies outside the cache (a negative number for
+ * a padded one) is left out: nothing of it is written.  Slots should differ; of rows that name the same one either may be kept, and
+ * pieces of both.  int8: q = round(127 v / max |v|) of the turned values before any rounding, as ivit_gated_quant has it.
+ * q [rows, n_q_heads * d], k, v [rows, G * d] of `type` (float16, bfloat16), slots int32 [rows].  No overlap.
+ * Requirements: 0 <= rows < 2^31, n_q_heads * d and G * d <= 2^24.
+ * Errors: NULL, SHAPE, PARAM (type, the cache's type, n_axes), ALIGN, HIP. */
+int ivit_cache_append(void* stream, const void* q, int64_t ldq, void* q_out, int64_t ldq_out, int32_t n_q_heads, const void* k,
+                      int64_t ldk, const void* v, int64_t ldv, const int32_t* slots, int64_t rows, int32_t type,
+                      const ivit_rotary_params* r, const ivit_cache* c);
+
+/* Attention over whole prompts: o_i = sum_j p_ij v_j, p_i = softmax over j of scale q_i . k_j, within each of n_seq sequences.
+ * Sequence s has rows q_start[s] .. q_start[s + 1] of q and o and rows k_start[s] .. k_start[s + 1] of k and v (k_start NULL: those of
+ * q_start).  causal != 0: query i of n sees keys j <= i + (m - n) of m, so that the last query sees all (the first ones, where there
+ * are fewer keys than queries, none).
+ * q, o [n_q, H * d], k, v [n_k, G * d] of `type`; starts int32 [n_seq + 1] (device), not falling; a sequence that is not within the
+ * rows is left out.  scale > 0 and finite.  No overlap.
+ * Requirements: 0 <= n_q, n_k < 2^31, 0 <= n_seq < 2^20, H and G <= 4096, (n_q / 64 + n_seq) H < 2^24; ldk, ldv <= 2^24; leading dimensions and
+ * pointers of q, k, v, o whole 16 bytes.
+ * Errors: NULL, SHAPE, PARAM (type, scale), ALIGN, HIP. */
+int ivit_prompt_attention(void* stream, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, void* o,
+                          int64_t ldo, const int32_t* q_start, const int32_t* k_start, int32_t n_seq, int64_t n_q, int64_t n_k,
+                          int32_t H, int32_t G, int32_t d, int32_t type, float scale, int32_t causal);
+
+/* Attention of one token per request over the cache.  Request b reads the first prefix_len slots of the pages prefix_pages[0 ..]
+ * (shared: read once for all requests) and the first lens[b] of the pages pages[b * ld_pages + 0 ..], and attends over both.
+ * lens[b] < 0: not a request (a padded batch), its row of o is left as it was; a length beyond max_pages * page_size is taken as that.
+ * A page number outside the cache is taken as the nearest page (never a fault).
+ * q, o [B, H * d] of `type`; the cache of `type` or IVIT_I8; pages int32 [B, max_pages], lens int32 [B], prefix_pages int32
+ * [ceil(prefix_len / page_size)] (device; NULL where empty).  Graphs that may run at the same time need a workspace each; it holds nothing
+ * between calls.
+ * Requirements: 0 <= B <= 65536, H <= 4096, B H < 2^24, 0 <= prefix_len <= 2^30, max_pages * page_size <= 2^30; leading dimensions and pointers of q and o whole
+ * 16 bytes; workspace 256-byte aligned, at least ivit_cached_attention_workspace_bytes (0 for arguments that the call refuses).
+ * Errors: NULL, SHAPE, PARAM (types, scale), ALIGN, WORKSPACE, HIP. */
+size_t ivit_cached_attention_workspace_bytes(int32_t B, int32_t H, const ivit_cache* c, int32_t max_pages, int32_t prefix_len);
+int ivit_cached_attention(void* stream, const void* q, int64_t ldq, void* o, int64_t ldo, const ivit_cache* c,
+                          const int32_t* prefix_pages, int32_t prefix_len, const int32_t* pages, int64_t ld_pages, int32_t max_pages,
+                          const int32_t* lens, int32_t B, int32_t H, int32_t type, float scale, void* workspace,
+                          size_t workspace_bytes);
 
 /* ---- Host helpers: the floating-point side of a quantised model -> the integers this library takes. --------
  * Pure host code on HOST pointers; nothing is launched.  They realise Sec. 3.1 Eq. 6 (symmetric uniform

@@ -23,11 +23,13 @@ EXPORTS = ("ivit_strerror", "ivit_build_id", "ivit_linear_requant", "ivit_shiftm
            "ivit_mean_pool", "ivit_swin_window_index", "ivit_swin_shift_mask", "ivit_swin_workspace_bytes",
            "ivit_forward_swin", "ivit_shiftgelu_rowmax", "ivit_encoder_block_static", "ivit_linear_requant_ex",
            "ivit_last_hip_error", "ivit_probe_mfma_rate", "ivit_ilayernorm_limits", "ivit_rmsnorm_quant",
-           "ivit_linear_scaled", "ivit_gated_quant")
+           "ivit_linear_scaled", "ivit_gated_quant", "ivit_rotary", "ivit_cache_append", "ivit_prompt_attention",
+           "ivit_cached_attention_workspace_bytes", "ivit_cached_attention")
 
 KIND_NAMES = {1: "ilayernorm", 2: "gemm", 3: "gemm_residual", 4: "gemm_gelu", 5: "attention", 6: "shiftmax",
               7: "shiftgelu", 8: "embed_tokens", 9: "patch_merge_gather", 10: "mean_pool",
-              11: "gemm_token_block", 12: "gemm_token_tables", 13: "rmsnorm", 14: "gemm_scaled", 15: "gated"}
+              11: "gemm_token_block", 12: "gemm_token_tables", 13: "rmsnorm", 14: "gemm_scaled", 15: "gated",
+              16: "rotary", 17: "cache_append", 18: "prompt_attention", 19: "cached_attention", 20: "cached_attention_join"}
 
 
 class ShiftParams(C.Structure):
@@ -99,6 +101,16 @@ class SwinParams(C.Structure):
                 ("n_classes", C.c_int32), ("w_patch", _P), ("bias_patch", _P), ("patch_rq_b", _P), ("patch_rq_c", _P),
                 ("embed_ln", FinalLN), ("stages", SwinStage * 4), ("final_ln", FinalLN), ("pool_rq", Dyadic),
                 ("w_head", _P), ("bias_head", _P), ("head_rq_b", _P), ("head_rq_c", _P)]
+
+
+class RotaryParams(C.Structure):
+    _fields_ = [("positions", _P), ("ld_positions", C.c_int64), ("n_axes", C.c_int32), ("freq", _P), ("axis", _P), ("rotary_dim", C.c_int32),
+                ("adjacent", C.c_int32)]
+
+
+class Cache(C.Structure):
+    _fields_ = [("k", _P), ("v", _P), ("k_scale", _P), ("v_scale", _P), ("ld_page", C.c_int64)] + [
+        (n, C.c_int32) for n in ("n_pages", "page_size", "n_heads", "head_dim", "type")]
 
 
 class IvitError(RuntimeError):
@@ -188,6 +200,17 @@ def load():
     lib.ivit_linear_scaled.argtypes = [_P, _P, i64, _P, i32, _P, _P, _P, i32, _P, i64, _P, i64, i32, f32, i64, i32, i32]
     lib.ivit_gated_quant.restype = C.c_int
     lib.ivit_gated_quant.argtypes = [_P, _P, i64, _P, i64, _P, i64, i32, i32, i32, i32]
+    rotary, cache = C.POINTER(RotaryParams), C.POINTER(Cache)
+    lib.ivit_rotary.restype = C.c_int
+    lib.ivit_rotary.argtypes = [_P, _P, i64, _P, i64, i64, i32, i32, i32, rotary]
+    lib.ivit_cache_append.restype = C.c_int
+    lib.ivit_cache_append.argtypes = [_P, _P, i64, _P, i64, i32, _P, i64, _P, i64, _P, i64, i32, rotary, cache]
+    lib.ivit_prompt_attention.restype = C.c_int
+    lib.ivit_prompt_attention.argtypes = [_P, _P, i64, _P, i64, _P, i64, _P, i64, _P, _P, i32, i64, i64, i32, i32, i32, i32, C.c_float, i32]
+    lib.ivit_cached_attention_workspace_bytes.restype = C.c_size_t
+    lib.ivit_cached_attention_workspace_bytes.argtypes = [i32, i32, cache, i32, i32]
+    lib.ivit_cached_attention.restype = C.c_int
+    lib.ivit_cached_attention.argtypes = [_P, _P, i64, _P, i64, cache, _P, i32, _P, i64, i32, _P, i32, i32, i32, C.c_float, _P, C.c_size_t]
     lib.ivit_trace_begin.restype = C.c_int; lib.ivit_trace_begin.argtypes = [i32]
     lib.ivit_trace_end.restype = C.c_int
     lib.ivit_trace_end.argtypes = [C.POINTER(C.c_float), C.POINTER(i32), C.POINTER(i64), C.POINTER(i64), i32,
@@ -577,13 +600,13 @@ def ivit_forward_swin(patches, logits, params, B, workspace, stream=None):
 # ------------------------------------------------------------------ float layers around int8 products
 ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3, "gelu_tanh": 4, "gelu_sigmoid": 5}
 _TYPES = None           # torch dtype -> ivit_type (torch is imported by the first call)
-_FLOAT32 = _INT8 = _current_device = _raw_stream = None
+_FLOAT32 = _FLOAT64 = _INT8 = _INT32 = _current_device = _raw_stream = None
 
 
 def _setup():
-    global _TYPES, _FLOAT32, _INT8, _current_device, _raw_stream
+    global _TYPES, _FLOAT32, _FLOAT64, _INT8, _INT32, _current_device, _raw_stream
     import torch
-    _FLOAT32, _INT8 = torch.float32, torch.int8
+    _FLOAT32, _FLOAT64, _INT8, _INT32 = torch.float32, torch.float64, torch.int8, torch.int32
     # numbers alone, where torch has them: making a Stream object costs about as much as a launch
     _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
     _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
@@ -691,3 +714,143 @@ def ivit_gated_quant(x, y, y_scale, act="silu", gated=True, stream=None):
     if st:
         _check(st, where)
     return y
+
+
+# ------------------------------------------------------------------ attention over float rows and its cache
+def _whole_numbers(t, shape, device, where):
+    """Pointer of a dense int32 tensor (None: NULL)."""
+    if t is None:
+        return None
+    if t.shape == shape and t.dtype is _INT32 and t.get_device() == device and t.is_contiguous():
+        return t.data_ptr()
+    raise ValueError("%s: wanted dense int32 values %s on device %d, got %s of %s on %s" % (where, tuple(shape), device, tuple(t.shape), t.dtype, t.device))
+
+
+def rotary_params(r, rows, device, where="rotary_params"):
+    """RotaryParams from a dict: positions int32 [rows] or [axes, rows]; freq float64 [rotary_dim / 2], radians a step; axis int32
+    [rotary_dim / 2] or absent; adjacent: pairs (2 i, 2 i + 1) in place of (i, i + rotary_dim / 2)."""
+    pos, freq, axis = r["positions"], r["freq"], r.get("axis")
+    shape = pos.shape
+    axes = shape[0] if len(shape) == 2 else 1
+    if len(shape) not in (1, 2) or shape[-1] != rows or pos.dtype is not _INT32 or pos.get_device() != device or (rows > 1 and pos.stride(-1) != 1):
+        raise ValueError("%s: positions %s of %s on %s, wanted int32 [%d] or [axes, %d] on device %d" % (where, tuple(shape), pos.dtype, pos.device, rows, rows, device))
+    if freq.dim() != 1 or freq.dtype is not _FLOAT64 or freq.get_device() != device or not freq.is_contiguous():
+        raise ValueError("%s: freq has to be dense float64 [rotary_dim / 2] on device %d" % (where, device))
+    half = freq.shape[0]
+    return RotaryParams(pos.data_ptr(), pos.stride(0) if axes > 1 else rows, axes, freq.data_ptr(), _whole_numbers(axis, (half,), device, where), 2 * half,
+                        bool(r.get("adjacent", False)))
+
+
+def cache_struct(c, device, where="cache_struct"):
+    """Cache from a dict: k, v [n_pages, heads, page_size, head_dim], pages of one stride, each dense; int8 ones with k_scale, v_scale float32
+    [n_pages, heads, page_size]."""
+    k, v = c["k"], c["v"]
+    shape, kind = k.shape, _type(k, where)
+    if len(shape) != 4 or v.shape != shape or v.dtype is not k.dtype or k.get_device() != device or v.get_device() != device:
+        raise ValueError("%s: a cache of %s, %s on %s and %s, %s on %s, wanted two [pages, heads, page_size, head_dim] of one type on device %d" % (
+            where, tuple(shape), k.dtype, k.device, tuple(v.shape), v.dtype, v.device, device))
+    pages, heads, page, d = shape
+    inner = (page * d, d, 1)
+    ld = k.stride(0) if pages > 1 else heads * page * d
+    if k.stride()[1:] != inner or v.stride()[1:] != inner or (pages > 1 and v.stride(0) != ld):
+        raise ValueError("%s: pages of the cache have to be dense, and those of k and v one stride apart: %s and %s" % (where, k.stride(), v.stride()))
+    scales = [None, None]
+    if kind == 3:
+        scales = [_vector(c[n], pages * heads * page, device, where) for n in ("k_scale", "v_scale")]
+    return Cache(k.data_ptr(), v.data_ptr(), scales[0], scales[1], ld, pages, page, heads, d, kind)
+
+
+def ivit_rotary(x, y, head_dim, rotary, stream=None):
+    """x, y (may be x): [rows, heads * head_dim] float tensors of one type; rotary: see rotary_params.  Returns y."""
+    where = "ivit_rotary"
+    kind, dev, shape = _type(x, where), x.get_device(), x.shape
+    rows, cols = shape
+    if head_dim < 1 or cols % head_dim:
+        raise ValueError("%s: rows of %d are no heads of %d" % (where, cols, head_dim))
+    st = (_lib or load()).ivit_rotary(
+        _launch_stream(stream, dev, where), x.data_ptr(), _rows(x, shape, x.dtype, dev, where), y.data_ptr(), _rows(y, shape, x.dtype, dev, where),
+        rows, cols // head_dim, head_dim, kind, C.byref(rotary_params(rotary, rows, dev, where)))
+    if st:
+        _check(st, where)
+    return y
+
+
+def ivit_cache_append(k, v, slots, cache, rotary=None, q=None, q_out=None, stream=None):
+    """k, v: [rows, heads * head_dim] float16 or bfloat16; slots: int32 [rows]; cache: see cache_struct; rotary: see rotary_params, or None; q, q_out:
+    [rows, query heads * head_dim] or None.  Returns q_out."""
+    where = "ivit_cache_append"
+    kind, dev, shape, dtype = _type(k, where), k.get_device(), k.shape, k.dtype
+    c = cache_struct(cache, dev, where)
+    rows = shape[0]
+    if len(shape) != 2 or shape[1] != c.n_heads * c.head_dim:
+        raise ValueError("%s: keys %s for a cache of %d heads of %d" % (where, tuple(shape), c.n_heads, c.head_dim))
+    heads = 0
+    if q is not None:
+        heads = q.shape[1] // c.head_dim
+        if q.dim() != 2 or q.shape[1] != heads * c.head_dim or q_out is None:
+            raise ValueError("%s: queries %s are no heads of %d, or there is no q_out" % (where, tuple(q.shape), c.head_dim))
+    elif q_out is not None:
+        raise ValueError("%s: q_out without q" % where)
+    wide = (rows, heads * c.head_dim)
+    st = (_lib or load()).ivit_cache_append(
+        _launch_stream(stream, dev, where), _ptr(q), 0 if q is None else _rows(q, wide, dtype, dev, where),
+        _ptr(q_out), 0 if q is None else _rows(q_out, wide, dtype, dev, where), heads, k.data_ptr(), _rows(k, shape, dtype, dev, where),
+        v.data_ptr(), _rows(v, shape, dtype, dev, where), _whole_numbers(slots, (rows,), dev, where), rows, kind,
+        None if rotary is None else C.byref(rotary_params(rotary, rows, dev, where)), C.byref(c))
+    if st:
+        _check(st, where)
+    return q_out
+
+
+def ivit_prompt_attention(q, k, v, o, head_dim, q_start, k_start=None, scale=None, causal=True, stream=None):
+    """q, o: [rows, heads * head_dim], k, v: [key rows, key heads * head_dim], float16 or bfloat16; q_start, k_start: int32 [sequences + 1], the rows where
+    sequences begin and the end of the last (k_start None: as q_start); scale: None for 1 / sqrt(head_dim).  Returns o."""
+    where = "ivit_prompt_attention"
+    kind, dev, shape, kshape, dtype = _type(q, where), q.get_device(), q.shape, k.shape, q.dtype
+    n_q, n_k = shape[0], kshape[0]
+    if len(shape) != 2 or len(kshape) != 2 or head_dim < 1 or shape[1] % head_dim or kshape[1] % head_dim:
+        raise ValueError("%s: rows of %s and %s are no heads of %d" % (where, tuple(shape), tuple(kshape), head_dim))
+    if q_start.dim() != 1 or q_start.shape[0] < 1:
+        raise ValueError("%s: q_start has to hold a number more than there are sequences" % where)
+    n = q_start.shape[0]
+    st = (_lib or load()).ivit_prompt_attention(
+        _launch_stream(stream, dev, where), q.data_ptr(), _rows(q, shape, dtype, dev, where), k.data_ptr(), _rows(k, kshape, dtype, dev, where),
+        v.data_ptr(), _rows(v, kshape, dtype, dev, where), o.data_ptr(), _rows(o, shape, dtype, dev, where), _whole_numbers(q_start, (n,), dev, where),
+        _whole_numbers(k_start, (n,), dev, where), n - 1, n_q, n_k, shape[1] // head_dim, kshape[1] // head_dim, head_dim, kind,
+        head_dim ** -0.5 if scale is None else scale, bool(causal))
+    if st:
+        _check(st, where)
+    return o
+
+
+def ivit_cached_attention_workspace_bytes(requests, heads, cache, max_pages, prefix_len=0):
+    """Bytes of workspace of ivit_cached_attention; cache: see cache_struct."""
+    if _TYPES is None:
+        _setup()
+    c = cache_struct(cache, cache["k"].get_device(), "ivit_cached_attention_workspace_bytes")
+    return int((_lib or load()).ivit_cached_attention_workspace_bytes(requests, heads, C.byref(c), max_pages, prefix_len))
+
+
+def ivit_cached_attention(q, o, cache, pages, lens, workspace, prefix_pages=None, prefix_len=0, scale=None, stream=None):
+    """q, o: [requests, heads * head_dim] float16 or bfloat16; cache: see cache_struct; pages: int32 [requests, max_pages] with dense rows; lens: int32
+    [requests], -1 for a padded one; prefix_pages: int32, the pages that all requests share, with prefix_len slots of them in use; workspace: bytes, see
+    ivit_cached_attention_workspace_bytes; scale: None for 1 / sqrt(head_dim).  Returns o."""
+    where = "ivit_cached_attention"
+    kind, dev, shape, dtype = _type(q, where), q.get_device(), q.shape, q.dtype
+    c = cache_struct(cache, dev, where)
+    B, d, most = shape[0], c.head_dim, pages.shape[1]
+    if len(shape) != 2 or shape[1] % d:
+        raise ValueError("%s: rows of %s are no heads of %d" % (where, tuple(shape), d))
+    need = -(-prefix_len // c.page_size)
+    if prefix_len and (prefix_pages is None or prefix_pages.shape[0] < need):
+        raise ValueError("%s: a prefix of %d slots takes %d pages" % (where, prefix_len, need))
+    if workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError("%s: the workspace has to be dense, on device %d" % (where, dev))
+    st = (_lib or load()).ivit_cached_attention(
+        _launch_stream(stream, dev, where), q.data_ptr(), _rows(q, shape, dtype, dev, where), o.data_ptr(), _rows(o, shape, dtype, dev, where), C.byref(c),
+        None if prefix_pages is None else _whole_numbers(prefix_pages, prefix_pages.shape, dev, where), prefix_len,
+        pages.data_ptr(), _rows(pages, (B, most), _INT32, dev, where), most, _whole_numbers(lens, (B,), dev, where), B, shape[1] // d, kind,
+        d ** -0.5 if scale is None else scale, workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    if st:
+        _check(st, where)
+    return o

@@ -754,4 +754,130 @@ int ivit_gated_quant(void* stream, const void* x, int64_t ldx, int8_t* y, int64_
     return hip_status(ivit::launch_gated(static_cast<hipStream_t>(stream), a));
 }
 
+// ---- Attention over float rows and its cache
+
+static bool whole16(const void* p, int64_t ld, int type) { return aligned(p, 16) && (ld * ivit::element_bytes(type)) % 16 == 0; }
+
+// Rows that attention reads or writes 16 bytes at a time.
+static int check_wide_rows(const void* p, int64_t ld, int64_t cols, int type) {
+    const int st = check_rows(p, ld, cols, type);
+    return st != IVIT_OK ? st : whole16(p, ld, type) ? IVIT_OK : IVIT_ERR_ALIGN;
+}
+
+static int check_rotary(const ivit_rotary_params* r, int64_t rows, int32_t d, ivit::RotaryArgs* out) {
+    if (!r->freq || (rows > 0 && !r->positions)) return IVIT_ERR_NULL;
+    if (r->n_axes < 1 || r->n_axes > 8) return IVIT_ERR_PARAM;
+    if (r->rotary_dim < 2 || (r->rotary_dim & 1) || r->rotary_dim > d || r->ld_positions < rows || r->ld_positions > 0x7fffffffLL) return IVIT_ERR_SHAPE;
+    if (!aligned(r->positions, 4) || !aligned(r->freq, 8) || !aligned(r->axis, 4)) return IVIT_ERR_ALIGN;
+    *out = ivit::RotaryArgs{r->positions, r->freq, r->axis, r->ld_positions, r->n_axes, r->rotary_dim / 2, r->adjacent != 0};
+    return IVIT_OK;
+}
+
+// The cache as the kernels take it; row_type: of the rows that go in or of the queries.
+static int check_cache(const ivit_cache* c, int row_type, ivit::CacheArgs* out) {
+    if (row_type != IVIT_F16 && row_type != IVIT_BF16) return IVIT_ERR_PARAM;
+    if (c->type != row_type && c->type != IVIT_I8) return IVIT_ERR_PARAM;
+    if (c->head_dim != 64 && c->head_dim != 128) return IVIT_ERR_SHAPE;
+    if (c->page_size < 16 || c->page_size > 1024 || (c->page_size & (c->page_size - 1)) || c->n_pages < 1 ||
+        (int64_t)c->n_pages * c->page_size > 0x7fffffffLL || c->n_heads < 1 || c->n_heads > 4096) return IVIT_ERR_SHAPE;
+    const int64_t page = (int64_t)c->n_heads * c->page_size * c->head_dim;
+    if (c->ld_page < page || c->ld_page > ((int64_t)1 << 40)) return IVIT_ERR_SHAPE;
+    if (!c->k || !c->v || (c->type == IVIT_I8 && (!c->k_scale || !c->v_scale))) return IVIT_ERR_NULL;
+    if (!whole16(c->k, c->ld_page, c->type) || !whole16(c->v, c->ld_page, c->type)) return IVIT_ERR_ALIGN;
+    const bool i8 = c->type == IVIT_I8;
+    if (i8 && (!aligned(c->k_scale, 4) || !aligned(c->v_scale, 4))) return IVIT_ERR_ALIGN;
+    *out = ivit::CacheArgs{c->k, c->v, i8 ? c->k_scale : nullptr, i8 ? c->v_scale : nullptr, c->ld_page, c->n_pages, c->page_size, c->n_heads, c->head_dim,
+                           c->type};
+    return IVIT_OK;
+}
+
+int ivit_rotary(void* stream, const void* x, int64_t ldx, void* y, int64_t ldy, int64_t rows, int32_t heads, int32_t d, int32_t type,
+                const ivit_rotary_params* r) {
+    if (type != IVIT_F32 && type != IVIT_F16 && type != IVIT_BF16) return IVIT_ERR_PARAM;
+    if (!r) return IVIT_ERR_NULL;
+    if (rows < 0 || rows > 0x7fffffffLL || heads < 1 || d < 2 || (d & 1) || d > 1024 || (int64_t)heads * d > (1 << 24)) return IVIT_ERR_SHAPE;
+    ivit::RotaryArgs ra;
+    int st;
+    if ((st = check_rotary(r, rows, d, &ra)) != IVIT_OK) return st;
+    if (rows == 0) return IVIT_OK;
+    if (!x || !y) return IVIT_ERR_NULL;
+    const int64_t cols = (int64_t)heads * d;
+    if ((st = check_rows(x, ldx, cols, type)) != IVIT_OK || (st = check_rows(y, ldy, cols, type)) != IVIT_OK) return st;
+    if (x == y && ldx != ldy) return IVIT_ERR_PARAM;
+    return hip_status(ivit::launch_rotary(static_cast<hipStream_t>(stream), x, ldx, y, ldy, rows, heads, d, type, ra));
+}
+
+int ivit_cache_append(void* stream, const void* q, int64_t ldq, void* q_out, int64_t ldq_out, int32_t n_q_heads, const void* k, int64_t ldk,
+                      const void* v, int64_t ldv, const int32_t* slots, int64_t rows, int32_t type, const ivit_rotary_params* r, const ivit_cache* c) {
+    if (!c) return IVIT_ERR_NULL;
+    ivit::AppendArgs a{q, k, v, q_out, slots, ldq, ldq_out, ldk, ldv, rows, q ? n_q_heads : 0, type, {}, {}};
+    int st;
+    if ((st = check_cache(c, type, &a.c)) != IVIT_OK) return st;
+    if (rows < 0 || rows > 0x7fffffffLL) return IVIT_ERR_SHAPE;
+    const int d = c->head_dim;
+    if (r && (st = check_rotary(r, rows, d, &a.r)) != IVIT_OK) return st;
+    if ((int64_t)c->n_heads * d > (1 << 24)) return IVIT_ERR_SHAPE;
+    if (rows == 0) return IVIT_OK;
+    if (!k || !v || !slots || !q != !q_out) return IVIT_ERR_NULL;
+    if (q && (n_q_heads < 1 || (int64_t)n_q_heads * d > (1 << 24))) return IVIT_ERR_SHAPE;
+    if ((st = check_rows(k, ldk, (int64_t)c->n_heads * d, type)) != IVIT_OK || (st = check_rows(v, ldv, (int64_t)c->n_heads * d, type)) != IVIT_OK) return st;
+    if (q && ((st = check_rows(q, ldq, (int64_t)n_q_heads * d, type)) != IVIT_OK || (st = check_rows(q_out, ldq_out, (int64_t)n_q_heads * d, type)) != IVIT_OK))
+        return st;
+    if (!aligned(slots, 4)) return IVIT_ERR_ALIGN;
+    return hip_status(ivit::launch_cache_append(static_cast<hipStream_t>(stream), a));
+}
+
+int ivit_prompt_attention(void* stream, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, void* o, int64_t ldo,
+                          const int32_t* q_start, const int32_t* k_start, int32_t n_seq, int64_t n_q, int64_t n_k, int32_t H, int32_t G, int32_t d,
+                          int32_t type, float scale, int32_t causal) {
+    if ((type != IVIT_F16 && type != IVIT_BF16) || !std::isfinite(scale) || !(scale > 0.0f)) return IVIT_ERR_PARAM;
+    if (n_q < 0 || n_q > 0x7fffffffLL || n_k < 0 || n_k > 0x7fffffffLL || n_seq < 0 || n_seq >= (1 << 20) || (d != 64 && d != 128)) return IVIT_ERR_SHAPE;
+    if (H < 1 || H > 4096 || G < 1 || G > H || H % G || (!k_start && n_q != n_k) || (n_q / 64 + n_seq) * H >= (1 << 24)) return IVIT_ERR_SHAPE;
+    if (n_k > 0 && (ldk > (1 << 24) || ldv > (1 << 24))) return IVIT_ERR_SHAPE;
+    if (n_q == 0 || n_seq == 0) return IVIT_OK;
+    if (!q || !o || !q_start || (n_k > 0 && (!k || !v))) return IVIT_ERR_NULL;
+    int st;
+    if ((st = check_wide_rows(q, ldq, (int64_t)H * d, type)) != IVIT_OK || (st = check_wide_rows(o, ldo, (int64_t)H * d, type)) != IVIT_OK) return st;
+    if (n_k > 0 && ((st = check_wide_rows(k, ldk, (int64_t)G * d, type)) != IVIT_OK || (st = check_wide_rows(v, ldv, (int64_t)G * d, type)) != IVIT_OK)) return st;
+    if (!aligned(q_start, 4) || !aligned(k_start, 4)) return IVIT_ERR_ALIGN;
+    const ivit::PromptArgs a{q, k, v, o, q_start, k_start ? k_start : q_start, ldq, ldk, ldv, ldo, n_q, n_k, n_seq, H, G, d, type, scale, causal != 0};
+    return hip_status(ivit::launch_prompt_attention(static_cast<hipStream_t>(stream), a));
+}
+
+// What the size of the workspace goes by; row_type < 0: any that the cache takes.
+static int check_cached(const ivit_cache* c, int32_t B, int32_t H, int32_t max_pages, int32_t prefix_len, int row_type, ivit::CachedArgs* a) {
+    if (!c) return IVIT_ERR_NULL;
+    int st;
+    if ((st = check_cache(c, row_type >= 0 ? row_type : c->type == IVIT_I8 ? IVIT_BF16 : c->type, &a->c)) != IVIT_OK) return st;
+    if (B < 0 || B > 65536 || H < 1 || H > 4096 || c->n_heads > H || H % c->n_heads || prefix_len < 0 || prefix_len > (1 << 30) || max_pages < 0 ||
+        (int64_t)max_pages * c->page_size > (1 << 30) || (int64_t)B * H >= (1 << 24)) return IVIT_ERR_SHAPE;
+    a->B = B; a->H = H; a->max_pages = max_pages; a->prefix_len = prefix_len;
+    return IVIT_OK;
+}
+
+size_t ivit_cached_attention_workspace_bytes(int32_t B, int32_t H, const ivit_cache* c, int32_t max_pages, int32_t prefix_len) {
+    ivit::CachedArgs a{};
+    return check_cached(c, B, H, max_pages, prefix_len, -1, &a) == IVIT_OK ? ivit::cached_attention_workspace(a) : 0;
+}
+
+int ivit_cached_attention(void* stream, const void* q, int64_t ldq, void* o, int64_t ldo, const ivit_cache* c, const int32_t* prefix_pages,
+                          int32_t prefix_len, const int32_t* pages, int64_t ld_pages, int32_t max_pages, const int32_t* lens, int32_t B, int32_t H,
+                          int32_t type, float scale, void* workspace, size_t workspace_bytes) {
+    if ((type != IVIT_F16 && type != IVIT_BF16) || !std::isfinite(scale) || !(scale > 0.0f)) return IVIT_ERR_PARAM;
+    ivit::CachedArgs a{};
+    int st;
+    if ((st = check_cached(c, B, H, max_pages, prefix_len, type, &a)) != IVIT_OK) return st;
+    if (B == 0) return IVIT_OK;
+    if (!q || !o || !lens || (max_pages > 0 && !pages) || (prefix_len > 0 && !prefix_pages)) return IVIT_ERR_NULL;
+    if (ld_pages < max_pages || ld_pages > 0x7fffffffLL) return IVIT_ERR_SHAPE;
+    const int64_t cols = (int64_t)H * c->head_dim;
+    if ((st = check_wide_rows(q, ldq, cols, type)) != IVIT_OK || (st = check_wide_rows(o, ldo, cols, type)) != IVIT_OK) return st;
+    if (!aligned(pages, 4) || !aligned(lens, 4) || !aligned(prefix_pages, 4)) return IVIT_ERR_ALIGN;
+    if (!workspace || workspace_bytes < ivit::cached_attention_workspace(a)) return IVIT_ERR_WORKSPACE;
+    if (!aligned(workspace, 256)) return IVIT_ERR_ALIGN;
+    a.q = q; a.o = o; a.prefix_pages = prefix_pages; a.pages = pages; a.lens = lens; a.ldq = ldq; a.ldo = ldo; a.ld_pages = ld_pages;
+    a.type = type; a.scale = scale; a.workspace = workspace;
+    return hip_status(ivit::launch_cached_attention(static_cast<hipStream_t>(stream), a));
+}
+
 }  // extern "C"

@@ -114,13 +114,31 @@ struct ScaledArgs {
 hipError_t launch_linear_scaled(hipStream_t s, const ScaledArgs& a);
 hipError_t launch_linear_scaled_rows(hipStream_t s, const ScaledArgs& a);      // few rows (gemm_scaled_rows.hip)
 
+// Attention over float rows and its cache (rotary.hip, prompt_attention.hip, cached_attention.hip).  Leading dimensions count elements.
+struct RotaryArgs { const int32_t* positions; const double* freq; const int32_t* axis; int64_t ld_positions; int n_axes, half; bool adjacent; };   // half 0: no turn
+struct CacheArgs { void *k, *v; float *k_scale, *v_scale; int64_t ld_page; int n_pages, page_size, G, d, type; };
+hipError_t launch_rotary(hipStream_t s, const void* x, int64_t ldx, void* y, int64_t ldy, int64_t rows, int heads, int d, int type, const RotaryArgs& r);
+struct AppendArgs { const void *q, *k, *v; void* q_out; const int32_t* slots; int64_t ldq, ldq_out, ldk, ldv, rows; int H, type; RotaryArgs r; CacheArgs c; };
+hipError_t launch_cache_append(hipStream_t s, const AppendArgs& a);
+struct PromptArgs {
+    const void *q, *k, *v; void* o; const int32_t *q_start, *k_start; int64_t ldq, ldk, ldv, ldo, n_q, n_k; int n_seq, H, G, d, type; float scale; bool causal;
+};
+hipError_t launch_prompt_attention(hipStream_t s, const PromptArgs& a);
+struct CachedArgs {
+    const void* q; void* o; const int32_t *prefix_pages, *pages, *lens; int64_t ldq, ldo, ld_pages; int prefix_len, max_pages, B, H, type; float scale;
+    CacheArgs c; void* workspace;
+};
+size_t cached_attention_workspace(const CachedArgs& a);
+hipError_t launch_cached_attention(hipStream_t s, const CachedArgs& a);
+
 // Number of compute units of the current device (cached); used to size persistent grids.
 int num_cus();
 
 // Kinds of launches reported by the trace (ivit_trace_end); values are part of the C ABI.
 enum LaunchKind { KIND_ILAYERNORM = 1, KIND_GEMM = 2, KIND_GEMM_RESIDUAL = 3, KIND_GEMM_GELU = 4,
                   KIND_ATTENTION = 5, KIND_SHIFTMAX = 6, KIND_SHIFTGELU = 7, KIND_EMBED = 8, KIND_PATCH_MERGE = 9, KIND_MEAN_POOL = 10,
-                  KIND_TOKEN_BLOCK = 11, KIND_TOKEN_TABLES = 12, KIND_RMSNORM = 13, KIND_GEMM_SCALED = 14, KIND_GATED = 15 };
+                  KIND_TOKEN_BLOCK = 11, KIND_TOKEN_TABLES = 12, KIND_RMSNORM = 13, KIND_GEMM_SCALED = 14, KIND_GATED = 15, KIND_ROTARY = 16,
+                  KIND_CACHE_APPEND = 17, KIND_PROMPT_ATTENTION = 18, KIND_CACHED_ATTENTION = 19, KIND_CACHED_JOIN = 20 };
 
 // Brackets one kernel launch with two HIP events on its stream while a trace is active; otherwise a no-op.
 // ops = algorithmic integer operations (2 per int8 multiply-accumulate), bytes = algorithmic HBM bytes.

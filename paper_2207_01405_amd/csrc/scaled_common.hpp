@@ -1,5 +1,5 @@
 // Pieces shared by the operators around int8 Dense layers whose scales are real numbers taken at run time (rows_scaled.hip,
-// gemm_scaled.hip, gemm_scaled_rows.hip): element types, activations, rounding.
+// gemm_scaled.hip, gemm_scaled_rows.hip) and those that bring float rows into a cache (rotary.hip): element types, activations, rounding.
 //
 // Arithmetic is in 32-bit floating point throughout; int8 products are summed exactly in 32-bit integers.  A value is rounded to
 // fewer bits once, where it is stored (round to nearest, ties to even).
@@ -115,6 +115,47 @@ __device__ __forceinline__ uint32_t round_bits(float a, float b) { return __floa
 // the low bytes of four words
 __device__ __forceinline__ uint32_t pack4(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     return __builtin_amdgcn_perm(b, a, 0x0c0c0400u) | __builtin_amdgcn_perm(d, c, 0x04000c0cu);
+}
+
+constexpr uint32_t kNormal = 0x00800000u, kInf = 0x7f800000u;      // the bits of |v|, as unsigned numbers, are in the order of |v|; NaN comes last
+
+// What a row's int8 form needs: the largest |v|, 127 / it in 32 bits, and the scale of a row whose v still lack `factor`.  A row of zeros (or
+// whose factor leaves nothing of it) has the scale 0; a row with a NaN or an infinite value, or with one that the factor takes beyond the range,
+// NaN; both count as rows with a largest of 0: zeros.
+struct Quant { float top, inv, scale; };
+__device__ __forceinline__ Quant quant_of(uint32_t top_bits, float factor) {
+    const float top = __uint_as_float(top_bits);
+    if (top_bits >= kInf) return Quant{0.0f, 0.0f, __uint_as_float(0x7fc00000u)};
+    const float most = top * factor, scale = most / 127.0f;
+    if (most > 0x1.fffffep127f) return Quant{0.0f, 0.0f, __uint_as_float(0x7fc00000u)};
+    if (scale == 0.0f) return Quant{0.0f, 0.0f, 0.0f};
+    return Quant{top, 127.0f / top, scale};
+}
+
+// q = round(127 v / top), ties to even, of the exact quotient.  v inv is within 127 units of 2^-24 of it, so a value whose v inv is not that near a
+// tie is rounded as it stands, by one multiply-add.  Next to ties (half of the largest is one: 63.5) 64 bits decide: there the quotient is
+// within 2^-45, a quotient of two 24-bit numbers that is no tie is 2^-32 from one at least, and adding and taking away 1.5 2^12 leaves it at a
+// multiple of 2^-40, ties as they are.  Tiny rows, whose inv may not be finite, go the same way.
+__device__ __forceinline__ int32_t nearest(float v, double up) { return (int32_t)__builtin_rint(__builtin_fma((double)v, up, 6144.0) - 6144.0); }
+__device__ __forceinline__ void store_q(int8_t* p, const v8f& v, const Quant& q, int n) {
+    uint32_t w[8];
+    float far = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        w[e] = round_bits(v[e], q.inv);
+        far = __builtin_fmaxf(far, __builtin_fabsf(__builtin_fmaf(v[e], q.inv, kRound - __uint_as_float(w[e]))));
+    }
+    if (__builtin_expect(far >= 0.5f - 0x1p-16f || q.top < 0x1p-100f, 0)) {
+        const double up = q.top > 0.0f ? 127.0 / (double)q.top : 0.0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = q.top > 0.0f ? (uint32_t)nearest(v[e], up) : 0u;
+    }
+    typedef uint32_t v2u __attribute__((ext_vector_type(2), aligned(1)));
+    const v2u out = {pack4(w[0], w[1], w[2], w[3]), pack4(w[4], w[5], w[6], w[7])};
+    if (n >= 8) { *reinterpret_cast<v2u*>(p) = out; return; }
+#pragma unroll
+    for (int e = 0; e < 7; ++e)
+        if (e < n) p[e] = (int8_t)(out[e >> 2] >> (8 * (e & 3)));
 }
 
 }  // namespace scaled
