@@ -22,7 +22,7 @@ _REGST = ["-mllvm", "-amdgpu-mfma-vgpr-form", "-Wno-inline-asm"]
 EXTRA_FLAGS = {"gemm_rs.hip": _REGST, "gemm_ks.hip": _REGST, "gemm_tl.hip": ["-Wno-inline-asm"],
                "gemm_st.hip": ["-Wno-inline-asm"], "gemm_kq.hip": ["-Wno-inline-asm"], "token_block.hip": ["-Wno-inline-asm"],
                "token_stream.hip": ["-Wno-inline-asm"], "gemm_scaled.hip": ["-Wno-inline-asm"], "gemm_scaled_rows.hip": ["-Wno-inline-asm"],
-               "prompt_attention.hip": ["-Wno-inline-asm"], "cached_attention.hip": ["-Wno-inline-asm"]}
+               "prompt_attention.hip": _REGST, "cached_attention.hip": _REGST}
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++20", "-fPIC", "-Wall", "-Wno-unused-function",
          # packed FP32 instructions are kept out of every code object of this library
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]

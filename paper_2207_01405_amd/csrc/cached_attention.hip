@@ -159,16 +159,17 @@ __global__ __launch_bounds__(64 * W) void cached_attention_kernel(CaParams P) {
             for (int r = 0; r < 16; ++r)
                 if (8 * (r / 4) + r % 4 > rel) s[0][r] = -__builtin_inff();
         }
-        V8 p[2];
+        V8 pw[1][2];
+        V8 (&p)[2] = pw[0];
         if constexpr (I8) {
             // Weights times the values' scales, over 2^ref: what float16 holds goes by the largest scale so far.
             const float most = scale[BK + li];
             float top = most;
 #pragma unroll
             for (int x = 1; x < 32; x *= 2) top = __builtin_fmaxf(top, __shfl_xor(top, x));
-            softmax_step_scaled<T, DT>(s[0], p, m, l, acc, P.c, ref, n == 0, top, scale + BK + 4 * half);
+            softmax_step_scaled<T, DT>(s, p, m, l, acc, P.c, ref, n == 0, top, scale + BK + 4 * half);
         } else {
-            softmax_step<T, 1, DT>(s, p, m, l, acc, P.c);
+            softmax_step<T, 1, DT>(s, pw, m, l, acc, P.c);
         }
 #pragma unroll
         for (int t = 0; t < 2; ++t)
@@ -181,12 +182,12 @@ __global__ __launch_bounds__(64 * W) void cached_attention_kernel(CaParams P) {
                     const int j = (lane & 15) >> 1, row = 16 * t + 4 * half + (j & 3) + 8 * (j >> 2), col = 32 * i + 16 * ((lane >> 4) & 1) + 8 * (lane & 1);
                     vf = spread<T>(__builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr8_b64_v2i32((at)(vl + row * RB + 16 * ((col >> 4) ^ mix8<D>(row)) + (col & 15)))));
                 } else {
-                    vf = transposed<T, D>(vl, 16 * t, i, lane);
+                    vf = transposed<T, D>(vl + transposed_at<D>(i, lane) + 16 * t * RB);
                 }
                 acc[i] = mfma(vf, p[t], acc[i]);
             }
     }
-    l += __shfl_xor(l, 32);
+    l = add_halves(l);
 
     // the wavefronts' parts: largest scores and sums, then the outputs
     if (half == 0) { join_m[wv][li] = m; join_l[wv][li] = l; }
@@ -273,7 +274,6 @@ Plan plan_of(const CachedArgs& a) {
 size_t ml_bytes(const CachedArgs& a, int parts) { return ((size_t)parts * a.B * a.H * 8 + 255) & ~(size_t)255; }
 
 template <class T, int D, bool I8> hipError_t launch(hipStream_t s, const CachedArgs& a) {
-    using TL = CaTile<T, D, I8>;
     const Plan p = plan_of(a);
     const int parts = p.prefix_parts + p.own_parts;
     float* const ml = static_cast<float*>(a.workspace);

@@ -26,6 +26,30 @@ __device__ __forceinline__ v16f mfma(Elem<_Float16>::v8 a, Elem<_Float16>::v8 b,
 __device__ __forceinline__ float add_pair(Elem<__bf16>::v2 a, float c) { return __builtin_amdgcn_fdot2_f32_bf16(a, Elem<__bf16>::v2{(__bf16)1.0f, (__bf16)1.0f}, c, false); }
 __device__ __forceinline__ float add_pair(Elem<_Float16>::v2 a, float c) { return __builtin_amdgcn_fdot2(a, Elem<_Float16>::v2{(_Float16)1.0f, (_Float16)1.0f}, c, false); }
 
+// The largest of three, NaN if one is (the other kind of maximum would quiet the operands first, an instruction a score)
+__device__ __forceinline__ float max3(float a, float b, float c) { return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c); }
+// The larger of a lane's value and that of its place in the other half of the wavefront; their sum
+__device__ __forceinline__ float max_halves(float x) {
+    const v2u r = __builtin_bit_cast(v2u, __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false));
+    return __builtin_elementwise_maximum(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float add_halves(float x) {
+    const v2u r = __builtin_bit_cast(v2u, __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false));
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+// The largest of a lane's 16 N scores and of the other half's.
+template <int N> __device__ __forceinline__ float largest_of(const v16f (&s)[N]) {
+    float a = max3(s[0][0], s[0][1], s[0][2]), b = max3(s[0][3], s[0][4], s[0][5]);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int r = i ? 0 : 6; r < 16; r += 4) {
+            a = max3(a, s[i][r], s[i][r + 1]);
+            if (r + 2 < 16) b = max3(b, s[i][r + 2], s[i][r + 3]);
+        }
+    return max_halves(__builtin_elementwise_maximum(a, b));
+}
+
 // The 16-byte pieces of a key's row are stored at piece ^ mix(row), so that reads of many rows are spread over the banks: for keys 16 lanes read the
 // same piece of 16 rows, for values 32 lanes read 64 bytes of four rows (4 n .. 4 n + 3).
 template <int D> __device__ __forceinline__ int mix_k(int row) { return D == 128 ? row & 15 : (row >> 1) & 7; }
@@ -33,10 +57,12 @@ template <int D> __device__ __forceinline__ int mix_v(int row) { return D == 128
 
 // The fragment of values for the keys of registers 8 t .. 8 t + 7 of a lane's scores, k0 = 16 t: keys k0 + 4 half + 0 .. 3 and k0 + 8 + 4 half + 0 .. 3 of
 // dimension 32 i + lane % 32.  The transposing read takes 4 rows x 16 elements from 16 lanes, 8 bytes each, and gives a lane one column.
-template <class T, int D> __device__ __forceinline__ typename Elem<T>::v8 transposed(const int8_t* tile, int k0, int i, int lane) {
+template <int D> __device__ __forceinline__ int transposed_at(int i, int lane) {              // where its first row's bytes are, of k0 = 0
+    const int row = 4 * (lane >> 5) + ((lane >> 2) & 3), col = 32 * i + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+    return row * 2 * D + 16 * ((col >> 3) ^ mix_v<D>(row)) + 2 * (col & 7);
+}
+template <class T, int D> __device__ __forceinline__ typename Elem<T>::v8 transposed(const int8_t* p) {
     typedef v4s __attribute__((address_space(3)))* at;
-    const int row = k0 + 4 * (lane >> 5) + ((lane >> 2) & 3), col = 32 * i + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);      // of the first of the two
-    const int8_t* const p = tile + row * 2 * D + 16 * ((col >> 3) ^ mix_v<D>(row)) + 2 * (col & 7);
     const v4s a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((at)p), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((at)(p + 8 * 2 * D));      // (mix_v(row + 8) is mix_v(row))
     return __builtin_bit_cast(typename Elem<T>::v8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
@@ -44,14 +70,7 @@ template <class T, int D> __device__ __forceinline__ typename Elem<T>::v8 transp
 // One step of the softmax of a lane's query over 32 KB scores (both halves of the wavefront hold one query's): the weights of the scores, rounded and
 // packed, and their sum; maximum, sum and output brought along.  The maximum that the weights stand against is moved only where a score exceeds it by
 // more than 2^8 in weight: the output's 16 DT registers are rescaled a few times in all then, not at every step, and no weight exceeds 2^8.
-template <class T, int KB, int DT>
-__device__ __forceinline__ void softmax_step(const v16f (&s)[KB], typename Elem<T>::v8 (&p)[2 * KB], float& m, float& l, v16f (&acc)[DT], float c) {
-    float top = s[0][0];
-#pragma unroll
-    for (int b = 0; b < KB; ++b)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) top = __builtin_fmaxf(top, s[b][r]);
-    top = __builtin_fmaxf(top, __shfl_xor(top, 32));
+template <int DT> __device__ __forceinline__ void move_largest(float top, float& m, float& l, v16f (&acc)[DT], float c) {
     if (__builtin_expect(__any((top - m) * c > 8.0f), 0)) {             // (m = -infinity to begin with; -infinity less -infinity is NaN and not more)
         const float to = __builtin_fmaxf(top, m), f = to > m ? __builtin_amdgcn_exp2f((m - to) * c) : 1.0f;
         m = to;
@@ -61,28 +80,33 @@ __device__ __forceinline__ void softmax_step(const v16f (&s)[KB], typename Elem<
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][r] *= f;
     }
-    const float base = Elem<T>::kUp - (m == -__builtin_inff() ? 0.0f : m * c);
+}
+// what the exponents of the weights start from
+template <class T> __device__ __forceinline__ float base_of(float m, float c) { return Elem<T>::kUp - (m == -__builtin_inff() ? 0.0f : m * c); }
+// weights r and r + 1 of a lane's 16 scores
+template <class T> __device__ __forceinline__ void weigh(const v16f& s, int r, typename Elem<T>::v8 (&p)[2], float& l, float c, float base) {
+    const v2f w = {__builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c, base)), __builtin_amdgcn_exp2f(__builtin_fmaf(s[r + 1], c, base))};
+    const typename Elem<T>::v2 q = __builtin_convertvector(w, typename Elem<T>::v2);
+    l = add_pair(q, l);
+    p[r / 8][r % 8] = q[0];
+    p[r / 8][r % 8 + 1] = q[1];
+}
+template <class T, int KB, int DT>
+__device__ __forceinline__ void softmax_step(const v16f (&s)[KB], typename Elem<T>::v8 (&p)[KB][2], float& m, float& l, v16f (&acc)[DT], float c) {
+    move_largest<DT>(largest_of(s), m, l, acc, c);
+    const float base = base_of<T>(m, c);
 #pragma unroll
     for (int b = 0; b < KB; ++b)
 #pragma unroll
-        for (int r = 0; r < 16; r += 2) {
-            const v2f w = {__builtin_amdgcn_exp2f(__builtin_fmaf(s[b][r], c, base)), __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][r + 1], c, base))};
-            const typename Elem<T>::v2 q = __builtin_convertvector(w, typename Elem<T>::v2);
-            l = add_pair(q, l);
-            p[2 * b + r / 8][r % 8] = q[0];
-            p[2 * b + r / 8][r % 8 + 1] = q[1];
-        }
+        for (int r = 0; r < 16; r += 2) weigh<T>(s[b], r, p[b], l, c, base);
 }
 
 // The same over 16 scores, for values of int8 rows: the weights that leave are times the values' scales (scale[8 (r / 4) + r % 4]) over 2^ref, ref following
 // the largest scale of the block, the same for all lanes; the sum is that of the weights alone.  The output is in units of 2^ref.
 template <class T, int DT>
-__device__ __forceinline__ void softmax_step_scaled(const v16f& s, typename Elem<T>::v8 (&p)[2], float& m, float& l, v16f (&acc)[DT], float c, float& ref,
+__device__ __forceinline__ void softmax_step_scaled(const v16f (&s)[1], typename Elem<T>::v8 (&p)[2], float& m, float& l, v16f (&acc)[DT], float c, float& ref,
                                                     bool first, float largest, const float* scale) {
-    float top = s[0];
-#pragma unroll
-    for (int r = 0; r < 16; ++r) top = __builtin_fmaxf(top, s[r]);
-    top = __builtin_fmaxf(top, __shfl_xor(top, 32));
+    const float top = largest_of(s);
     const float power = __builtin_fminf(__builtin_fmaxf(__builtin_ceilf(__builtin_amdgcn_logf(largest)), -120.0f), 120.0f);
     if (__builtin_expect(__any((top - m) * c > 8.0f) || first || power > ref, 0)) {
         const float to = (top - m) * c > 8.0f ? top : m, by = first ? power : __builtin_fmaxf(power, ref);
@@ -98,7 +122,7 @@ __device__ __forceinline__ void softmax_step_scaled(const v16f& s, typename Elem
     const float base = Elem<T>::kUp - (m == -__builtin_inff() ? 0.0f : m * c), down = __builtin_amdgcn_exp2f(-ref);
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-        const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c, base));
+        const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[0][r], c, base));
         l += w;
         p[r / 8][r % 8] = (T)(w * (scale[8 * (r / 4) + r % 4] * down));
     }

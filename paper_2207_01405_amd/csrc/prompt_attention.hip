@@ -64,18 +64,23 @@ __global__ __launch_bounds__(64 * W) void prompt_attention_kernel(PaParams P) {
     const uint32_t ldk2 = (uint32_t)P.ldk * 2, ldv2 = (uint32_t)P.ldv * 2;
     const uint32_t kpiece = 16 * (lp ^ mix_k<D>(lr)), vpiece = 16 * (lp ^ mix_v<D>(lr));
     const uint32_t lds0 = lds_offset(lds) + 1024 * wv;
-    auto issue = [&](int kt, int buf) __attribute__((always_inline)) {
-        const int8_t* const kp = uniform_ptr(reinterpret_cast<const int8_t*>(kbase + (int64_t)kt * BK * P.ldk));
-        const int8_t* const vp = uniform_ptr(reinterpret_cast<const int8_t*>(vbase + (int64_t)kt * BK * P.ldv));
+    // tile n of the order in which they are taken, the last keys first; keys into buffer n % 2 of theirs, values likewise
+    auto issue = [&](int n, auto values) __attribute__((always_inline)) {
+        constexpr bool V = decltype(values)::value;
+        const int kt = tiles - 1 - n;
+        const int64_t ld = V ? P.ldv : P.ldk;
+        const int8_t* const p = uniform_ptr(reinterpret_cast<const int8_t*>((V ? vbase : kbase) + (int64_t)kt * BK * ld));
         const int last = nk - 1 - kt * BK;                                        // (rows behind the sequence: its last row again)
+        const uint32_t to = lds0 + (n & 1) * 2 * TILE + (V ? TILE : 0);
 #pragma unroll
-        for (int i = 0; i < LI; ++i) {
-            const int r = min(LR * W * i + lr, last);
-            dma16(kp, (uint32_t)r * ldk2 + kpiece, lds0 + buf * 2 * TILE + i * 1024 * W);
-            dma16(vp, (uint32_t)r * ldv2 + vpiece, lds0 + buf * 2 * TILE + TILE + i * 1024 * W);
-        }
+        for (int i = 0; i < LI; ++i) dma16(p, (uint32_t)min(LR * W * i + lr, last) * (V ? ldv2 : ldk2) + (V ? vpiece : kpiece), to + i * 1024 * W);
     };
-    if (tiles > 0) issue(tiles - 1, 0);
+    constexpr std::false_type keys{};
+    constexpr std::true_type values{};
+    if (tiles > 0) {
+        issue(0, keys);
+        issue(0, values);
+    }
 
     // the queries: B operand, query li, elements 16 s + 8 half on
     V8 qf[QT][DS];
@@ -97,69 +102,137 @@ __global__ __launch_bounds__(64 * W) void prompt_attention_kernel(PaParams P) {
 #pragma unroll
         for (int i = 0; i < DT; ++i) acc[t][i] = v16f{};
     }
-    const int sees_all = P.causal ? min(mine + shift, nk - 1) : nk - 1;            // the last key that all of the wavefront's queries see
     const int sees_any = P.causal ? min(min(mine + 32 * QT, nq) - 1 + shift, nk - 1) : nk - 1;
     const bool idle = mine >= nq;
+    // tiles of which not all queries of the workgroup see all keys
+    const int all_see = P.causal ? min(first + shift, nk - 1) : nk - 1;
+    const int odd = tiles - max(min((all_see + 1) / BK, tiles), 0);
+
+    int at_k[DS], at_v[DT];                                                       // where this lane's fragments lie in a tile
+#pragma unroll
+    for (int d = 0; d < DS; ++d) at_k[d] = li * RB + 16 * ((2 * d + half) ^ mix_k<D>(li));
+#pragma unroll
+    for (int i = 0; i < DT; ++i) at_v[i] = TILE + transposed_at<D>(i, lane);
+    auto key_frag = [&](int buf, int b, int d) __attribute__((always_inline)) {
+        return *reinterpret_cast<const V8*>(lds + at_k[d] + buf * 2 * TILE + 32 * b * RB);
+    };
+    auto value_frag = [&](int buf, int b, int i) __attribute__((always_inline)) { return transposed<T, D>(lds + at_v[i] + buf * 2 * TILE + 16 * b * RB); };
+    auto scores = [&](v16f (&s)[QT][KB], int buf) __attribute__((always_inline)) {
+#pragma unroll
+        for (int d = 0; d < DS; ++d)
+#pragma unroll
+            for (int b = 0; b < KB; ++b) {
+                const V8 kf = key_frag(buf, b, d);
+#pragma unroll
+                for (int t = 0; t < QT; ++t) s[t][b] = mfma(kf, qf[t][d], d ? s[t][b] : v16f{});
+            }
+    };
 
 #pragma unroll 1
-    for (int n = 0; n < tiles; ++n) {
-        const int kt = tiles - 1 - n, buf = n & 1, k0 = kt * BK;
+    for (int n = 0; n < odd; ++n) {
+        const int k0 = (tiles - 1 - n) * BK, buf = n & 1;
         arrive<0>();
-        if (kt > 0) issue(kt - 1, buf ^ 1);
+        if (n + 1 < tiles) {
+            issue(n + 1, keys);
+            issue(n + 1, values);
+        }
         if (idle || k0 > sees_any) continue;
-        const int8_t* const kl = lds + buf * 2 * TILE;
-        const int8_t* const vl = kl + TILE;
-        const bool masked = k0 + BK - 1 > sees_all;
         v16f s[QT][KB];
-#pragma unroll
-        for (int b = 0; b < KB; ++b)
-#pragma unroll
-            for (int t = 0; t < QT; ++t) s[t][b] = v16f{};
-#pragma unroll
-        for (int b = 0; b < KB; ++b)
-#pragma unroll
-            for (int d = 0; d < DS; ++d) {
-                const V8 kf = *reinterpret_cast<const V8*>(kl + (32 * b + li) * RB + 16 * ((2 * d + half) ^ mix_k<D>(li)));
-#pragma unroll
-                for (int t = 0; t < QT; ++t) s[t][b] = mfma(kf, qf[t][d], s[t][b]);
-            }
-        V8 p[QT][2 * KB];
+        scores(s, buf);
+        V8 p[QT][KB][2];
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
-            if (masked) {
-                const int rel = limit[t] - k0 - 4 * half;
+            const int rel = limit[t] - k0 - 4 * half;
 #pragma unroll
-                for (int b = 0; b < KB; ++b)
+            for (int b = 0; b < KB; ++b)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        if (32 * b + 8 * (r / 4) + r % 4 > rel) s[t][b][r] = -__builtin_inff();
-            }
+                for (int r = 0; r < 16; ++r) s[t][b][r] = 32 * b + 8 * (r / 4) + r % 4 > rel ? -__builtin_inff() : s[t][b][r];
             softmax_step<T, KB, DT>(s[t], p[t], m[t], l[t], acc[t], P.c);
         }
 #pragma unroll
         for (int b = 0; b < 2 * KB; ++b)
 #pragma unroll
             for (int i = 0; i < DT; ++i) {
-                const V8 vf = transposed<T, D>(vl, 16 * b, i, lane);
+                const V8 vf = value_frag(buf, b, i);
 #pragma unroll
-                for (int t = 0; t < QT; ++t) acc[t][i] = mfma(vf, p[t][b], acc[t][i]);
+                for (int t = 0; t < QT; ++t) acc[t][i] = mfma(vf, p[t][b / 2][b % 2], acc[t][i]);
             }
-        if (masked) {
-            // A key left out has the weight 0, and 0 times an infinite value or NaN is NaN: where the masked tiles, which come first, leave a value that is
-            // not finite, they are done again, key by key, with those that count only.
+        // A key left out has the weight 0, and 0 times an infinite value or NaN is NaN: where these tiles, which come first, leave a value that is
+        // not finite, they are done again, key by key, with those that count only.
+#pragma unroll
+        for (int t = 0; t < QT; ++t)
+            if (__builtin_expect(__any(not_finite<DT>(acc[t])), 0)) {
+                const int row = min(mine + 32 * t + li, nq - 1);
+                key_by_key<T, D>(static_cast<const T*>(P.q) + (int64_t)(qa + row) * P.ldq + (int64_t)head * D, kbase, P.ldk, vbase, P.ldv, k0, limit[t],
+                                 P.c, half, m[t], l[t], acc[t]);
+            }
+    }
+    // The tiles that all queries see.  Scores are formed a tile ahead of the values' product, so that its matrix instructions stand between the vector
+    // instructions of the softmax.
+    if (odd < tiles) {
+        arrive<0>();
+        if (odd + 1 < tiles) issue(odd + 1, keys);
+        v16f even_s[QT][KB], odd_s[QT][KB];
+        float top[QT];
+        // one tile: its scores in s, the next one's into next; buf: the buffer of its values, the next keys are in the other one
+        auto step = [&](int n, auto buf_c, v16f (&s)[QT][KB], v16f (&next)[QT][KB]) __attribute__((always_inline)) {
+            constexpr int buf = decltype(buf_c)::value;
+            arrive<0>();
+            if (n + 2 < tiles) issue(n + 2, keys);
+            if (n + 1 < tiles) issue(n + 1, values);
+            float base[QT];
+#pragma unroll
+            for (int t = 0; t < QT; ++t) {
+                move_largest<DT>(top[t], m[t], l[t], acc[t], P.c);
+                base[t] = base_of<T>(m[t], P.c);
+            }
+            V8 p[QT][KB][2];
+            scores(next, buf ^ 1);                                                // (of the last tile: of what the other buffer holds, not used)
 #pragma unroll
             for (int t = 0; t < QT; ++t)
-                if (__builtin_expect(__any(not_finite<DT>(acc[t])), 0)) {
-                    const int row = min(mine + 32 * t + li, nq - 1);
-                    key_by_key<T, D>(static_cast<const T*>(P.q) + (int64_t)(qa + row) * P.ldq + (int64_t)head * D, kbase, P.ldk, vbase, P.ldv, k0, limit[t],
-                                     P.c, half, m[t], l[t], acc[t]);
+#pragma unroll
+                for (int b = 0; b < KB; ++b)
+#pragma unroll
+                    for (int r = 0; r < 16; r += 2) weigh<T>(s[t][b], r, p[t][b], l[t], P.c, base[t]);
+#pragma unroll
+            for (int b = 0; b < 2 * KB; ++b)
+#pragma unroll
+                for (int i = 0; i < DT; ++i) {
+                    const V8 vf = value_frag(buf, b, i);
+#pragma unroll
+                    for (int t = 0; t < QT; ++t) acc[t][i] = mfma(vf, p[t][b / 2][b % 2], acc[t][i]);
                 }
+#pragma unroll
+            for (int t = 0; t < QT; ++t) top[t] = largest_of(next[t]);
+#ifdef SCHED
+            SCHED
+#endif
+        };
+        constexpr std::integral_constant<int, 0> b0{};
+        constexpr std::integral_constant<int, 1> b1{};
+        int n = odd;
+        if (n & 1) {
+            scores(odd_s, 1);
+#pragma unroll
+            for (int t = 0; t < QT; ++t) top[t] = largest_of(odd_s[t]);
+            step(n, b1, odd_s, even_s);
+            ++n;
+        } else {
+            scores(even_s, 0);
+#pragma unroll
+            for (int t = 0; t < QT; ++t) top[t] = largest_of(even_s[t]);
         }
+#pragma unroll 1
+        for (; n + 1 < tiles; n += 2) {
+            step(n, b0, even_s, odd_s);
+            step(n + 1, b1, odd_s, even_s);
+        }
+        if (n < tiles) step(n, b0, even_s, odd_s);
     }
     if (idle) return;
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
-        const float total = l[t] + __shfl_xor(l[t], 32), inv = total > 0.0f ? 1.0f / total : total != total ? total : 0.0f;
+        const float total = add_halves(l[t]), inv = total > 0.0f ? 1.0f / total : total != total ? total : 0.0f;
         const int row = mine + 32 * t + li;
         if (row < nq) store_rows<T, DT>(static_cast<T*>(P.o) + (int64_t)(qa + row) * P.ldo + (int64_t)head * D, acc[t], inv, half);
     }
