@@ -137,10 +137,10 @@ template <int DT> __device__ __forceinline__ bool not_finite(const v16f (&acc)[D
     return z != z;
 }
 
-// The state of a lane's query after keys first .. last, one key after the other, from memory.
-template <class T, int D>
+// The state of a lane's query after those of the keys first .. last that count, one key after the other, from memory.
+template <class T, int D, class Counts>
 __device__ __forceinline__ void key_by_key(const T* q, const T* k, int64_t ldk, const T* v, int64_t ldv, int first, int last, float c, int half, float& m,
-                                           float& l, v16f (&acc)[D / 32]) {
+                                           float& l, v16f (&acc)[D / 32], Counts&& counts) {
     auto score = [&](int j) __attribute__((always_inline)) {
         const T* const kj = k + j * ldk;
         float sum = 0.0f;
@@ -153,10 +153,12 @@ __device__ __forceinline__ void key_by_key(const T* q, const T* k, int64_t ldk, 
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) acc[i] = v16f{};
 #pragma unroll 1
-    for (int j = first; j <= last; ++j) m = __builtin_fmaxf(m, score(j));
+    for (int j = first; j <= last; ++j)
+        if (counts(j)) m = __builtin_fmaxf(m, score(j));
     const float base = Elem<T>::kUp - (m == -__builtin_inff() ? 0.0f : m * c);
 #pragma unroll 1
     for (int j = first; j <= last; ++j) {
+        if (!counts(j)) continue;
         const float w = (float)(T)__builtin_amdgcn_exp2f(__builtin_fmaf(score(j), c, base));
         const T* const vj = v + j * ldv + 4 * half;
         l += half ? 0.0f : w;                                           // (the halves' sums are added in the end)
