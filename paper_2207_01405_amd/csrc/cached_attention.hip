@@ -3,9 +3,9 @@
 //   o_b = softmax over the prefix's keys and the request's own of scale q_b . k, times their values
 //
 // The keys are cut into parts: the prefix into some for all requests together, whose queries (all requests, the heads of a group) are then rows of one
-// product, and each request's own keys into as many for every request.  A workgroup takes 32 query rows against one part; its wavefronts take blocks of
-// 32 keys of it in turn, each through LDS of its own, and join what they have at the end.  The parts of a row, its largest score, sum and unscaled output
-// each, are joined by a second launch, in a fixed order.
+// product, and each request's own keys by their number.  A workgroup takes 32 query rows against one part; its wavefronts take blocks of 32 keys of it in
+// turn, each through LDS of its own without a barrier, and join what they have at the end.  The parts of a row, its largest score, sum and unscaled
+// output each, are joined by a second launch, in a fixed order.
 //
 // int8 rows come into LDS as they are and are spread to 16 bits on the way to the matrix cores, where whole numbers up to 127 are exact.  The keys' scales
 // go to the scores, the values' to the weights.
@@ -18,22 +18,31 @@ namespace {
 using namespace regst;
 using namespace fatt;
 
-constexpr int W = 4, BK = 32, S = 2;           // wavefronts; keys of a block; blocks of a wavefront in LDS
+typedef float v4f __attribute__((ext_vector_type(4)));
+
+constexpr int W = 4, BK = 32, LEAST = 2 * W;   // wavefronts; keys of a block; blocks of the smallest part
 
 struct CaParams {
     const void* q; void* o; const int8_t *k, *v; const float *ks, *vs; const int32_t *prefix_pages, *pages, *lens; float *ml, *part;
     int64_t ldq, ldo, ld_pages, ld_page;       // ld_page in bytes
-    int prefix_len, max_len, B, H, G, group, page_shift, n_pages, prefix_parts, own_parts, prefix_tiles, own_tiles; float c;
+    int prefix_len, max_len, B, H, G, group, page_shift, n_pages, prefix_parts, own_parts, own_least, prefix_tiles; float c;
+    FastDiv by_head, by_prefix_part, by_own_part, by_own_tile, by_group, by_heads;
 };
 
-template <class T, int D, bool I8> struct CaTile {
-    static constexpr int RB = I8 ? D : 2 * D, BYTES = BK * RB, STAGE = 2 * BYTES + (I8 ? 2 * 4 * BK : 0);      // of a key's row; keys or values; a block
-    static constexpr int OUT = BK * (D + 4) * 4;                                                              // a wavefront's output on its way to the others
-    static constexpr int WAVE = S * STAGE > OUT ? S * STAGE : OUT;
+// RB: bytes of a key's row; BYTES: of the keys or values of a block.  A wavefront has S blocks of keys and S of values in LDS or on their way there, some
+// 16 KB in all, so that two workgroups fit a CU; keys are asked for again as soon as the scores are formed, values behind their product.  In the end
+// the space takes the wavefronts' outputs.
+template <int D, bool I8> struct CaTile {
+    static constexpr int RB = I8 ? D : 2 * D, BYTES = BK * RB, S = I8 || D == 64 ? 2 : 1, STAGE = 2 * BYTES + (I8 ? 2 * 4 * BK : 0);
+    static constexpr int OUT = 64 * 16 * (D / 32) * 4, WAVE = S * STAGE > OUT ? S * STAGE : OUT;
 };
 
 // 16-byte pieces of an int8 row: piece ^ mix8(row), for keys (8 bytes of 32 rows at a time) and values (8 bytes of 8 rows, twice) alike
 template <int D> __device__ __forceinline__ int mix8(int row) { return D == 128 ? row & 7 : (row >> 1) & 3; }
+
+// all loads but the newest N have arrived; all LDS reads have
+template <int N> __device__ __forceinline__ void wait_but() { asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory"); }
+__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
 // 4 bytes per lane from an address of its own into LDS at dst + 4 lane
 __device__ __forceinline__ void dma4_at(const float* p, uint32_t dst) {
@@ -49,76 +58,91 @@ template <class T> __device__ __forceinline__ typename Elem<T>::v8 spread(v2u b)
 }
 
 template <class T, int D, bool I8>
-__global__ __launch_bounds__(64 * W) void cached_attention_kernel(CaParams P) {
-    using TL = CaTile<T, D, I8>;
+__global__ __launch_bounds__(64 * W, 2) void cached_attention_kernel(CaParams P) {
+    using TL = CaTile<D, I8>;
     using V8 = typename Elem<T>::v8;
-    constexpr int RB = TL::RB, DS = D / 16, DT = D / 32, PC = RB / 16, LR = 64 / PC, LI = BK / LR;      // pieces of a row; rows of a load instruction; loads of a block
+    constexpr int RB = TL::RB, S = TL::S, DS = D / 16, DT = D / 32, PC = RB / 16, LR = 64 / PC, LI = BK / LR;      // pieces of a row; rows of a load instruction; loads
     __shared__ __align__(16) int8_t lds[W * TL::WAVE];
     __shared__ float join_m[W][32], join_l[W][32];
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, li = lane & 31;
 
-    // which rows, which keys
-    const int prefix_items = P.prefix_tiles * P.G * P.prefix_parts;
-    int item = blockIdx.x, g, b = 0, r0, rows, len, part, parts;
+    // which rows, which keys; a head's workgroups are G apart: on the same XCD, if G is a multiple of 8
+    uint32_t g_, part_;
+    const uint32_t item = P.by_head.divide(blockIdx.x, g_), prefix_items = (uint32_t)(P.prefix_tiles * P.prefix_parts);
+    const int g = (int)g_;
+    int b = 0, r0, rows, len, parts, least = LEAST;
     const bool prefix = item < prefix_items;
     const int32_t* table;
-    if (prefix) {                                          // items of the same keys are a multiple of the heads' and parts' number apart
-        part = item % P.prefix_parts; item /= P.prefix_parts;
-        g = item % P.G;
-        r0 = 32 * (item / P.G);
+    if (prefix) {
+        r0 = 32 * (int)P.by_prefix_part.divide(item, part_);
         rows = P.B * P.group;
         len = P.prefix_len; parts = P.prefix_parts; table = P.prefix_pages;
     } else {
-        item -= prefix_items;
-        part = item % P.own_parts; item /= P.own_parts;
-        g = item % P.G; item /= P.G;
-        r0 = 32 * (item % P.own_tiles);
-        b = item / P.own_tiles;
+        uint32_t t;
+        b = (int)P.by_own_tile.divide(P.by_own_part.divide(item - prefix_items, part_), t);
+        r0 = 32 * (int)t;
         rows = P.group;
-        len = P.lens[b]; parts = P.own_parts; table = P.pages + (int64_t)b * P.ld_pages;
+        len = P.lens[b]; parts = P.own_parts; least = P.own_least; table = P.pages + (int64_t)b * P.ld_pages;
         if (len < 0) return;
         len = min(len, P.max_len);
     }
-    const int blocks = (len + BK - 1) / BK, each = max((blocks + parts - 1) / parts, W);
-    const int b0 = min(part * (int64_t)each, (int64_t)blocks), b1 = min(b0 + each, blocks);
+    const int part = (int)part_, blocks = (len + BK - 1) / BK, each = max((blocks + parts - 1) / parts, least);
+    const int b0 = (int)min64(part * (int64_t)each, blocks), b1 = min(b0 + each, blocks);
     const int out_part = prefix ? part : P.prefix_parts + part, all_parts = P.prefix_parts + P.own_parts;
     auto row_of = [&](int r, int& rb, int& rh) __attribute__((always_inline)) {        // request and head of row r
-        const int x = r0 + r;
-        rb = prefix ? x / P.group : b;
-        rh = g * P.group + (prefix ? x % P.group : x);
+        uint32_t rest = (uint32_t)(r0 + r);
+        rb = prefix ? (int)P.by_group.divide(rest, rest) : b;
+        rh = g * P.group + (int)rest;
     };
+    if (b0 == b1 && all_parts > 1) {                       // no keys here
+        int rb, rh;
+        row_of(tid, rb, rh);
+        if (tid < 32 && r0 + tid < rows) {
+            const int64_t at = (int64_t)out_part * P.B * P.H + (int64_t)rb * P.H + rh;
+            P.ml[2 * at] = -__builtin_inff();
+            P.ml[2 * at + 1] = 0.0f;
+        }
+        return;
+    }
 
     // loads: instruction i brings rows LR i + lane / PC, physical piece lane % PC
     int8_t* const mine = lds + wv * TL::WAVE;
     const uint32_t lds0 = lds_offset(mine);
     const int mask = (1 << P.page_shift) - 1, lr = lane / PC, lp = lane % PC;
     typedef const int32_t __attribute__((address_space(4)))* scalar_table;
-    auto issue = [&](int blk, int buf) __attribute__((always_inline)) {
+    auto issue = [&](int blk, int buf, auto values) __attribute__((always_inline)) {
+        constexpr bool V = decltype(values)::value;
         const int k0 = blk * BK, last = len - 1;
-        int scale_page[2];
+        int page[2];
 #pragma unroll
-        for (int a = 0; a < 2; ++a) {                      // 16 keys, which lie in one page (behind the last key: that one again)
-            const int first = min(k0 + 16 * a, last);
-            const int page = min(max(((scalar_table)table)[first >> P.page_shift], 0), P.n_pages - 1);
-            const int64_t at = (int64_t)page * P.ld_page + ((int64_t)g << P.page_shift) * RB;
-            const int8_t *const kp = uniform_ptr(P.k + at), *const vp = uniform_ptr(P.v + at);
+        for (int a = 0; a < 2; ++a)                        // 16 keys lie in one page (behind the last key: that one again)
+            page[a] = min(max(((scalar_table)table)[min(k0 + 16 * a, last) >> P.page_shift], 0), P.n_pages - 1);
+#pragma unroll
+        for (int a = 0; a < 2; ++a) {
+            const int8_t* const p = uniform_ptr((V ? P.v : P.k) + (int64_t)page[a] * P.ld_page + ((int64_t)g << P.page_shift) * RB);
 #pragma unroll
             for (int i = 0; i < LI / 2; ++i) {
                 const int r = 16 * a + LR * i + lr, slot = min(k0 + r, last) & mask;
-                const int mk = I8 ? mix8<D>(r) : mix_k<D>(r), mv = I8 ? mix8<D>(r) : mix_v<D>(r);
-                const uint32_t to = lds0 + buf * TL::STAGE + (a * (LI / 2) + i) * 1024;
-                dma16(kp, slot * RB + 16 * (lp ^ mk), to);
-                dma16(vp, slot * RB + 16 * (lp ^ mv), to + TL::BYTES);
+                const int mix = I8 ? mix8<D>(r) : V ? mix_v<D>(r) : mix_k<D>(r);
+                dma16(p, slot * RB + 16 * (lp ^ mix), lds0 + buf * TL::STAGE + (V ? TL::BYTES : 0) + (a * (LI / 2) + i) * 1024);
             }
-            if constexpr (I8) scale_page[a] = page;
         }
-        if constexpr (I8) {                                // lanes 0 .. 31: the keys' scales, 32 .. 63: the values'
-            const int64_t slots = ((int64_t)(li < 16 ? scale_page[0] : scale_page[1]) * P.G + g) << P.page_shift;
+        if constexpr (I8 && !V) {                          // lanes 0 .. 31: the keys' scales, 32 .. 63: the values'
+            const int64_t slots = ((int64_t)(li < 16 ? page[0] : page[1]) * P.G + g) << P.page_shift;
             dma4_at((half ? P.vs : P.ks) + slots + (min(k0 + li, last) & mask), lds0 + buf * TL::STAGE + 2 * TL::BYTES);
         }
     };
-    int blk = b0 + wv;
-    if (blk < b1) issue(blk, 0);
+    constexpr std::false_type keys{};
+    constexpr std::true_type values{};
+    constexpr int KL = LI + (I8 ? 1 : 0), PAIR = KL + LI;  // loads of a block's keys; of its keys and values
+    const int own = (b1 - b0 - wv + W - 1) / W;            // the wavefront's blocks: b0 + wv + W n
+    auto block = [&](int n) __attribute__((always_inline)) { return b0 + wv + W * n; };
+#pragma unroll
+    for (int n = 0; n < S; ++n)
+        if (n < own) {
+            issue(block(n), n, keys);
+            issue(block(n), n, values);
+        }
 
     V8 qf[DS];
     {
@@ -128,16 +152,18 @@ __global__ __launch_bounds__(64 * W) void cached_attention_kernel(CaParams P) {
 #pragma unroll
         for (int s = 0; s < DS; ++s) qf[s] = *reinterpret_cast<const V8*>(qp + 16 * s);
     }
+    // (here, where all loads so far are waited for: the waits in the loop count its own ones)
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     v16f acc[DT];
     float m = -__builtin_inff(), l = 0.0f, ref = 0.0f;
 #pragma unroll
     for (int i = 0; i < DT; ++i) acc[i] = v16f{};
 
 #pragma unroll 1
-    for (int n = 0; blk < b1; ++n, blk += W) {
-        const int buf = n & 1;
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-        if (blk + W < b1) issue(blk + W, buf ^ 1);
+    for (int n = 0; n < own; ++n) {
+        const int blk = block(n), buf = S == 1 ? 0 : n & 1;
+        if (n + S - 1 < own) wait_but<LI + (S - 1) * PAIR>();              // behind the block's keys: its values, the next S - 1 blocks
+        else wait_but<0>();
         const int8_t* const kl = mine + buf * TL::STAGE;
         const int8_t* const vl = kl + TL::BYTES;
         v16f s[1] = {v16f{}};
@@ -148,10 +174,21 @@ __global__ __launch_bounds__(64 * W) void cached_attention_kernel(CaParams P) {
             else kf = *reinterpret_cast<const V8*>(kl + li * RB + 16 * ((2 * d + half) ^ mix_k<D>(li)));
             s[0] = mfma(kf, qf[d], s[0]);
         }
-        const float* const scale = reinterpret_cast<const float*>(kl + 2 * TL::BYTES);
+        float ks[16], vs[16], top_scale = 0.0f;
+        if constexpr (I8) {
+            const float* const scale = reinterpret_cast<const float*>(kl + 2 * TL::BYTES);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                ks[r] = scale[8 * (r / 4) + 4 * half + r % 4];
+                vs[r] = scale[BK + 8 * (r / 4) + 4 * half + r % 4];
+            }
+            top_scale = scale[BK + li];
+        }
+        wait_lds();
+        if (n + S < own) issue(block(n + S), buf, keys);
         if constexpr (I8) {
 #pragma unroll
-            for (int r = 0; r < 16; ++r) s[0][r] *= scale[8 * (r / 4) + 4 * half + r % 4];
+            for (int r = 0; r < 16; ++r) s[0][r] *= ks[r];
         }
         if ((blk + 1) * BK > len) {
             const int rel = len - 1 - blk * BK - 4 * half;
@@ -159,18 +196,17 @@ __global__ __launch_bounds__(64 * W) void cached_attention_kernel(CaParams P) {
             for (int r = 0; r < 16; ++r)
                 if (8 * (r / 4) + r % 4 > rel) s[0][r] = -__builtin_inff();
         }
-        V8 pw[1][2];
-        V8 (&p)[2] = pw[0];
+        V8 p[1][2];
         if constexpr (I8) {
             // Weights times the values' scales, over 2^ref: what float16 holds goes by the largest scale so far.
-            const float most = scale[BK + li];
-            float top = most;
 #pragma unroll
-            for (int x = 1; x < 32; x *= 2) top = __builtin_fmaxf(top, __shfl_xor(top, x));
-            softmax_step_scaled<T, DT>(s, p, m, l, acc, P.c, ref, n == 0, top, scale + BK + 4 * half);
+            for (int x = 1; x < 32; x *= 2) top_scale = __builtin_fmaxf(top_scale, __shfl_xor(top_scale, x));
+            softmax_step_scaled<T, DT>(s, p[0], m, l, acc, P.c, ref, n == 0, top_scale, vs);
         } else {
-            softmax_step<T, 1, DT>(s, pw, m, l, acc, P.c);
+            softmax_step<T, 1, DT>(s, p, m, l, acc, P.c);
         }
+        if (n + S < own) wait_but<(S - 1) * PAIR + KL>();                  // behind its values: the next S - 1 blocks, and the keys behind them
+        else wait_but<0>();
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -184,91 +220,129 @@ __global__ __launch_bounds__(64 * W) void cached_attention_kernel(CaParams P) {
                 } else {
                     vf = transposed<T, D>(vl + transposed_at<D>(i, lane) + 16 * t * RB);
                 }
-                acc[i] = mfma(vf, p[t], acc[i]);
+                acc[i] = mfma(vf, p[0][t], acc[i]);
             }
+        wait_lds();
+        if (n + S < own) issue(block(n + S), buf, values);
     }
     l = add_halves(l);
 
-    // the wavefronts' parts: largest scores and sums, then the outputs
+    // The wavefronts' parts: largest scores and sums, then the outputs, a lane's registers to the same lane; a wavefront joins every fourth tile of 32 elements.
     if (half == 0) { join_m[wv][li] = m; join_l[wv][li] = l; }
-    float* const out = reinterpret_cast<float*>(mine);
     const float up = I8 ? __builtin_amdgcn_exp2f(ref) : 1.0f;
-    __syncthreads();                                       // (every wavefront has read its last block)
+    float* const out = reinterpret_cast<float*>(mine) + lane;
 #pragma unroll
     for (int i = 0; i < DT; ++i)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) out[li * (D + 4) + 32 * i + 8 * (r / 4) + 4 * half + r % 4] = acc[i][r] * up;
+        for (int r = 0; r < 16; ++r) out[64 * (16 * i + r)] = acc[i][r] * up;
     __syncthreads();
-    constexpr int TPR = 256 / 32, E = D / TPR;             // threads of a row; elements of a thread
-    const int row = tid / TPR, e0 = tid % TPR * E;
-    if (r0 + row >= rows) return;
-    float top = join_m[0][row], f[W], sum = 0.0f, val[E] = {};
+    float top = join_m[0][li], f[W], sum = 0.0f;
 #pragma unroll
-    for (int w = 1; w < W; ++w) top = __builtin_fmaxf(top, join_m[w][row]);
+    for (int w = 1; w < W; ++w) top = __builtin_fmaxf(top, join_m[w][li]);
 #pragma unroll
     for (int w = 0; w < W; ++w) {
-        f[w] = join_l[w][row] == 0.0f ? 0.0f : __builtin_amdgcn_exp2f((join_m[w][row] - top) * P.c);
-        if (join_l[w][row] == 0.0f) continue;              // (no keys)
-        sum = __builtin_fmaf(f[w], join_l[w][row], sum);
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-            val[e] = __builtin_fmaf(f[w], reinterpret_cast<const float*>(lds + w * TL::WAVE)[row * (D + 4) + e0 + e], val[e]);
+        f[w] = join_m[w][li] == top ? 1.0f : __builtin_amdgcn_exp2f((join_m[w][li] - top) * P.c);
+        sum = __builtin_fmaf(f[w], join_l[w][li], sum);
     }
+    if (r0 + li >= rows) return;
     int rb, rh;
-    row_of(row, rb, rh);
-    if (all_parts == 1) {
-        if (P.lens[rb] < 0) return;
-        T* const o = static_cast<T*>(P.o) + (int64_t)rb * P.ldo + (int64_t)rh * D + e0;
-        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-#pragma unroll
-        for (int e = 0; e < E; ++e) o[e] = (T)(val[e] * inv);
-        return;
-    }
+    row_of(li, rb, rh);
+    if (all_parts == 1 && P.lens[rb] < 0) return;
     const int64_t at = (int64_t)out_part * P.B * P.H + (int64_t)rb * P.H + rh;
-    if (e0 == 0) { P.ml[2 * at] = top; P.ml[2 * at + 1] = sum; }
-    if (sum != 0.0f)
+    if (all_parts > 1 && tid < 32) { P.ml[2 * at] = top; P.ml[2 * at + 1] = sum; }
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    static_assert(DT <= W, "a tile a wavefront");
+    if (wv >= DT) return;
+    v16f o[1] = {v16f{}};
 #pragma unroll
-        for (int e = 0; e < E; ++e) P.part[at * D + e0 + e] = val[e];
+    for (int w = 0; w < W; ++w)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[0][r] = __builtin_fmaf(f[w], reinterpret_cast<const float*>(lds + w * TL::WAVE)[lane + 64 * (16 * wv + r)], o[0][r]);
+    if (all_parts == 1) {
+        store_rows<T, 1>(static_cast<T*>(P.o) + (int64_t)rb * P.ldo + (int64_t)rh * D + 32 * wv, o, inv, half);
+    } else {
+        float* const to = P.part + at * D + 32 * wv + 4 * half;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) *reinterpret_cast<v4f*>(to + 8 * q) = v4f{o[0][4 * q], o[0][4 * q + 1], o[0][4 * q + 2], o[0][4 * q + 3]};
+    }
 }
 
 // One wavefront a row: the parts' outputs, each times 2^(its maximum less the largest).
 template <class T, int D> __global__ __launch_bounds__(256) void join_kernel(CaParams P, int parts) {
+    constexpr int E = D / 64;
     const int lane = threadIdx.x & 63;
     const int64_t rows = (int64_t)P.B * P.H, row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (row >= rows) return;
-    const int b = (int)(row / P.H);
+    uint32_t h;
+    const int b = (int)P.by_heads.divide((uint32_t)row, h);
     if (P.lens[b] < 0) return;
-    float top = -__builtin_inff();
-    for (int p = 0; p < parts; ++p)
-        if (P.ml[2 * (p * rows + row) + 1] != 0.0f) top = __builtin_fmaxf(top, P.ml[2 * (p * rows + row)]);
-    float sum = 0.0f, val[D / 64] = {};
-    for (int p = 0; p < parts; ++p) {
-        const int64_t at = p * rows + row;
-        const float l = P.ml[2 * at + 1];
-        if (l == 0.0f) continue;
-        const float f = __builtin_amdgcn_exp2f((P.ml[2 * at] - top) * P.c);
-        sum = __builtin_fmaf(f, l, sum);
+    float top = -__builtin_inff(), sum = 0.0f, val[E] = {};
+#pragma unroll 1
+    for (int p0 = 0; p0 < parts; p0 += 64) {               // 64 parts at once: lane i has part p0 + i
+        float m = -__builtin_inff(), l = 0.0f;
+        if (p0 + lane < parts) {
+            m = P.ml[2 * ((p0 + lane) * rows + row)];
+            l = P.ml[2 * ((p0 + lane) * rows + row) + 1];
+        }
+        float most = l != 0.0f ? m : -__builtin_inff();
 #pragma unroll
-        for (int e = 0; e < D / 64; ++e) val[e] = __builtin_fmaf(f, P.part[at * D + lane * (D / 64) + e], val[e]);
+        for (int x = 1; x < 64; x *= 2) most = __builtin_fmaxf(most, __shfl_xor(most, x));
+        const float to = __builtin_fmaxf(top, most), f = to == top ? 1.0f : __builtin_amdgcn_exp2f((top - to) * P.c);
+        sum *= f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) val[e] *= f;
+        top = to;
+        const float w = l == 0.0f ? 0.0f : m == top ? 1.0f : __builtin_amdgcn_exp2f((m - top) * P.c);
+        const uint64_t there = __ballot(l != 0.0f);
+        // four at once: those without keys were not written, and one that was is loaded in their place, for nothing
+        const int n = min(64, parts - p0), some = there ? __builtin_ctzll(there) : 0;
+        if (there)
+#pragma unroll 1
+            for (int i0 = 0; i0 < n; i0 += 4) {
+                float x[4][E], wi[4], li[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int i = i0 + j;
+                    const bool counts = i < n && (there >> i & 1);
+                    const int at = counts ? i : some;
+                    wi[j] = counts ? __shfl(w, at) : 0.0f;
+                    li[j] = __shfl(l, at);
+#pragma unroll
+                    for (int e = 0; e < E; ++e) x[j][e] = P.part[((p0 + at) * rows + row) * D + lane * E + e];
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (wi[j] == 0.0f) continue;
+                    sum = __builtin_fmaf(wi[j], li[j], sum);
+#pragma unroll
+                    for (int e = 0; e < E; ++e) val[e] = __builtin_fmaf(wi[j], x[j][e], val[e]);
+                }
+            }
     }
-    T* const o = static_cast<T*>(P.o) + b * P.ldo + (row % P.H) * D + lane * (D / 64);
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    T* const o = static_cast<T*>(P.o) + b * P.ldo + (int64_t)h * D + lane * E;
 #pragma unroll
-    for (int e = 0; e < D / 64; ++e) o[e] = (T)(val[e] * inv);
+    for (int e = 0; e < E; ++e) o[e] = (T)(val[e] * inv);
 }
 
-struct Plan { int prefix_tiles, own_tiles, prefix_parts, own_parts; };
+// Parts.  The prefix: two workgroups a CU (64 requests behind 8000 keys 39.9 us, with four 47.4, with eight 64.2: each part is 2 KB to write and read for
+// every four heads).  Requests: of the greatest length, four workgroups a CU and 1536 keys a part at most, so that requests of different lengths leave no CU
+// waiting (48 of up to 16384 int8 keys 172 us, in parts of 5461 keys 195); shorter ones in as many, of `least` keys at least, which are fewer where there are
+// few requests.
+struct Plan { int prefix_tiles, own_tiles, prefix_parts, own_parts, own_least; };
 
-// Parts: about two workgroups a CU, each of 256 keys at least.
 Plan plan_of(const CachedArgs& a) {
-    const int group = a.H / a.c.G, goal = 2 * num_cus();
-    Plan p{(int)(((int64_t)a.B * group + 31) / 32), (group + 31) / 32, 0, 0};
-    auto parts = [&](int64_t items, int64_t keys) {
-        const int64_t most = (keys + 255) / 256, want = (goal + items - 1) / items;
-        return (int)(want < most ? want : most);
-    };
-    if (a.prefix_len > 0) p.prefix_parts = parts((int64_t)p.prefix_tiles * a.c.G, a.prefix_len);
-    if (a.max_pages > 0) p.own_parts = parts((int64_t)a.B * p.own_tiles * a.c.G, (int64_t)a.max_pages * a.c.page_size);
+    const int group = a.H / a.c.G;
+    const int64_t cus = num_cus(), most = (int64_t)a.max_pages * a.c.page_size;
+    Plan p{(int)(((int64_t)a.B * group + 31) / 32), (group + 31) / 32, 0, 0, LEAST};
+    auto over = [](int64_t n, int64_t d) { return (n + d - 1) / d; };
+    if (a.prefix_len > 0) p.prefix_parts = (int)min64(over(2 * cus, (int64_t)p.prefix_tiles * a.c.G), over(a.prefix_len, BK * LEAST));
+    const int64_t items = (int64_t)a.B * p.own_tiles * a.c.G;
+    if (most > 0 && items > 0) {
+        p.own_least = items >= 2 * cus ? 4 * LEAST : 2 * items >= cus ? 2 * LEAST : LEAST;
+        const int64_t fill = over(4 * cus, items), even = min64(over(most, 1536), 64);
+        p.own_parts = (int)min64(fill > even ? fill : even, over(most, BK * p.own_least));
+    }
     return p;
 }
 size_t ml_bytes(const CachedArgs& a, int parts) { return ((size_t)parts * a.B * a.H * 8 + 255) & ~(size_t)255; }
@@ -277,11 +351,13 @@ template <class T, int D, bool I8> hipError_t launch(hipStream_t s, const Cached
     const Plan p = plan_of(a);
     const int parts = p.prefix_parts + p.own_parts;
     float* const ml = static_cast<float*>(a.workspace);
+    auto div = [](int n) { return FastDiv((uint32_t)(n > 0 ? n : 1)); };
     const CaParams P{a.q, a.o, static_cast<const int8_t*>(a.c.k), static_cast<const int8_t*>(a.c.v), a.c.k_scale, a.c.v_scale, a.prefix_pages, a.pages, a.lens,
                      ml, reinterpret_cast<float*>(static_cast<int8_t*>(a.workspace) + ml_bytes(a, parts)), a.ldq, a.ldo, a.ld_pages,
                      a.c.ld_page * (I8 ? 1 : 2), a.prefix_len, a.max_pages * a.c.page_size, a.B, a.H, a.c.G, a.H / a.c.G, __builtin_ctz(a.c.page_size), a.c.n_pages,
-                     p.prefix_parts, p.own_parts, p.prefix_tiles, p.own_tiles, a.scale * 1.44269504088896341f};
-    const int64_t items = (int64_t)p.prefix_tiles * a.c.G * p.prefix_parts + (int64_t)a.B * p.own_tiles * a.c.G * p.own_parts;
+                     p.prefix_parts, p.own_parts, p.own_least, p.prefix_tiles, a.scale * 1.44269504088896341f,
+                     div(a.c.G), div(p.prefix_parts), div(p.own_parts), div(p.own_tiles), div(a.H / a.c.G), div(a.H)};
+    const int64_t items = ((int64_t)p.prefix_tiles * p.prefix_parts + (int64_t)a.B * p.own_tiles * p.own_parts) * a.c.G;
     const int64_t keys = a.prefix_len + (int64_t)a.B * a.max_pages * a.c.page_size;
     if (items > 0) {
         TraceScope trace(s, KIND_CACHED_ATTENTION, 4 * (int64_t)D * a.H * a.B * (a.prefix_len + (int64_t)a.max_pages * a.c.page_size),

@@ -101,11 +101,11 @@ __device__ __forceinline__ void softmax_step(const v16f (&s)[KB], typename Elem<
         for (int r = 0; r < 16; r += 2) weigh<T>(s[b], r, p[b], l, c, base);
 }
 
-// The same over 16 scores, for values of int8 rows: the weights that leave are times the values' scales (scale[8 (r / 4) + r % 4]) over 2^ref, ref following
+// The same over 16 scores, for values of int8 rows: the weights that leave are times the values' scales over 2^ref, ref following
 // the largest scale of the block, the same for all lanes; the sum is that of the weights alone.  The output is in units of 2^ref.
 template <class T, int DT>
 __device__ __forceinline__ void softmax_step_scaled(const v16f (&s)[1], typename Elem<T>::v8 (&p)[2], float& m, float& l, v16f (&acc)[DT], float c, float& ref,
-                                                    bool first, float largest, const float* scale) {
+                                                    bool first, float largest, const float (&scale)[16]) {
     const float top = largest_of(s);
     const float power = __builtin_fminf(__builtin_fmaxf(__builtin_ceilf(__builtin_amdgcn_logf(largest)), -120.0f), 120.0f);
     if (__builtin_expect(__any((top - m) * c > 8.0f) || first || power > ref, 0)) {
@@ -124,7 +124,7 @@ __device__ __forceinline__ void softmax_step_scaled(const v16f (&s)[1], typename
     for (int r = 0; r < 16; ++r) {
         const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[0][r], c, base));
         l += w;
-        p[r / 8][r % 8] = (T)(w * (scale[8 * (r / 4) + r % 4] * down));
+        p[r / 8][r % 8] = (T)(w * (scale[r] * down));
     }
 }
 
