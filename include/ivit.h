@@ -479,8 +479,9 @@ int ivit_gated_quant(void* stream, const void* x, int64_t ldx, int8_t* y, int64_
 
 /* ---- Attention over float rows: rotary positions, a paged cache, whole prompts, single tokens behind a shared prefix. --
  * For the models of the section above whose sequences are longer than ivit_attention takes, causal, or answered token by
- * token:  linear_scaled (q | k | v rows) -> cache_append (or rotary) -> prompt_attention, then per token cached_attention ->
- * gated_quant (IVIT_ACT_NONE, not gated) -> linear_scaled.
+ * token.  A prompt: linear_scaled (q | k | v rows) -> rotary (q and k, in place) -> cache_append -> prompt_attention; a token:
+ * linear_scaled -> cache_append (with its rotary positions) -> cached_attention; either -> gated_quant (IVIT_ACT_NONE, not
+ * gated) -> linear_scaled.
  *
  *  - Heads lie side by side in a row: head h owns elements h d .. (h + 1) d.  H query heads share G key heads, H a multiple of
  *    G: query head h reads key head h / (H / G).

@@ -65,8 +65,6 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void prompt_attention_kernel(PaPar
     const T* const kbase = static_cast<const T*>(P.k) + (int64_t)ka * P.ldk + (int64_t)(head / P.group) * D;
     const T* const vbase = static_cast<const T*>(P.v) + (int64_t)ka * P.ldv + (int64_t)(head / P.group) * D;
     // Load instruction i of a wavefront brings rows LR (RW i + rw) + lane / PC, physical piece lane % PC.
-    const int lr = LR * rw + lane / PC, lp = lane % PC;
-    const uint32_t ldk2 = (uint32_t)P.ldk * 2, ldv2 = (uint32_t)P.ldv * 2;
     int8_t* const ring = lds + g * 2 * STAGE;
     const uint32_t lds0 = lds_offset(ring) + 1024 * rw;
     // rounds with tiles of which not all queries of the workgroup see all keys
@@ -77,6 +75,7 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void prompt_attention_kernel(PaPar
         constexpr bool V = decltype(values)::value;
         const int kt = tiles - 1 - (n * KG + g);
         if (kt < 0) return;
+        const int lr = LR * rw + lane / PC, lp = lane % PC;
         const int64_t ld = V ? P.ldv : P.ldk;
         const int8_t* const p = uniform_ptr(reinterpret_cast<const int8_t*>((V ? vbase : kbase) + (int64_t)kt * BK * ld));
         const int last = nk - 1 - kt * BK;                                        // (rows behind the sequence: its last row again)
@@ -84,7 +83,7 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void prompt_attention_kernel(PaPar
 #pragma unroll
         for (int i = 0; i < LI; ++i) {
             const int r = LR * RW * i + lr;
-            dma16(p, (uint32_t)min(r, last) * (V ? ldv2 : ldk2) + 16 * (lp ^ (V ? mix_v<D>(r) : mix_k<D>(r))), to + i * 1024 * RW);
+            dma16(p, (uint32_t)min(r, last) * ((uint32_t)ld * 2) + 16 * (lp ^ (V ? mix_v<D>(r) : mix_k<D>(r))), to + i * 1024 * RW);
         }
     };
     constexpr std::false_type keys{};
@@ -201,7 +200,7 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void prompt_attention_kernel(PaPar
         for (int i = 0; i < DT; ++i)
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][r] *= f;
-#pragma unroll
+#pragma unroll 1
         for (int o = 1; o < KG; ++o, in += RW * 64 * (16 * DT + 2)) {
             const float h = in[0] == to ? 1.0f : __builtin_amdgcn_exp2f((in[0] - to) * P.c);
             l = __builtin_fmaf(h, in[64], l);
