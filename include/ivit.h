@@ -545,7 +545,7 @@ int ivit_cache_append(void* stream, const void* q, int64_t ldq, void* q_out, int
  * are fewer keys than queries, none).
  * q, o [n_q, H * d], k, v [n_k, G * d] of `type`; starts int32 [n_seq + 1] (device), not falling; a sequence that is not within the
  * rows is left out.  scale > 0 and finite.  No overlap.
- * Requirements: 0 <= n_q, n_k < 2^31, 0 <= n_seq < 2^20, H and G <= 4096, (n_q / 64 + n_seq) H < 2^24; ldk, ldv <= 2^24; leading dimensions and
+ * Requirements: 0 <= n_q, n_k < 2^31, 0 <= n_seq < 2^20, H and G <= 4096, (n_q / 64 + n_seq) H < 2^24; ldq, ldk, ldv <= 2^24; leading dimensions and
  * pointers of q, k, v, o whole 16 bytes.
  * Errors: NULL, SHAPE, PARAM (type, scale), ALIGN, HIP. */
 int ivit_prompt_attention(void* stream, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, void* o,

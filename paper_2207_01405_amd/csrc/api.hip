@@ -833,7 +833,7 @@ int ivit_prompt_attention(void* stream, const void* q, int64_t ldq, const void* 
     if ((type != IVIT_F16 && type != IVIT_BF16) || !std::isfinite(scale) || !(scale > 0.0f)) return IVIT_ERR_PARAM;
     if (n_q < 0 || n_q > 0x7fffffffLL || n_k < 0 || n_k > 0x7fffffffLL || n_seq < 0 || n_seq >= (1 << 20) || (d != 64 && d != 128)) return IVIT_ERR_SHAPE;
     if (H < 1 || H > 4096 || G < 1 || G > H || H % G || (!k_start && n_q != n_k) || (n_q / 64 + n_seq) * H >= (1 << 24)) return IVIT_ERR_SHAPE;
-    if (n_k > 0 && (ldk > (1 << 24) || ldv > (1 << 24))) return IVIT_ERR_SHAPE;
+    if (ldq > (1 << 24) || (n_k > 0 && (ldk > (1 << 24) || ldv > (1 << 24)))) return IVIT_ERR_SHAPE;
     if (n_q == 0 || n_seq == 0) return IVIT_OK;
     if (!q || !o || !q_start || (n_k > 0 && (!k || !v))) return IVIT_ERR_NULL;
     int st;

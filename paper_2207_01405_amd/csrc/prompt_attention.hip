@@ -22,17 +22,21 @@ struct PaParams {
 };
 
 // The sequence of tile slot x: sequence s has the slots q_start[s] / ROWS + s on, which are enough for its rows whatever they begin at.  64 places are
-// looked at at once.
-template <int ROWS> __device__ __forceinline__ int sequence_of(const int32_t* start, int n_seq, int x, int lane) {
+// looked at at once; with up to 64 sequences their bounds come with the same loads.
+struct Span { int seq, qa, qb, ka, kb; };
+template <int ROWS> __device__ __forceinline__ Span span_of(const int32_t* q_start, const int32_t* k_start, int n_seq, int x, int lane) {
     int lo = 0, n = n_seq;                                          // it is one of lo .. lo + n - 1
-    while (n > 1) {
+    while (n > 64) {
         const int step = (n + 63) / 64, s = lo + lane * step;
-        const bool behind = lane * step < n && (max(start[s], 0) / ROWS + s) <= x;
+        const bool behind = lane * step < n && (max(q_start[s], 0) / ROWS + s) <= x;
         const int at = 63 - __builtin_clzll(__ballot(behind) | 1);
         lo += at * step;
         n = min(step, n - at * step);
     }
-    return __builtin_amdgcn_readfirstlane(lo);
+    const int s = lo + min(lane, n - 1), qa = q_start[s], qb = q_start[s + 1], ka = k_start[s], kb = k_start[s + 1];
+    const int at = 63 - __builtin_clzll(__ballot(lane < n && max(qa, 0) / ROWS + s <= x) | 1);
+    return Span{__builtin_amdgcn_readfirstlane(lo + at), __builtin_amdgcn_readlane(qa, at), __builtin_amdgcn_readlane(qb, at), __builtin_amdgcn_readlane(ka, at),
+                __builtin_amdgcn_readlane(kb, at)};
 }
 
 // RW wavefronts of 32 rows, KG times: group g takes tiles g, g + KG, .. of BK keys, each group through LDS of its own, and the groups join what they have at
@@ -44,16 +48,19 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void prompt_attention_kernel(PaPar
     constexpr int PC = RB / 16, LR = 64 / PC;                                    // pieces of a row; rows of a load instruction
     static_assert(LI >= 1 && TILE % (1024 * RW) == 0, "whole load instructions");
     using V8 = typename Elem<T>::v8;
-    __shared__ __align__(16) int8_t lds[KG * 2 * STAGE];
-    static_assert(KG == 1 || KG * 2 * STAGE >= (KG - 1) * RW * 64 * 4 * (16 * DT + 2), "room for the groups' parts");
+    constexpr int ROWS_OF = 32 * RB, GROUP = 2 * STAGE;                          // bytes of a wavefront's queries or results; LDS of a group
+    static_assert(RW * ROWS_OF <= STAGE, "room for the queries");
+    constexpr int OUT = 64 * 4 * (16 * DT + 2);                                  // a wavefront's part on its way to another
+    __shared__ __align__(16) int8_t lds[KG * GROUP];
+    static_assert(KG == 1 || KG * GROUP >= (KG - 1) * RW * OUT, "room for the groups' parts");
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, li = lane & 31;
     const int rw = wv % RW, g = wv / RW;
 
     uint32_t hn;
     const int slot = P.slots - 1 - (int)P.heads.divide(blockIdx.x, hn);           // the last rows of a sequence, which see the most keys, come first
     const int head = P.by_xcd ? (int)(hn % NXCD) * (P.H / NXCD) + (int)hn / NXCD : (int)hn;
-    const int seq = sequence_of<ROWS>(P.q_start, P.n_seq, slot, lane);
-    const int qa = P.q_start[seq], qb = P.q_start[seq + 1], ka = P.k_start[seq], kb = P.k_start[seq + 1];
+    const Span span = span_of<ROWS>(P.q_start, P.k_start, P.n_seq, slot, lane);
+    const int seq = span.seq, qa = span.qa, qb = span.qb, ka = span.ka, kb = span.kb;
     const int tile = slot - (max(qa, 0) / ROWS + seq), nq = qb - qa, nk = kb - ka;
     if (qa < 0 || qb < qa || qb > P.n_q || ka < 0 || kb < ka || kb > P.n_k || tile < 0 || (int64_t)tile * ROWS >= nq) return;
     const int first = tile * ROWS, mine = first + 32 * rw;                        // first row of the workgroup and of the wavefront
@@ -65,7 +72,7 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void prompt_attention_kernel(PaPar
     const T* const kbase = static_cast<const T*>(P.k) + (int64_t)ka * P.ldk + (int64_t)(head / P.group) * D;
     const T* const vbase = static_cast<const T*>(P.v) + (int64_t)ka * P.ldv + (int64_t)(head / P.group) * D;
     // Load instruction i of a wavefront brings rows LR (RW i + rw) + lane / PC, physical piece lane % PC.
-    int8_t* const ring = lds + g * 2 * STAGE;
+    int8_t* const ring = lds + g * GROUP;
     const uint32_t lds0 = lds_offset(ring) + 1024 * rw;
     // rounds with tiles of which not all queries of the workgroup see all keys
     const int all_see = P.causal ? min(first + shift, nk - 1) : nk - 1;
@@ -88,17 +95,31 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void prompt_attention_kernel(PaPar
     };
     constexpr std::false_type keys{};
     constexpr std::true_type values{};
+
+    // The queries, B operand: query li, elements 16 s + 8 half on.  Their rows come whole through LDS, where the second tile will be: fragments straight from
+    // memory are 32 bytes of 32 rows an instruction, and every line is asked for four times (with that of the results 32 sequences of 512, 32 heads 143 -> 128 us,
+    // 32 of 128 29.0 -> 22.5).
+    const int row = min(mine + li, nq - 1), limit = P.causal ? min(row + shift, nk - 1) : nk - 1;      // the last key that the lane's query sees
+    const T* const qbase = static_cast<const T*>(P.q) + (int64_t)qa * P.ldq + (int64_t)head * D;
+    int8_t* const rows = ring + ((odd + 1) & 1) * STAGE + rw * ROWS_OF;
+    {
+        const int from = min(mine, nq - 1);
+        const int8_t* const p = uniform_ptr(reinterpret_cast<const int8_t*>(qbase + (int64_t)from * P.ldq));
+#pragma unroll
+        for (int i = 0; i < 32 / LR; ++i) {
+            const int r = LR * i + lane / PC;
+            dma16(p, (uint32_t)min(r, nq - 1 - from) * ((uint32_t)P.ldq * 2) + 16 * (lane % PC ^ mix_k<D>(r)), lds_offset(rows) + 1024 * i);
+        }
+    }
     if (rounds > 0) {
         issue(0, keys);
         issue(0, values);
     }
-
-    // the queries: B operand, query li, elements 16 s + 8 half on
+    if (KG == 1 && tiles > 0) asm volatile("s_waitcnt vmcnt(%0)" : : "n"(2 * LI) : "memory");
+    else wait_vm0();                                                              // (a group may be without a tile)
     V8 qf[DS];
-    const int row = min(mine + li, nq - 1), limit = P.causal ? min(row + shift, nk - 1) : nk - 1;      // the last key that the lane's query sees
-    const T* const qp = static_cast<const T*>(P.q) + (int64_t)(qa + row) * P.ldq + (int64_t)head * D;
 #pragma unroll
-    for (int s = 0; s < DS; ++s) qf[s] = *reinterpret_cast<const V8*>(qp + 16 * s + 8 * half);
+    for (int s = 0; s < DS; ++s) qf[s] = *reinterpret_cast<const V8*>(rows + li * RB + 16 * ((2 * s + half) ^ mix_k<D>(li)));
     v16f acc[DT];
     float m = -__builtin_inff(), l = 0.0f;
 #pragma unroll
@@ -143,7 +164,7 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void prompt_attention_kernel(PaPar
         // A key left out has the weight 0, and 0 times an infinite value or NaN is NaN: where these tiles, which come first, leave a value that is
         // not finite, they are done again, key by key, with those that count only.
         if (__builtin_expect(__any(not_finite<DT>(acc)), 0))
-            key_by_key<T, D>(qp, kbase, P.ldk, vbase, P.ldv, k0, limit, P.c, half, m, l, acc, [&](int j) { return (tiles - 1 - j / BK) % KG == g; });
+            key_by_key<T, D>(qbase + (int64_t)row * P.ldq, kbase, P.ldk, vbase, P.ldv, k0, limit, P.c, half, m, l, acc, [&](int j) { return (tiles - 1 - j / BK) % KG == g; });
     }
     // The tiles that all queries see.  Scores are formed a tile ahead of the values' product, so that its matrix instructions stand between the vector
     // instructions of the softmax.
@@ -179,7 +200,7 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void prompt_attention_kernel(PaPar
     l = add_halves(l);
     if constexpr (KG > 1) {                                                       // the other groups' parts to the first, a lane's to the same lane
         __syncthreads();
-        float* const out = reinterpret_cast<float*>(lds) + ((g - 1) * RW + rw) * 64 * (16 * DT + 2) + lane;
+        float* const out = reinterpret_cast<float*>(lds + ((g - 1) * RW + rw) * OUT) + lane;
         if (g > 0) {
             out[0] = m;
             out[64] = l;
@@ -190,10 +211,10 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void prompt_attention_kernel(PaPar
         }
         __syncthreads();
         if (g > 0) return;
-        const float* in = reinterpret_cast<const float*>(lds) + rw * 64 * (16 * DT + 2) + lane;
+        const float* in = reinterpret_cast<const float*>(lds + rw * OUT) + lane;
         float to = m;
 #pragma unroll
-        for (int o = 1; o < KG; ++o) to = __builtin_fmaxf(to, in[(o - 1) * RW * 64 * (16 * DT + 2)]);
+        for (int o = 1; o < KG; ++o) to = __builtin_fmaxf(to, in[(o - 1) * RW * OUT / 4]);
         const float f = m == to ? 1.0f : __builtin_amdgcn_exp2f((m - to) * P.c);
         l *= f;
 #pragma unroll
@@ -201,7 +222,7 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void prompt_attention_kernel(PaPar
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][r] *= f;
 #pragma unroll 1
-        for (int o = 1; o < KG; ++o, in += RW * 64 * (16 * DT + 2)) {
+        for (int o = 1; o < KG; ++o, in += RW * OUT / 4) {
             const float h = in[0] == to ? 1.0f : __builtin_amdgcn_exp2f((in[0] - to) * P.c);
             l = __builtin_fmaf(h, in[64], l);
 #pragma unroll
@@ -210,9 +231,24 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void prompt_attention_kernel(PaPar
                 for (int r = 0; r < 16; ++r) acc[i][r] = __builtin_fmaf(h, in[64 * (2 + 16 * i + r)], acc[i][r]);
         }
     }
-    if (mine + li >= nq) return;
+    // Results leave as whole rows, turned over in LDS of the wavefront's own: as they lie, a store instruction would write 16 bytes of 32 rows.
+    if constexpr (KG == 1) __syncthreads();
+    int8_t* const mine_l = lds + rw * (KG == 1 ? ROWS_OF : OUT);
     const float inv = l > 0.0f ? 1.0f / l : l != l ? l : 0.0f;
-    store_rows<T, DT>(static_cast<T*>(P.o) + (int64_t)(qa + mine + li) * P.ldo + (int64_t)head * D, acc, inv, half);
+    typedef T v4 __attribute__((ext_vector_type(4)));
+    typedef float v4f __attribute__((ext_vector_type(4)));
+#pragma unroll
+    for (int i = 0; i < DT; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            *reinterpret_cast<v4*>(mine_l + li * RB + 16 * ((4 * i + q) ^ mix_k<D>(li)) + 8 * half) =
+                __builtin_convertvector((v4f{acc[i][4 * q] * inv, acc[i][4 * q + 1] * inv, acc[i][4 * q + 2] * inv, acc[i][4 * q + 3] * inv}), v4);
+    T* const obase = static_cast<T*>(P.o) + (int64_t)(qa + mine) * P.ldo + (int64_t)head * D;
+#pragma unroll
+    for (int i = 0; i < 32 / LR; ++i) {
+        const int r = LR * i + lane / PC;
+        if (mine + r < nq) *reinterpret_cast<v4i*>(obase + r * P.ldo + 8 * (lane % PC ^ mix_k<D>(r))) = *reinterpret_cast<const v4i*>(mine_l + 1024 * i + 16 * lane);
+    }
 }
 
 template <class T, int D, int RW, int KG, int BK> hipError_t launch(hipStream_t s, const PromptArgs& a) {
@@ -225,13 +261,12 @@ template <class T, int D, int RW, int KG, int BK> hipError_t launch(hipStream_t 
 }
 // Where 128 rows a workgroup leave CUs without one (taking the sequences for equally long), the keys are shared out inside a workgroup: 500 queries after 7500
 // keys, 32 heads of 128, are 128 such workgroups, 128 us; two groups of 128 rows 106, four of 64 rows 88.  1000 after 7000: 140, 130, 155; 1500 after
-// 7000: 213, 226, 237.  Heads of 64 take tiles of 32 keys: 128 sequences of 197 25.8 us for 28.0 with 64, 8192 tokens 305 and 303.
+// 7000: 213, 226, 237.
 template <class T, int D> hipError_t choose(hipStream_t s, const PromptArgs& a) {
-    constexpr int BK = D == 128 ? 64 : 32;
     const int64_t blocks = (int64_t)a.n_seq * ((a.n_q + 128 * (int64_t)a.n_seq - 1) / (128 * (int64_t)a.n_seq)) * a.H, cus = num_cus();
     if (2 * blocks <= cus) return launch<T, D, 2, 4, 32>(s, a);
     if (blocks <= cus) return launch<T, D, 4, 2, 64>(s, a);
-    return launch<T, D, 4, 1, BK>(s, a);
+    return launch<T, D, 4, 1, 64>(s, a);
 }
 
 }  // namespace
