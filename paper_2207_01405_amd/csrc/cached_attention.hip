@@ -21,11 +21,12 @@ using namespace fatt;
 typedef float v4f __attribute__((ext_vector_type(4)));
 
 constexpr int W = 4, BK = 32, LEAST = 2 * W;   // wavefronts; keys of a block; blocks of the smallest part
+constexpr int WIDE = 32 * W, TK = 16 * W;      // rows of a workgroup that shares its keys, keys of its tiles
 
 struct CaParams {
     const void* q; void* o; const int8_t *k, *v; const float *ks, *vs; const int32_t *prefix_pages, *pages, *lens; float *ml, *part;
     int64_t ldq, ldo, ld_pages, ld_page;       // ld_page in bytes
-    int prefix_len, max_len, B, H, G, group, page_shift, n_pages, prefix_parts, own_parts, own_least, prefix_tiles; float c;
+    int prefix_len, max_len, B, H, G, group, page_shift, n_pages, prefix_parts, own_parts, own_least, prefix_tiles, wide; float c;
     FastDiv by_head, by_prefix_part, by_own_part, by_own_tile, by_group, by_heads;
 };
 
@@ -35,6 +36,8 @@ struct CaParams {
 template <int D, bool I8> struct CaTile {
     static constexpr int RB = I8 ? D : 2 * D, BYTES = BK * RB, S = I8 || D == 64 ? 2 : 1, STAGE = 2 * BYTES + (I8 ? 2 * 4 * BK : 0);
     static constexpr int OUT = 64 * 16 * (D / 32) * 4, WAVE = S * STAGE > OUT ? S * STAGE : OUT;
+    static constexpr int SHARED = 2 * TK * RB + (I8 ? W * 256 : 0);               // a tile of keys and values that the wavefronts share, two of them
+    static_assert(2 * SHARED <= W * WAVE, "room for two");
 };
 
 // 16-byte pieces of an int8 row: piece ^ mix8(row), for keys (8 bytes of 32 rows at a time) and values (8 bytes of 8 rows, twice) alike
@@ -57,6 +60,174 @@ template <class T> __device__ __forceinline__ typename Elem<T>::v8 spread(v2u b)
     return v;
 }
 
+// The page of a key by its number, as a scalar load.  (Kept 64 at a time in a vector register: no change.)
+__device__ __forceinline__ int page_at(const CaParams& P, const int32_t* table, int key) {
+    return min(max(((const int32_t __attribute__((address_space(4)))*)table)[key >> P.page_shift], 0), P.n_pages - 1);
+}
+
+// Fragments of 32 keys and of 16 keys' values (as transposed has them) from rows in LDS.
+template <class T, int D, bool I8> __device__ __forceinline__ typename Elem<T>::v8 key_frag(const int8_t* kl, int d, int li, int half) {
+    if constexpr (I8) return spread<T>(*reinterpret_cast<const v2u*>(kl + li * D + 16 * (d ^ mix8<D>(li)) + 8 * half));
+    else return *reinterpret_cast<const typename Elem<T>::v8*>(kl + li * 2 * D + 16 * ((2 * d + half) ^ mix_k<D>(li)));
+}
+template <class T, int D, bool I8> __device__ __forceinline__ typename Elem<T>::v8 value_frag(const int8_t* vl, int i, int lane) {
+    if constexpr (I8) {
+        // the transposing read of bytes takes 8 rows x 16 elements from 16 lanes: keys 4 half + 0 .. 3 and + 8 .. 11
+        typedef v2i __attribute__((address_space(3)))* at;
+        const int j = (lane & 15) >> 1, row = 4 * (lane >> 5) + (j & 3) + 8 * (j >> 2), col = 32 * i + 16 * ((lane >> 4) & 1) + 8 * (lane & 1);
+        return spread<T>(__builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr8_b64_v2i32((at)(vl + row * D + 16 * ((col >> 4) ^ mix8<D>(row)) + (col & 15)))));
+    } else {
+        return transposed<T, D>(vl + transposed_at<D>(i, lane));
+    }
+}
+
+// The prefix for more than 64 query rows: a wavefront has 32 rows of its own, and all share tiles of 64 keys, of which each brings 16.  Scores are formed
+// a tile ahead of the values' product.
+template <class T, int D, bool I8, class RowOf>
+__device__ __forceinline__ void shared_keys(const CaParams& P, int8_t* lds, int g, int first, int k0, int k1, int part, RowOf&& row_of) {
+    using TL = CaTile<D, I8>;
+    using V8 = typename Elem<T>::v8;
+    constexpr int RB = TL::RB, DS = D / 16, DT = D / 32, PC = RB / 16, LR = 64 / PC, LI = 16 / LR, KB = TK / 32;
+    const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, li = lane & 31;
+    const int rows = P.B * P.group, last = k1 - 1, tiles = (k1 - k0 + TK - 1) / TK, mask = (1 << P.page_shift) - 1;
+    const uint32_t lds0 = lds_offset(lds);
+    auto issue = [&](int n, auto values) __attribute__((always_inline)) {
+        constexpr bool V = decltype(values)::value;
+        if (n >= tiles) return;
+        const int from = k0 + n * TK + 16 * wv, page = page_at(P, P.prefix_pages, min(from, last));
+        const int8_t* const p = uniform_ptr((V ? P.v : P.k) + (int64_t)page * P.ld_page + ((int64_t)g << P.page_shift) * RB);
+        const uint32_t to = lds0 + (n & 1) * TL::SHARED + (V ? TK * RB : 0) + 16 * RB * wv;
+#pragma unroll
+        for (int i = 0; i < LI; ++i) {
+            const int r = LR * i + lane / PC, slot = min(from + r, last) & mask;
+            const int mix = I8 ? mix8<D>(r) : V ? mix_v<D>(r) : mix_k<D>(r);
+            dma16(p, slot * RB + 16 * ((lane % PC) ^ mix), to + i * 1024);
+        }
+        if constexpr (I8) {                                // the scales of the 16 keys, and 64 bytes behind them, of the values
+            const int64_t slots = ((int64_t)page * P.G + g) << P.page_shift;
+            if (lane < 16) dma4_at((V ? P.vs : P.ks) + slots + (min(from + lane, last) & mask), lds0 + (n & 1) * TL::SHARED + 2 * TK * RB + 256 * wv + (V ? 64 : 0));
+        }
+    };
+    constexpr std::false_type keys{};
+    constexpr std::true_type values{};
+    issue(0, keys);
+    issue(0, values);
+    const int mine = first + 32 * wv;
+    V8 qf[DS];
+    {
+        int rb, rh;
+        row_of(min(mine + li, rows - 1), rb, rh);
+        const T* const qp = static_cast<const T*>(P.q) + (int64_t)rb * P.ldq + (int64_t)rh * D + 8 * half;
+#pragma unroll
+        for (int s = 0; s < DS; ++s) qf[s] = *reinterpret_cast<const V8*>(qp + 16 * s);
+    }
+    v16f acc[DT];
+    float m = -__builtin_inff(), l = 0.0f, ref = 0.0f;
+#pragma unroll
+    for (int i = 0; i < DT; ++i) acc[i] = v16f{};
+    auto scale_at = [&](int buf, int b, int r) __attribute__((always_inline)) {        // of the keys; 16 further on: of the values
+        return lds + buf * TL::SHARED + 2 * TK * RB + 256 * (2 * b + r / 8) + 4 * (8 * (r / 4 % 2) + 4 * half + r % 4);
+    };
+    auto scores = [&](int n, int buf, v16f (&s)[KB]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int d = 0; d < DS; ++d)
+#pragma unroll
+            for (int b = 0; b < KB; ++b) s[b] = mfma(key_frag<T, D, I8>(lds + buf * TL::SHARED + 32 * b * RB, d, li, half), qf[d], d ? s[b] : v16f{});
+    };
+    auto finish = [&](int n, int buf, v16f (&s)[KB]) __attribute__((always_inline)) {  // scales, and keys behind the last one
+        if constexpr (I8) {
+#pragma unroll
+            for (int b = 0; b < KB; ++b)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[b][r] *= *reinterpret_cast<const float*>(scale_at(buf, b, r));
+        }
+        const int left = last - k0 - n * TK;
+        if (left < TK - 1) {
+#pragma unroll
+            for (int b = 0; b < KB; ++b)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (32 * b + 8 * (r / 4) + r % 4 > left - 4 * half) s[b][r] = -__builtin_inff();
+        }
+    };
+    arrive<0>();
+    issue(1, keys);
+    v16f even_s[KB], odd_s[KB];
+    scores(0, 0, even_s);
+    finish(0, 0, even_s);
+    auto step = [&](int n, int buf, v16f (&s)[KB], v16f (&next)[KB]) __attribute__((always_inline)) {
+        arrive<0>();
+        issue(n + 2, keys);
+        issue(n + 1, values);
+        V8 p[KB][2];
+        if constexpr (I8) {
+#pragma unroll
+            for (int b = 0; b < KB; ++b) {
+                v16f one[1] = {s[b]};
+                float vs[16], top = 0.0f;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    vs[r] = *reinterpret_cast<const float*>(scale_at(buf, b, r) + 64);
+                    top = __builtin_fmaxf(top, vs[r]);
+                }
+                softmax_step_scaled<T, DT>(one, p[b], m, l, acc, P.c, ref, n == 0 && b == 0, max_halves(top), vs);
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int i = 0; i < DT; ++i) acc[i] = mfma(value_frag<T, D, I8>(lds + buf * TL::SHARED + (TK + 32 * b + 16 * t) * RB, i, lane), p[b][t], acc[i]);
+            }
+            scores(n + 1, buf ^ 1, next);                  // (of the last tile: of what that buffer holds, not used)
+        } else {
+            move_largest<DT>(largest_of(s), m, l, acc, P.c);
+            const float base = base_of<T>(m, P.c);
+            scores(n + 1, buf ^ 1, next);
+#pragma unroll
+            for (int b = 0; b < KB; ++b)
+#pragma unroll
+                for (int r = 0; r < 16; r += 2) weigh<T>(s[b], r, p[b], l, P.c, base);
+#pragma unroll
+            for (int t = 0; t < 2 * KB; ++t)
+#pragma unroll
+                for (int i = 0; i < DT; ++i) acc[i] = mfma(value_frag<T, D, I8>(lds + buf * TL::SHARED + (TK + 16 * t) * RB, i, lane), p[t / 2][t % 2], acc[i]);
+        }
+        finish(n + 1, buf ^ 1, next);
+    };
+#pragma unroll 1
+    for (int n = 0; n < tiles; n += 2) {
+        step(n, 0, even_s, odd_s);
+        if (n + 1 < tiles) step(n + 1, 1, odd_s, even_s);
+    }
+    l = add_halves(l);
+    // results as whole lines: a lane's registers into LDS of the wavefront's own, and out of it 4 elements of row lane / 8 + 8 n at 4 (lane % 8)
+    __syncthreads();
+    float* const out = reinterpret_cast<float*>(lds + wv * TL::WAVE);
+    const float up = I8 ? __builtin_amdgcn_exp2f(ref) : 1.0f;
+#pragma unroll
+    for (int i = 0; i < DT; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) out[64 * (16 * i + r) + lane] = acc[i][r] * up;
+    int rb, rh;
+    if (half == 0 && mine + li < rows) {
+        row_of(mine + li, rb, rh);
+        const int64_t at = (int64_t)part * P.B * P.H + (int64_t)rb * P.H + rh;
+        P.ml[2 * at] = m;
+        P.ml[2 * at + 1] = l;
+    }
+    const int q = lane % 8;
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+        const int r = lane / 8 + 8 * n;
+        if (mine + r >= rows) continue;
+        row_of(mine + r, rb, rh);
+        float* const to = P.part + ((int64_t)part * P.B * P.H + (int64_t)rb * P.H + rh) * D + 4 * q;
+#pragma unroll
+        for (int i = 0; i < DT; ++i) {
+            const float* const x = out + 64 * (16 * i + 4 * (q / 2)) + r + 32 * (q % 2);
+            *reinterpret_cast<v4f*>(to + 32 * i) = v4f{x[0], x[64], x[128], x[192]};
+        }
+    }
+}
+
 template <class T, int D, bool I8>
 __global__ __launch_bounds__(64 * W, 2) void cached_attention_kernel(CaParams P) {
     using TL = CaTile<D, I8>;
@@ -74,7 +245,7 @@ __global__ __launch_bounds__(64 * W, 2) void cached_attention_kernel(CaParams P)
     const bool prefix = item < prefix_items;
     const int32_t* table;
     if (prefix) {
-        r0 = 32 * (int)P.by_prefix_part.divide(item, part_);
+        r0 = (P.wide ? WIDE : 32) * (int)P.by_prefix_part.divide(item, part_);
         rows = P.B * P.group;
         len = P.prefix_len; parts = P.prefix_parts; table = P.prefix_pages;
     } else {
@@ -94,10 +265,10 @@ __global__ __launch_bounds__(64 * W, 2) void cached_attention_kernel(CaParams P)
         rb = prefix ? (int)P.by_group.divide(rest, rest) : b;
         rh = g * P.group + (int)rest;
     };
-    if (b0 == b1 && all_parts > 1) {                       // no keys here
+    if (b0 == b1 && (all_parts > 1 || P.wide)) {           // no keys here
         int rb, rh;
         row_of(tid, rb, rh);
-        if (tid < 32 && r0 + tid < rows) {
+        if (tid < (P.wide ? WIDE : 32) && r0 + tid < rows) {
             const int64_t at = (int64_t)out_part * P.B * P.H + (int64_t)rb * P.H + rh;
             P.ml[2 * at] = -__builtin_inff();
             P.ml[2 * at + 1] = 0.0f;
@@ -105,18 +276,22 @@ __global__ __launch_bounds__(64 * W, 2) void cached_attention_kernel(CaParams P)
         return;
     }
 
+    if (prefix && P.wide) {
+        shared_keys<T, D, I8>(P, lds, g, r0, b0 * BK, min(b1 * BK, len), part, [&](int r, int& rb, int& rh) __attribute__((always_inline)) { row_of(r - r0, rb, rh); });
+        return;
+    }
+
     // loads: instruction i brings rows LR i + lane / PC, physical piece lane % PC
     int8_t* const mine = lds + wv * TL::WAVE;
     const uint32_t lds0 = lds_offset(mine);
     const int mask = (1 << P.page_shift) - 1, lr = lane / PC, lp = lane % PC;
-    typedef const int32_t __attribute__((address_space(4)))* scalar_table;
     auto issue = [&](int blk, int buf, auto values) __attribute__((always_inline)) {
         constexpr bool V = decltype(values)::value;
         const int k0 = blk * BK, last = len - 1;
         int page[2];
 #pragma unroll
         for (int a = 0; a < 2; ++a)                        // 16 keys lie in one page (behind the last key: that one again)
-            page[a] = min(max(((scalar_table)table)[min(k0 + 16 * a, last) >> P.page_shift], 0), P.n_pages - 1);
+            page[a] = page_at(P, table, min(k0 + 16 * a, last));
 #pragma unroll
         for (int a = 0; a < 2; ++a) {
             const int8_t* const p = uniform_ptr((V ? P.v : P.k) + (int64_t)page[a] * P.ld_page + ((int64_t)g << P.page_shift) * RB);
@@ -169,10 +344,7 @@ __global__ __launch_bounds__(64 * W, 2) void cached_attention_kernel(CaParams P)
         v16f s[1] = {v16f{}};
 #pragma unroll
         for (int d = 0; d < DS; ++d) {
-            V8 kf;
-            if constexpr (I8) kf = spread<T>(*reinterpret_cast<const v2u*>(kl + li * RB + 16 * (d ^ mix8<D>(li)) + 8 * half));
-            else kf = *reinterpret_cast<const V8*>(kl + li * RB + 16 * ((2 * d + half) ^ mix_k<D>(li)));
-            s[0] = mfma(kf, qf[d], s[0]);
+            s[0] = mfma(key_frag<T, D, I8>(kl, d, li, half), qf[d], s[0]);
         }
         float ks[16], vs[16], top_scale = 0.0f;
         if constexpr (I8) {
@@ -210,18 +382,7 @@ __global__ __launch_bounds__(64 * W, 2) void cached_attention_kernel(CaParams P)
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int i = 0; i < DT; ++i) {
-                V8 vf;
-                if constexpr (I8) {
-                    // the transposing read of bytes takes 8 rows x 16 elements from 16 lanes: keys 16 t + 4 half + 0 .. 3 and + 8 .. 11
-                    typedef v2i __attribute__((address_space(3)))* at;
-                    const int j = (lane & 15) >> 1, row = 16 * t + 4 * half + (j & 3) + 8 * (j >> 2), col = 32 * i + 16 * ((lane >> 4) & 1) + 8 * (lane & 1);
-                    vf = spread<T>(__builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr8_b64_v2i32((at)(vl + row * RB + 16 * ((col >> 4) ^ mix8<D>(row)) + (col & 15)))));
-                } else {
-                    vf = transposed<T, D>(vl + transposed_at<D>(i, lane) + 16 * t * RB);
-                }
-                acc[i] = mfma(vf, p[0][t], acc[i]);
-            }
+            for (int i = 0; i < DT; ++i) acc[i] = mfma(value_frag<T, D, I8>(vl + 16 * t * RB, i, lane), p[0][t], acc[i]);
         wait_lds();
         if (n + S < own) issue(block(n + S), buf, values);
     }
@@ -329,14 +490,16 @@ template <class T, int D> __global__ __launch_bounds__(256) void join_kernel(CaP
 // every four heads).  Requests: of the greatest length, four workgroups a CU and 1536 keys a part at most, so that requests of different lengths leave no CU
 // waiting (48 of up to 16384 int8 keys 172 us, in parts of 5461 keys 195); shorter ones in as many, of `least` keys at least, which are fewer where there are
 // few requests.
-struct Plan { int prefix_tiles, own_tiles, prefix_parts, own_parts, own_least; };
+struct Plan { int prefix_tiles, own_tiles, prefix_parts, own_parts, own_least; bool wide; };
 
 Plan plan_of(const CachedArgs& a) {
     const int group = a.H / a.c.G;
     const int64_t cus = num_cus(), most = (int64_t)a.max_pages * a.c.page_size;
-    Plan p{(int)(((int64_t)a.B * group + 31) / 32), (group + 31) / 32, 0, 0, LEAST};
     auto over = [](int64_t n, int64_t d) { return (n + d - 1) / d; };
-    if (a.prefix_len > 0) p.prefix_parts = (int)min64(over(2 * cus, (int64_t)p.prefix_tiles * a.c.G), over(a.prefix_len, BK * LEAST));
+    const int64_t rows = (int64_t)a.B * group;
+    Plan p{0, (group + 31) / 32, 0, 0, LEAST, rows > 64};
+    p.prefix_tiles = (int)over(rows, p.wide ? WIDE : 32);
+    if (a.prefix_len > 0) p.prefix_parts = (int)min64(over(2 * cus, (int64_t)p.prefix_tiles * a.c.G), over(a.prefix_len, (p.wide ? 2 : 1) * BK * LEAST));
     const int64_t items = (int64_t)a.B * p.own_tiles * a.c.G;
     if (most > 0 && items > 0) {
         p.own_least = items >= 2 * cus ? 4 * LEAST : 2 * items >= cus ? 2 * LEAST : LEAST;
@@ -355,7 +518,7 @@ template <class T, int D, bool I8> hipError_t launch(hipStream_t s, const Cached
     const CaParams P{a.q, a.o, static_cast<const int8_t*>(a.c.k), static_cast<const int8_t*>(a.c.v), a.c.k_scale, a.c.v_scale, a.prefix_pages, a.pages, a.lens,
                      ml, reinterpret_cast<float*>(static_cast<int8_t*>(a.workspace) + ml_bytes(a, parts)), a.ldq, a.ldo, a.ld_pages,
                      a.c.ld_page * (I8 ? 1 : 2), a.prefix_len, a.max_pages * a.c.page_size, a.B, a.H, a.c.G, a.H / a.c.G, __builtin_ctz(a.c.page_size), a.c.n_pages,
-                     p.prefix_parts, p.own_parts, p.own_least, p.prefix_tiles, a.scale * 1.44269504088896341f,
+                     p.prefix_parts, p.own_parts, p.own_least, p.prefix_tiles, p.wide, a.scale * 1.44269504088896341f,
                      div(a.c.G), div(p.prefix_parts), div(p.own_parts), div(p.own_tiles), div(a.H / a.c.G), div(a.H)};
     const int64_t items = ((int64_t)p.prefix_tiles * p.prefix_parts + (int64_t)a.B * p.own_tiles * p.own_parts) * a.c.G;
     const int64_t keys = a.prefix_len + (int64_t)a.B * a.max_pages * a.c.page_size;
@@ -366,7 +529,7 @@ template <class T, int D, bool I8> hipError_t launch(hipStream_t s, const Cached
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    if (parts == 1) return hipSuccess;
+    if (parts == 1 && !(p.wide && p.prefix_parts)) return hipSuccess;
     TraceScope trace(s, KIND_CACHED_JOIN, 0, (int64_t)a.B * a.H * (parts * (4 * (int64_t)D + 8) + 2 * D));
     join_kernel<T, D><<<dim3((unsigned)(((int64_t)a.B * a.H + 3) / 4)), 256, 0, s>>>(P, parts);
     return hipGetLastError();

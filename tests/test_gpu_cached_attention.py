@@ -39,8 +39,9 @@ class Setup:
         if garbage is not None:                              # slots that hold no key
             used = torch.zeros(pages, page, dtype=torch.bool, device="cuda")
             for tb, n in [(self.prefix_pages, prefix)] + [(self.pages[b], n) for b, n in enumerate(lens)]:
-                for i in range(max(n, 0)):
-                    used[int(tb[i // page]), i % page] = True
+                if n > 0:
+                    at = torch.arange(n, device="cuda")
+                    used[tb[at // page].long(), at % page] = True
             for n in "kv":
                 at = (~used)[:, None, :, None].expand(shape)
                 if i8:
@@ -140,6 +141,46 @@ def test_long(ivit, t):
             s = Setup(5, [9000, 4000, 1], 5000, 16, 4, d, t, i8, 64)
             s.call(ivit)
             s.compare("long", mean=not i8)
+
+
+# more than 64 query rows of a head: workgroups of 128 rows that share tiles of 64 keys of the prefix
+@pytest.mark.parametrize("B,H,G", [(65, 1, 1), (33, 4, 2), (17, 8, 2), (40, 32, 4), (130, 6, 6), (3, 200, 2)])
+@pytest.mark.parametrize("i8", [False, True])
+def test_prefix_of_many_rows(ivit, B, H, G, i8):
+    import torch
+    for d, t, page in ((64, "bf16", 16), (128, "f16", 32), (128, "bf16", 256)):
+        for prefix in (1, 63, 64, 65, 200, 1024, 3000):
+            if prefix > 200 and H * B > 600 and d == 64:
+                continue
+            lens = [(7 * b) % 90 - 1 for b in range(B)]
+            s = Setup(prefix + B, lens, prefix, H, G, d, t, i8, page, garbage=float("nan"))
+            first = s.call(ivit).clone()
+            if prefix in (65, 1024):
+                s.compare("wide")
+            else:                                           # a few requests stand for the others
+                for b in (0, 1, B // 2, B - 1):
+                    k, v = s.keys(b, 0)
+                    if lens[b] < 0:
+                        assert bool((s.o[b] == 5).all())
+                        continue
+                    group = H // G
+                    want, pv, err, _ = attend64(s.q[b, :group * d].double().reshape(group, d), k, v, d ** -0.5)
+                    check(s.o[b, :group * d].reshape(group, d), want, pv, err, k.shape[0], t, float(v.abs().max()), "request %d of %d behind %d" % (b, B, prefix),
+                          scaled=4 * U)
+            for _ in range(3):
+                assert torch.equal(first, s.call(ivit)), "equal calls"
+
+
+def test_prefix_alone(ivit):
+    """No keys of their own, and no pages for any: the prefix is all."""
+    import torch
+    for B, H, G in ((2, 4, 2), (70, 2, 1), (300, 4, 2)):
+        for i8 in (False, True):
+            for prefix in (5, 500):
+                s = Setup(B, [0] * (B - 1) + [-1], prefix, H, G, 128, "bf16", i8, 32)
+                s.call(ivit)
+                s.compare("no keys of their own")
+                assert s.pages.shape[1] == 0
 
 
 @pytest.mark.parametrize("bad", [float("nan"), float("inf")])
