@@ -750,10 +750,11 @@ def cache_struct(c, device, where="cache_struct"):
         raise ValueError("%s: a cache of %s, %s on %s and %s, %s on %s, wanted two [pages, heads, page_size, head_dim] of one type on device %d" % (
             where, tuple(shape), k.dtype, k.device, tuple(v.shape), v.dtype, v.device, device))
     pages, heads, page, d = shape
-    inner = (page * d, d, 1)
-    ld = k.stride(0) if pages > 1 else heads * page * d
-    if k.stride()[1:] != inner or v.stride()[1:] != inner or (pages > 1 and v.stride(0) != ld):
-        raise ValueError("%s: pages of the cache have to be dense, and those of k and v one stride apart: %s and %s" % (where, k.stride(), v.stride()))
+    ld = heads * page * d
+    if not (k.is_contiguous() and v.is_contiguous()):
+        ld = k.stride(0) if pages > 1 else ld
+        if not (k.stride()[1:] == v.stride()[1:] == (page * d, d, 1) and (pages == 1 or v.stride(0) == ld)):
+            raise ValueError("%s: pages of the cache have to be dense, and those of k and v one stride apart: %s and %s" % (where, k.stride(), v.stride()))
     scales = [None, None]
     if kind == 3:
         scales = [_vector(c[n], pages * heads * page, device, where) for n in ("k_scale", "v_scale")]

@@ -7,8 +7,10 @@
 // turn, each through LDS of its own without a barrier, and join what they have at the end.  The parts of a row, its largest score, sum and unscaled
 // output each, are joined by a second launch, in a fixed order.
 //
-// int8 rows come into LDS as they are and are spread to 16 bits on the way to the matrix cores, where whole numbers up to 127 are exact.  The keys' scales
-// go to the scores, the values' to the weights.
+// int8 rows come into LDS as they are and are spread to float16 on the way to the matrix cores, where whole numbers up to 128 are exact: an instruction and a
+// quarter an element, which bounds these caches (to bfloat16, which has no place for eight bits under a leading one, they were three, and 48 requests of 8192 keys took
+// 177 us for 163).  bfloat16 queries become float16 with a power of two of their own, which their scores get back.  The keys' scales go to the
+// scores, the values' to the weights.
 #include "regst_common.hpp"
 #include "float_attention.hpp"
 
@@ -53,11 +55,42 @@ __device__ __forceinline__ void dma4_at(const float* p, uint32_t dst) {
                  : : "s"(__builtin_amdgcn_readfirstlane(dst)), "v"(p) : "memory", "m0");
 }
 
-template <class T> __device__ __forceinline__ typename Elem<T>::v8 spread(v2u b) {
-    typename Elem<T>::v8 v;
+// Eight int8 numbers as float16: 128 + q in the low bits of 1024 is 1152 + q.
+__device__ __forceinline__ Elem<_Float16>::v8 spread(v2u b) {
+    const uint32_t x = b[0] ^ 0x80808080u, y = b[1] ^ 0x80808080u, up = 0x64646464u;
+    const v4u w = {__builtin_amdgcn_perm(up, x, 0x04010400u), __builtin_amdgcn_perm(up, x, 0x04030402u), __builtin_amdgcn_perm(up, y, 0x04010400u),
+                   __builtin_amdgcn_perm(up, y, 0x04030402u)};
+    return __builtin_bit_cast(Elem<_Float16>::v8, w) - (_Float16)1152.0f;
+}
+
+// What the matrix cores multiply: the rows' type, float16 where the cache is int8.
+template <class T, bool I8> using Mul = std::conditional_t<I8, _Float16, T>;
+
+// A lane's half of a query row, elements 16 s + 8 half on, as fragments; those of an int8 cache's bfloat16 queries over 2^e, e that of the row's largest: what is
+// below 2^-14 of it keeps 24 bits below it.  Returns 2^e.
+template <class T, bool I8, int DS> __device__ __forceinline__ float query(const T* q, typename Elem<Mul<T, I8>>::v8 (&qf)[DS]) {
+    if constexpr (!I8 || __is_same(T, _Float16)) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = (T)(float)(int8_t)(b[e / 4] >> (8 * (e % 4)));
-    return v;
+        for (int s = 0; s < DS; ++s) qf[s] = *reinterpret_cast<const typename Elem<T>::v8*>(q + 16 * s);
+        return 1.0f;
+    } else {
+        typename Elem<T>::v8 x[DS];
+        float top = 0.0f;
+#pragma unroll
+        for (int s = 0; s < DS; ++s) {
+            x[s] = *reinterpret_cast<const typename Elem<T>::v8*>(q + 16 * s);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = __builtin_fmaxf(top, __builtin_fabsf((float)x[s][e]));
+        }
+        top = max_halves(top);
+        const int e = top > 0.0f && top < 0x1p126f ? __builtin_amdgcn_frexp_expf(top) : top > 0.0f ? 120 : 0;
+        const float down = __builtin_amdgcn_ldexpf(1.0f, -e);
+#pragma unroll
+        for (int s = 0; s < DS; ++s)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) qf[s][i] = (_Float16)((float)x[s][i] * down);
+        return __builtin_amdgcn_ldexpf(1.0f, e);
+    }
 }
 
 // The page of a key by its number, as a scalar load.  (Kept 64 at a time in a vector register: no change.)
@@ -66,16 +99,16 @@ __device__ __forceinline__ int page_at(const CaParams& P, const int32_t* table, 
 }
 
 // Fragments of 32 keys and of 16 keys' values (as transposed has them) from rows in LDS.
-template <class T, int D, bool I8> __device__ __forceinline__ typename Elem<T>::v8 key_frag(const int8_t* kl, int d, int li, int half) {
-    if constexpr (I8) return spread<T>(*reinterpret_cast<const v2u*>(kl + li * D + 16 * (d ^ mix8<D>(li)) + 8 * half));
+template <class T, int D, bool I8> __device__ __forceinline__ typename Elem<Mul<T, I8>>::v8 key_frag(const int8_t* kl, int d, int li, int half) {
+    if constexpr (I8) return spread(*reinterpret_cast<const v2u*>(kl + li * D + 16 * (d ^ mix8<D>(li)) + 8 * half));
     else return *reinterpret_cast<const typename Elem<T>::v8*>(kl + li * 2 * D + 16 * ((2 * d + half) ^ mix_k<D>(li)));
 }
-template <class T, int D, bool I8> __device__ __forceinline__ typename Elem<T>::v8 value_frag(const int8_t* vl, int i, int lane) {
+template <class T, int D, bool I8> __device__ __forceinline__ typename Elem<Mul<T, I8>>::v8 value_frag(const int8_t* vl, int i, int lane) {
     if constexpr (I8) {
         // the transposing read of bytes takes 8 rows x 16 elements from 16 lanes: keys 4 half + 0 .. 3 and + 8 .. 11
         typedef v2i __attribute__((address_space(3)))* at;
         const int j = (lane & 15) >> 1, row = 4 * (lane >> 5) + (j & 3) + 8 * (j >> 2), col = 32 * i + 16 * ((lane >> 4) & 1) + 8 * (lane & 1);
-        return spread<T>(__builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr8_b64_v2i32((at)(vl + row * D + 16 * ((col >> 4) ^ mix8<D>(row)) + (col & 15)))));
+        return spread(__builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr8_b64_v2i32((at)(vl + row * D + 16 * ((col >> 4) ^ mix8<D>(row)) + (col & 15)))));
     } else {
         return transposed<T, D>(vl + transposed_at<D>(i, lane));
     }
@@ -86,7 +119,7 @@ template <class T, int D, bool I8> __device__ __forceinline__ typename Elem<T>::
 template <class T, int D, bool I8, class RowOf>
 __device__ __forceinline__ void shared_keys(const CaParams& P, int8_t* lds, int g, int first, int k0, int k1, int part, RowOf&& row_of) {
     using TL = CaTile<D, I8>;
-    using V8 = typename Elem<T>::v8;
+    using V8 = typename Elem<Mul<T, I8>>::v8;
     constexpr int RB = TL::RB, DS = D / 16, DT = D / 32, PC = RB / 16, LR = 64 / PC, LI = 16 / LR, KB = TK / 32;
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, li = lane & 31;
     const int rows = P.B * P.group, last = k1 - 1, tiles = (k1 - k0 + TK - 1) / TK, mask = (1 << P.page_shift) - 1;
@@ -114,12 +147,11 @@ __device__ __forceinline__ void shared_keys(const CaParams& P, int8_t* lds, int 
     issue(0, values);
     const int mine = first + 32 * wv;
     V8 qf[DS];
+    float unit;                                            // of the scores, and of m up to the end
     {
         int rb, rh;
         row_of(min(mine + li, rows - 1), rb, rh);
-        const T* const qp = static_cast<const T*>(P.q) + (int64_t)rb * P.ldq + (int64_t)rh * D + 8 * half;
-#pragma unroll
-        for (int s = 0; s < DS; ++s) qf[s] = *reinterpret_cast<const V8*>(qp + 16 * s);
+        unit = query<T, I8>(static_cast<const T*>(P.q) + (int64_t)rb * P.ldq + (int64_t)rh * D + 8 * half, qf);
     }
     v16f acc[DT];
     float m = -__builtin_inff(), l = 0.0f, ref = 0.0f;
@@ -164,13 +196,10 @@ __device__ __forceinline__ void shared_keys(const CaParams& P, int8_t* lds, int 
 #pragma unroll
             for (int b = 0; b < KB; ++b) {
                 v16f one[1] = {s[b]};
-                float vs[16], top = 0.0f;
+                float vs[16];
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    vs[r] = *reinterpret_cast<const float*>(scale_at(buf, b, r) + 64);
-                    top = __builtin_fmaxf(top, vs[r]);
-                }
-                softmax_step_scaled<T, DT>(one, p[b], m, l, acc, P.c, ref, n == 0 && b == 0, max_halves(top), vs);
+                for (int r = 0; r < 16; ++r) vs[r] = *reinterpret_cast<const float*>(scale_at(buf, b, r) + 64);
+                softmax_step_scaled<DT>(one, p[b], m, l, acc, P.c * unit, ref, n == 0 && b == 0, vs);
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -198,6 +227,7 @@ __device__ __forceinline__ void shared_keys(const CaParams& P, int8_t* lds, int 
         if (n + 1 < tiles) step(n + 1, 1, odd_s, even_s);
     }
     l = add_halves(l);
+    m *= unit;
     // results as whole lines: a lane's registers into LDS of the wavefront's own, and out of it 4 elements of row lane / 8 + 8 n at 4 (lane % 8)
     __syncthreads();
     float* const out = reinterpret_cast<float*>(lds + wv * TL::WAVE);
@@ -231,7 +261,7 @@ __device__ __forceinline__ void shared_keys(const CaParams& P, int8_t* lds, int 
 template <class T, int D, bool I8>
 __global__ __launch_bounds__(64 * W, 2) void cached_attention_kernel(CaParams P) {
     using TL = CaTile<D, I8>;
-    using V8 = typename Elem<T>::v8;
+    using V8 = typename Elem<Mul<T, I8>>::v8;
     constexpr int RB = TL::RB, S = TL::S, DS = D / 16, DT = D / 32, PC = RB / 16, LR = 64 / PC, LI = BK / LR;      // pieces of a row; rows of a load instruction; loads
     __shared__ __align__(16) int8_t lds[W * TL::WAVE];
     __shared__ float join_m[W][32], join_l[W][32];
@@ -320,12 +350,11 @@ __global__ __launch_bounds__(64 * W, 2) void cached_attention_kernel(CaParams P)
         }
 
     V8 qf[DS];
+    float unit;                                            // of the scores, and of m up to the end
     {
         int rb, rh;
         row_of(min(li, rows - 1 - r0), rb, rh);
-        const T* const qp = static_cast<const T*>(P.q) + (int64_t)rb * P.ldq + (int64_t)rh * D + 8 * half;
-#pragma unroll
-        for (int s = 0; s < DS; ++s) qf[s] = *reinterpret_cast<const V8*>(qp + 16 * s);
+        unit = query<T, I8>(static_cast<const T*>(P.q) + (int64_t)rb * P.ldq + (int64_t)rh * D + 8 * half, qf);
     }
     // (here, where all loads so far are waited for: the waits in the loop count its own ones)
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -346,7 +375,7 @@ __global__ __launch_bounds__(64 * W, 2) void cached_attention_kernel(CaParams P)
         for (int d = 0; d < DS; ++d) {
             s[0] = mfma(key_frag<T, D, I8>(kl, d, li, half), qf[d], s[0]);
         }
-        float ks[16], vs[16], top_scale = 0.0f;
+        float ks[16], vs[16];
         if constexpr (I8) {
             const float* const scale = reinterpret_cast<const float*>(kl + 2 * TL::BYTES);
 #pragma unroll
@@ -354,7 +383,6 @@ __global__ __launch_bounds__(64 * W, 2) void cached_attention_kernel(CaParams P)
                 ks[r] = scale[8 * (r / 4) + 4 * half + r % 4];
                 vs[r] = scale[BK + 8 * (r / 4) + 4 * half + r % 4];
             }
-            top_scale = scale[BK + li];
         }
         wait_lds();
         if (n + S < own) issue(block(n + S), buf, keys);
@@ -371,9 +399,7 @@ __global__ __launch_bounds__(64 * W, 2) void cached_attention_kernel(CaParams P)
         V8 p[1][2];
         if constexpr (I8) {
             // Weights times the values' scales, over 2^ref: what float16 holds goes by the largest scale so far.
-#pragma unroll
-            for (int x = 1; x < 32; x *= 2) top_scale = __builtin_fmaxf(top_scale, __shfl_xor(top_scale, x));
-            softmax_step_scaled<T, DT>(s, p[0], m, l, acc, P.c, ref, n == 0, top_scale, vs);
+            softmax_step_scaled<DT>(s, p[0], m, l, acc, P.c * unit, ref, n == 0, vs);
         } else {
             softmax_step<T, 1, DT>(s, p, m, l, acc, P.c);
         }
@@ -387,6 +413,7 @@ __global__ __launch_bounds__(64 * W, 2) void cached_attention_kernel(CaParams P)
         if (n + S < own) issue(block(n + S), buf, values);
     }
     l = add_halves(l);
+    m *= unit;
 
     // The wavefronts' parts: largest scores and sums, then the outputs, a lane's registers to the same lane; a wavefront joins every fourth tile of 32 elements.
     if (half == 0) { join_m[wv][li] = m; join_l[wv][li] = l; }

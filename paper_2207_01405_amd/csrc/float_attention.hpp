@@ -103,10 +103,14 @@ __device__ __forceinline__ void softmax_step(const v16f (&s)[KB], typename Elem<
 
 // The same over 16 scores, for values of int8 rows: the weights that leave are times the values' scales over 2^ref, ref following
 // the largest scale of the block, the same for all lanes; the sum is that of the weights alone.  The output is in units of 2^ref.
-template <class T, int DT>
-__device__ __forceinline__ void softmax_step_scaled(const v16f (&s)[1], typename Elem<T>::v8 (&p)[2], float& m, float& l, v16f (&acc)[DT], float c, float& ref,
-                                                    bool first, float largest, const float (&scale)[16]) {
+template <int DT>
+__device__ __forceinline__ void softmax_step_scaled(const v16f (&s)[1], Elem<_Float16>::v8 (&p)[2], float& m, float& l, v16f (&acc)[DT], float c, float& ref,
+                                                    bool first, const float (&scale)[16]) {
     const float top = largest_of(s);
+    float largest = 0.0f;                                               // (a NaN among them leaves the others)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) largest = __builtin_fmaxf(largest, scale[r]);
+    largest = __builtin_fmaxf(largest, __shfl_xor(largest, 32));
     const float power = __builtin_fminf(__builtin_fmaxf(__builtin_ceilf(__builtin_amdgcn_logf(largest)), -120.0f), 120.0f);
     if (__builtin_expect(__any((top - m) * c > 8.0f) || first || power > ref, 0)) {
         const float to = (top - m) * c > 8.0f ? top : m, by = first ? power : __builtin_fmaxf(power, ref);
@@ -119,12 +123,12 @@ __device__ __forceinline__ void softmax_step_scaled(const v16f (&s)[1], typename
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][r] *= g;
     }
-    const float base = Elem<T>::kUp - (m == -__builtin_inff() ? 0.0f : m * c), down = __builtin_amdgcn_exp2f(-ref);
+    const float base = Elem<_Float16>::kUp - (m == -__builtin_inff() ? 0.0f : m * c), down = __builtin_amdgcn_exp2f(-ref);
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
         const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[0][r], c, base));
         l += w;
-        p[r / 8][r % 8] = (T)(w * (scale[r] * down));
+        p[r / 8][r % 8] = (_Float16)(w * (scale[r] * down));
     }
 }
 

@@ -179,7 +179,7 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void prompt_attention_kernel(PaPar
             arrive<0>();
             issue(n + 2, keys);
             issue(n + 1, values);
-            if (KG > 1 && n * KG + g >= tiles) return;
+            if (idle || (KG > 1 && n * KG + g >= tiles)) return;
             move_largest<DT>(top, m, l, acc, P.c);
             const float base = base_of<T>(m, P.c);
             V8 p[KB][2];
