@@ -513,10 +513,11 @@ template <class T, int D> __global__ __launch_bounds__(256) void join_kernel(CaP
     for (int e = 0; e < E; ++e) o[e] = (T)(val[e] * inv);
 }
 
-// Parts.  The prefix: two workgroups a CU (64 requests behind 8000 keys 39.9 us, with four 47.4, with eight 64.2: each part is 2 KB to write and read for
-// every four heads).  Requests: of the greatest length, four workgroups a CU and 1536 keys a part at most, so that requests of different lengths leave no CU
-// waiting (48 of up to 16384 int8 keys 172 us, in parts of 5461 keys 195); shorter ones in as many, of `least` keys at least, which are fewer where there are
-// few requests.
+// Parts, each of which costs 2 KB to write and to read for every four heads.  The prefix, where the rows share their tiles: a workgroup a CU (128 requests
+// behind 16000 keys, up to 256 each of their own, 62 us; two workgroups 72, one for two CUs 86) and 512 keys a part at least, or 1024 where the requests' own
+// keys keep the CUs busy beside it (64 behind 8000, up to 600 of their own: 44.3 and 40.2 us; without their own 27.2 and 31.8).  Else two workgroups and 256
+// keys.  Requests: of the greatest length, four workgroups a CU and 1536 keys a part at most, so that requests of different lengths leave no CU waiting (48 of
+// up to 16384 int8 keys 172 us, in parts of 5461 keys 195); shorter ones in as many, of `least` keys at least, which are fewer where there are few requests.
 struct Plan { int prefix_tiles, own_tiles, prefix_parts, own_parts, own_least; bool wide; };
 
 Plan plan_of(const CachedArgs& a) {
@@ -526,8 +527,11 @@ Plan plan_of(const CachedArgs& a) {
     const int64_t rows = (int64_t)a.B * group;
     Plan p{0, (group + 31) / 32, 0, 0, LEAST, rows > 64};
     p.prefix_tiles = (int)over(rows, p.wide ? WIDE : 32);
-    if (a.prefix_len > 0) p.prefix_parts = (int)min64(over(2 * cus, (int64_t)p.prefix_tiles * a.c.G), over(a.prefix_len, (p.wide ? 2 : 1) * BK * LEAST));
     const int64_t items = (int64_t)a.B * p.own_tiles * a.c.G;
+    if (a.prefix_len > 0) {
+        const int64_t least = !p.wide ? LEAST : items >= 2 * cus && a.B * most >= a.prefix_len ? 4 * LEAST : 2 * LEAST;
+        p.prefix_parts = (int)min64(over((p.wide ? 1 : 2) * cus, (int64_t)p.prefix_tiles * a.c.G), over(a.prefix_len, BK * least));
+    }
     if (most > 0 && items > 0) {
         p.own_least = items >= 2 * cus ? 4 * LEAST : 2 * items >= cus ? 2 * LEAST : LEAST;
         const int64_t fill = over(4 * cus, items), even = min64(over(most, 1536), 64);
