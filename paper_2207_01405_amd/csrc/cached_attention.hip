@@ -456,7 +456,7 @@ __global__ __launch_bounds__(64 * W, 2) void cached_attention_kernel(CaParams P)
 }
 
 // One wavefront a row: the parts' outputs, each times 2^(its maximum less the largest).
-template <class T, int D> __global__ __launch_bounds__(256) void join_kernel(CaParams P, int parts) {
+template <class T, int D, int AT_ONCE> __global__ __launch_bounds__(256) void join_kernel(CaParams P, int parts) {
     constexpr int E = D / 64;
     const int lane = threadIdx.x & 63;
     const int64_t rows = (int64_t)P.B * P.H, row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -482,14 +482,14 @@ template <class T, int D> __global__ __launch_bounds__(256) void join_kernel(CaP
         top = to;
         const float w = l == 0.0f ? 0.0f : m == top ? 1.0f : __builtin_amdgcn_exp2f((m - top) * P.c);
         const uint64_t there = __ballot(l != 0.0f);
-        // four at once: those without keys were not written, and one that was is loaded in their place, for nothing
+        // AT_ONCE together: those without keys were not written, and one that was is loaded in their place, for nothing
         const int n = min(64, parts - p0), some = there ? __builtin_ctzll(there) : 0;
         if (there)
 #pragma unroll 1
-            for (int i0 = 0; i0 < n; i0 += 4) {
-                float x[4][E], wi[4], li[4];
+            for (int i0 = 0; i0 < n; i0 += AT_ONCE) {
+                float x[AT_ONCE][E], wi[AT_ONCE], li[AT_ONCE];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
+                for (int j = 0; j < AT_ONCE; ++j) {
                     const int i = i0 + j;
                     const bool counts = i < n && (there >> i & 1);
                     const int at = counts ? i : some;
@@ -499,7 +499,7 @@ template <class T, int D> __global__ __launch_bounds__(256) void join_kernel(CaP
                     for (int e = 0; e < E; ++e) x[j][e] = P.part[((p0 + at) * rows + row) * D + lane * E + e];
                 }
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
+                for (int j = 0; j < AT_ONCE; ++j) {
                     if (wi[j] == 0.0f) continue;
                     sum = __builtin_fmaf(wi[j], li[j], sum);
 #pragma unroll
@@ -562,7 +562,8 @@ template <class T, int D, bool I8> hipError_t launch(hipStream_t s, const Cached
     }
     if (parts == 1 && !(p.wide && p.prefix_parts)) return hipSuccess;
     TraceScope trace(s, KIND_CACHED_JOIN, 0, (int64_t)a.B * a.H * (parts * (4 * (int64_t)D + 8) + 2 * D));
-    join_kernel<T, D><<<dim3((unsigned)(((int64_t)a.B * a.H + 3) / 4)), 256, 0, s>>>(P, parts);
+    auto* const join = parts > 4 ? join_kernel<T, D, 16> : join_kernel<T, D, 4>;
+    join<<<dim3((unsigned)(((int64_t)a.B * a.H + 3) / 4)), 256, 0, s>>>(P, parts);
     return hipGetLastError();
 }
 
