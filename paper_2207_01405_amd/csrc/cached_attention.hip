@@ -42,8 +42,11 @@ template <int D, bool I8> struct CaTile {
     static_assert(2 * SHARED <= W * WAVE, "room for two");
 };
 
-// 16-byte pieces of an int8 row: piece ^ mix8(row), for keys (8 bytes of 32 rows at a time) and values (8 bytes of 8 rows, twice) alike
-template <int D> __device__ __forceinline__ int mix8(int row) { return D == 128 ? row & 7 : (row >> 1) & 3; }
+// 16-byte pieces of an int8 row are stored at piece ^ mix8(row).  Keys are read 8 bytes of 16 rows at a time, values 32 bytes of rows 0 .. 3 and 8 .. 11 or 4 .. 7
+// and 12 .. 15: either spreads over all banks.
+template <int D> __device__ __forceinline__ int mix8(int row) {
+    return D == 128 ? (row & 2) | ((row >> 2) & 1) | ((row >> 1) & 4) : ((row >> 2) & 1) | ((row >> 2) & 2);
+}
 
 // all loads but the newest N have arrived; all LDS reads have
 template <int N> __device__ __forceinline__ void wait_but() { asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory"); }

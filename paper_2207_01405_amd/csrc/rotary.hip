@@ -15,9 +15,10 @@ using namespace scaled;
 
 constexpr int BLOCK = 256;
 
-struct Turn { const int32_t* positions; const double* freq; const int32_t* axis; int64_t ld; int axes, half; FastDiv by_half; };
+struct Turn { const int32_t* positions; const double* freq; const int32_t* axis; int64_t ld; int axes, half; bool split; FastDiv by_half; };
 
-// sines and cosines of rows first .. first + n - 1, pair i of row t at [t half + i]
+// sines and cosines of rows first .. first + n - 1, pair i of row t at [t half + i]; or, where lanes read eight of them each from multiples of eight on, the first
+// four of every eight and then the others, so that lanes read side by side
 __device__ __forceinline__ void angles(const Turn& r, int64_t first, int n, float* cs, float* sn) {
     for (int i = threadIdx.x; i < n * r.half; i += BLOCK) {
         uint32_t p;
@@ -26,9 +27,17 @@ __device__ __forceinline__ void angles(const Turn& r, int64_t first, int n, floa
         const double turns = (double)r.positions[a * r.ld + first + t] * r.freq[p] * 0.15915494309189535;     // / (2 pi)
         float s, c;
         sincospif((float)(2.0 * (turns - __builtin_rint(turns))), &s, &c);
-        cs[i] = c;
-        sn[i] = s;
+        const int at = r.split ? (int)t * r.half + (p & 4 ? r.half / 2 : 0) + (int)(p / 8) * 4 + (int)(p & 3) : i;
+        cs[at] = c;
+        sn[at] = s;
     }
+}
+
+typedef float v4f __attribute__((ext_vector_type(4)));
+// pairs e .. e + 7 of a row's, split as above
+__device__ __forceinline__ v8f split8(const float* row, int half, int e) {
+    const v4f a = *reinterpret_cast<const v4f*>(row + e / 2), b = *reinterpret_cast<const v4f*>(row + half / 2 + e / 2);
+    return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
 __device__ __forceinline__ float first_of(float x1, float x2, float c, float s) { return __builtin_fmaf(x1, c, -(x2 * s)); }
@@ -42,7 +51,7 @@ struct RotaryParams {
 // whole starts earlier and does some pairs again, with the same result; in place, where they may be turned by then, it goes element by element
 // (5003 x 17 heads of 80 of which 60 are turned, float32: 18.5 us element by element, 12.4 so).
 template <class T> __global__ __launch_bounds__(BLOCK) void rotary_kernel(RotaryParams P) {
-    extern __shared__ float lds[];
+    extern __shared__ __align__(16) float lds[];
     const int64_t first = (int64_t)blockIdx.x * P.rows_each;
     const int n = (int)min64(P.rows - first, P.rows_each), half = P.r.half;
     float *const cs = lds, *const sn = lds + P.rows_each * half;
@@ -81,6 +90,18 @@ template <class T> __global__ __launch_bounds__(BLOCK) void rotary_kernel(Rotary
         }
         int e = 8 * (int)piece;
         if (again && half >= 8) e = min(e, half - 8);
+        if (P.r.split) {
+            const v8f c = split8(cs + t * half, half, e), s = split8(sn + t * half, half, e), v1 = load8(x + e), v2 = load8(x + half + e);
+            v8f w1, w2;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                w1[j] = first_of(v1[j], v2[j], c[j], s[j]);
+                w2[j] = second_of(v1[j], v2[j], c[j], s[j]);
+            }
+            store8(y + e, w1);
+            store8(y + half + e, w2);
+            continue;
+        }
         const int m = half - e;
         const float *const c = cs + t * half + e, *const s = sn + t * half + e;
         const v8f v1 = m >= 8 ? load8(x + e) : load_some(x + e, m), v2 = m >= 8 ? load8(x + half + e) : load_some(x + half + e, m);
@@ -110,7 +131,7 @@ struct AppendParams {
 // values.  int8: the largest of a head over its lanes.
 template <class T, int D, bool I8> __global__ __launch_bounds__(BLOCK) void append_kernel(AppendParams P) {
     constexpr int L = D / 8;
-    extern __shared__ float lds[];
+    extern __shared__ __align__(16) float lds[];
     const int64_t first = (int64_t)blockIdx.x * P.rows_each;
     const int n = (int)min64(P.rows - first, P.rows_each), half = P.r.half;
     float *const cs = lds, *const sn = lds + P.rows_each * half;
@@ -141,11 +162,11 @@ template <class T, int D, bool I8> __global__ __launch_bounds__(BLOCK) void appe
                         v[2 * j] = first_of(a, b, c[j], s[j]);
                         v[2 * j + 1] = second_of(a, b, c[j], s[j]);
                     }
-            } else if (half % 8 == 0) {
+            } else if (P.r.split) {
                 const bool lower = e < half;
                 const int at = lower ? e : e - half;
                 const v8f w = load8(x + (lower ? e + half : at));
-                const float *const c = cs + t * half + at, *const s = sn + t * half + at;
+                const v8f c = split8(cs + t * half, half, at), s = split8(sn + t * half, half, at);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[j] = lower ? first_of(v[j], w[j], c[j], s[j]) : second_of(w[j], v[j], c[j], s[j]);
             } else {
@@ -183,7 +204,7 @@ template <class T, int D, bool I8> __global__ __launch_bounds__(BLOCK) void appe
 }
 
 Turn turn_of(const RotaryArgs& r) {
-    return Turn{r.positions, r.freq, r.axis, r.ld_positions, r.n_axes, r.half, FastDiv((uint32_t)(r.half > 0 ? r.half : 1))};
+    return Turn{r.positions, r.freq, r.axis, r.ld_positions, r.n_axes, r.half, !r.adjacent && r.half % 8 == 0, FastDiv((uint32_t)(r.half > 0 ? r.half : 1))};
 }
 
 // Rows of a workgroup: some 1024 pieces, as long as there are four workgroups a CU; sines and cosines of at most 32 KB.  Few rows: the pieces of one go to
