@@ -298,10 +298,11 @@ __global__ __launch_bounds__(64 * W, 2) void cached_attention_kernel(CaParams P)
         rb = prefix ? (int)P.by_group.divide(rest, rest) : b;
         rh = g * P.group + (int)rest;
     };
-    if (b0 == b1 && (all_parts > 1 || P.wide)) {           // no keys here
+    const bool sharing = prefix && P.wide;
+    if (b0 == b1 && (all_parts > 1 || sharing)) {          // no keys here (the only part writes its rows of zeros itself)
         int rb, rh;
         row_of(tid, rb, rh);
-        if (tid < (P.wide ? WIDE : 32) && r0 + tid < rows) {
+        if (tid < (sharing ? WIDE : 32) && r0 + tid < rows) {
             const int64_t at = (int64_t)out_part * P.B * P.H + (int64_t)rb * P.H + rh;
             P.ml[2 * at] = -__builtin_inff();
             P.ml[2 * at + 1] = 0.0f;
@@ -309,7 +310,7 @@ __global__ __launch_bounds__(64 * W, 2) void cached_attention_kernel(CaParams P)
         return;
     }
 
-    if (prefix && P.wide) {
+    if (sharing) {
         shared_keys<T, D, I8>(P, lds, g, r0, b0 * BK, min(b1 * BK, len), part, [&](int r, int& rb, int& rh) __attribute__((always_inline)) { row_of(r - r0, rb, rh); });
         return;
     }

@@ -235,3 +235,12 @@ def test_errors(ivit):
     with pytest.raises(ValueError):
         s.prefix = 5
         s.call(ivit)
+
+
+@pytest.mark.parametrize("B,H,G", [(70, 1, 1), (70, 4, 2), (300, 2, 2), (3, 100, 1)])
+def test_requests_without_keys_among_many(ivit, B, H, G):
+    """One part of every request, no prefix: a row without keys is zeros, a padded one is left."""
+    for i8 in (False, True):
+        s = Setup(B, [(0, 5, -1, 60)[b % 4] for b in range(B)], 0, H, G, 64, "bf16", i8, 32)
+        s.call(ivit)
+        s.compare("without keys")
