@@ -208,6 +208,7 @@ __device__ __forceinline__ void shared_keys(const CaParams& P, int8_t* lds, int 
 #pragma unroll
                     for (int i = 0; i < DT; ++i) acc[i] = mfma(value_frag<T, D, I8>(lds + buf * TL::SHARED + (TK + 32 * b + 16 * t) * RB, i, lane), p[b][t], acc[i]);
             }
+            __builtin_amdgcn_sched_barrier(0);             // (products of both mixed need a register too many)
             scores(n + 1, buf ^ 1, next);                  // (of the last tile: of what that buffer holds, not used)
         } else {
             move_largest<DT>(largest_of(s), m, l, acc, P.c);
