@@ -493,19 +493,21 @@ template <class T, int D, int AT_ONCE> __global__ __launch_bounds__(256) void jo
 #pragma unroll 1
             for (int i0 = 0; i0 < n; i0 += AT_ONCE) {
                 float x[AT_ONCE][E], wi[AT_ONCE], li[AT_ONCE];
+                bool has[AT_ONCE];
 #pragma unroll
                 for (int j = 0; j < AT_ONCE; ++j) {
                     const int i = i0 + j;
                     const bool counts = i < n && (there >> i & 1);
                     const int at = counts ? i : some;
-                    wi[j] = counts ? __shfl(w, at) : 0.0f;
+                    has[j] = counts;
+                    wi[j] = __shfl(w, at);
                     li[j] = __shfl(l, at);
 #pragma unroll
                     for (int e = 0; e < E; ++e) x[j][e] = P.part[((p0 + at) * rows + row) * D + lane * E + e];
                 }
 #pragma unroll
                 for (int j = 0; j < AT_ONCE; ++j) {
-                    if (wi[j] == 0.0f) continue;
+                    if (!has[j]) continue;                             // (a weight of 0 counts: a sum of NaN stays one)
                     sum = __builtin_fmaf(wi[j], li[j], sum);
 #pragma unroll
                     for (int e = 0; e < E; ++e) val[e] = __builtin_fmaf(wi[j], x[j][e], val[e]);

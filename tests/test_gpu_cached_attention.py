@@ -244,3 +244,27 @@ def test_requests_without_keys_among_many(ivit, B, H, G):
         s = Setup(B, [(0, 5, -1, 60)[b % 4] for b in range(B)], 0, H, G, 64, "bf16", i8, 32)
         s.call(ivit)
         s.compare("without keys")
+
+
+@pytest.mark.parametrize("prefix", [0, 40, 1000])
+def test_keys_that_count_and_are_not_finite(ivit, prefix):
+    """NaN among the keys, the values or the scales of a request is NaN in its row, whatever parts it is in, and in no other."""
+    import torch
+    nan = float("nan")
+    for lens, where in (([5, 3000, 40], 0), ([5, 3000, 40], 2999), ([1, 700, 1], 3), ([1, 1, 1], 0)):
+        for i8 in (False, True):
+            for name in "kv":
+                s = Setup(12, lens, prefix, 4, 2, 64, "bf16", i8, 16)
+                want = s.call(ivit).clone()
+                at = int(s.pages[1, where // 16])
+                if i8:
+                    s.cache[name + "_scale"][at, :, where % 16] = nan
+                else:
+                    s.cache[name][at, :, where % 16] = nan
+                s.call(ivit)
+                assert bool(s.o[1].isnan().all()), "%s prefix %d at %d %s i8 %s" % (lens, prefix, where, name, i8)
+                assert torch.equal(s.o[[0, 2]], want[[0, 2]])
+                if not i8 and name == "k":                  # all of a request's own scores NaN
+                    s.cache["k"][s.pages[1, :-(-lens[1] // 16)].long()] = nan
+                    s.call(ivit)
+                    assert bool(s.o[1].isnan().all()) and torch.equal(s.o[[0, 2]], want[[0, 2]])
