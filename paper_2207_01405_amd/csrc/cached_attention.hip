@@ -70,7 +70,7 @@ __device__ __forceinline__ Elem<_Float16>::v8 spread(v2u b) {
 template <class T, bool I8> using Mul = std::conditional_t<I8, _Float16, T>;
 
 // A lane's half of a query row, elements 16 s + 8 half on, as fragments; those of an int8 cache's bfloat16 queries over 2^e, e that of the row's largest: what is
-// below 2^-14 of it keeps 24 bits below it.  Returns 2^e.
+// below 2^-14 of it keeps 24 bits below it.  Returns 2^e, a normal number as its reciprocal is.
 template <class T, bool I8, int DS> __device__ __forceinline__ float query(const T* q, typename Elem<Mul<T, I8>>::v8 (&qf)[DS]) {
     if constexpr (!I8 || __is_same(T, _Float16)) {
 #pragma unroll
@@ -86,7 +86,7 @@ template <class T, bool I8, int DS> __device__ __forceinline__ float query(const
             for (int e = 0; e < 8; ++e) top = __builtin_fmaxf(top, __builtin_fabsf((float)x[s][e]));
         }
         top = max_halves(top);
-        const int e = top > 0.0f && top < 0x1p126f ? __builtin_amdgcn_frexp_expf(top) : top > 0.0f ? 120 : 0;
+        const int e = top > 0.0f && top < 0x1p126f ? max(__builtin_amdgcn_frexp_expf(top), -125) : top > 0.0f ? 120 : 0;
         const float down = __builtin_amdgcn_ldexpf(1.0f, -e);
 #pragma unroll
         for (int s = 0; s < DS; ++s)
@@ -95,6 +95,9 @@ template <class T, bool I8, int DS> __device__ __forceinline__ float query(const
         return __builtin_amdgcn_ldexpf(1.0f, e);
     }
 }
+
+// Parts are joined by the exponents of their largest scores: scores of rows of int8 keys, each in units of its own, need not fit 32 bits otherwise.
+__device__ __forceinline__ float exponent(float m, float c) { return m == -__builtin_inff() ? m : m * c; }
 
 // The page of a key by its number, as a scalar load.  (Kept 64 at a time in a vector register: no change.)
 __device__ __forceinline__ int page_at(const CaParams& P, const int32_t* table, int key) {
@@ -150,11 +153,11 @@ __device__ __forceinline__ void shared_keys(const CaParams& P, int8_t* lds, int 
     issue(0, values);
     const int mine = first + 32 * wv;
     V8 qf[DS];
-    float unit;                                            // of the scores, and of m up to the end
+    float c = P.c;                                         // of scores in the row's units, as m is up to the end
     {
         int rb, rh;
         row_of(min(mine + li, rows - 1), rb, rh);
-        unit = query<T, I8>(static_cast<const T*>(P.q) + (int64_t)rb * P.ldq + (int64_t)rh * D + 8 * half, qf);
+        c *= query<T, I8>(static_cast<const T*>(P.q) + (int64_t)rb * P.ldq + (int64_t)rh * D + 8 * half, qf);
     }
     v16f acc[DT];
     float m = -__builtin_inff(), l = 0.0f, ref = 0.0f;
@@ -202,7 +205,7 @@ __device__ __forceinline__ void shared_keys(const CaParams& P, int8_t* lds, int 
                 float vs[16];
 #pragma unroll
                 for (int r = 0; r < 16; ++r) vs[r] = *reinterpret_cast<const float*>(scale_at(buf, b, r) + 64);
-                softmax_step_scaled<DT>(one, p[b], m, l, acc, P.c * unit, ref, n == 0 && b == 0, vs);
+                softmax_step_scaled<DT>(one, p[b], m, l, acc, c, ref, n == 0 && b == 0, vs);
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -211,13 +214,13 @@ __device__ __forceinline__ void shared_keys(const CaParams& P, int8_t* lds, int 
             __builtin_amdgcn_sched_barrier(0);             // (products of both mixed need a register too many)
             scores(n + 1, buf ^ 1, next);                  // (of the last tile: of what that buffer holds, not used)
         } else {
-            move_largest<DT>(largest_of(s), m, l, acc, P.c);
-            const float base = base_of<T>(m, P.c);
+            move_largest<DT>(largest_of(s), m, l, acc, c);
+            const float base = base_of<T>(m, c);
             scores(n + 1, buf ^ 1, next);
 #pragma unroll
             for (int b = 0; b < KB; ++b)
 #pragma unroll
-                for (int r = 0; r < 16; r += 2) weigh<T>(s[b], r, p[b], l, P.c, base);
+                for (int r = 0; r < 16; r += 2) weigh<T>(s[b], r, p[b], l, c, base);
 #pragma unroll
             for (int t = 0; t < 2 * KB; ++t)
 #pragma unroll
@@ -231,7 +234,7 @@ __device__ __forceinline__ void shared_keys(const CaParams& P, int8_t* lds, int 
         if (n + 1 < tiles) step(n + 1, 1, odd_s, even_s);
     }
     l = add_halves(l);
-    m *= unit;
+    m = exponent(m, c);
     // results as whole lines: a lane's registers into LDS of the wavefront's own, and out of it 4 elements of row lane / 8 + 8 n at 4 (lane % 8)
     __syncthreads();
     float* const out = reinterpret_cast<float*>(lds + wv * TL::WAVE);
@@ -355,11 +358,11 @@ __global__ __launch_bounds__(64 * W, 2) void cached_attention_kernel(CaParams P)
         }
 
     V8 qf[DS];
-    float unit;                                            // of the scores, and of m up to the end
+    float c = P.c;                                         // of scores in the row's units, as m is up to the end
     {
         int rb, rh;
         row_of(min(li, rows - 1 - r0), rb, rh);
-        unit = query<T, I8>(static_cast<const T*>(P.q) + (int64_t)rb * P.ldq + (int64_t)rh * D + 8 * half, qf);
+        c *= query<T, I8>(static_cast<const T*>(P.q) + (int64_t)rb * P.ldq + (int64_t)rh * D + 8 * half, qf);
     }
     // (here, where all loads so far are waited for: the waits in the loop count its own ones)
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -404,9 +407,9 @@ __global__ __launch_bounds__(64 * W, 2) void cached_attention_kernel(CaParams P)
         V8 p[1][2];
         if constexpr (I8) {
             // Weights times the values' scales, over 2^ref: what float16 holds goes by the largest scale so far.
-            softmax_step_scaled<DT>(s, p[0], m, l, acc, P.c * unit, ref, n == 0, vs);
+            softmax_step_scaled<DT>(s, p[0], m, l, acc, c, ref, n == 0, vs);
         } else {
-            softmax_step<T, 1, DT>(s, p, m, l, acc, P.c);
+            softmax_step<T, 1, DT>(s, p, m, l, acc, c);
         }
         if (n + S < own) wait_but<(S - 1) * PAIR + KL>();                  // behind its values: the next S - 1 blocks, and the keys behind them
         else wait_but<0>();
@@ -418,7 +421,7 @@ __global__ __launch_bounds__(64 * W, 2) void cached_attention_kernel(CaParams P)
         if (n + S < own) issue(block(n + S), buf, values);
     }
     l = add_halves(l);
-    m *= unit;
+    m = exponent(m, c);
 
     // The wavefronts' parts: largest scores and sums, then the outputs, a lane's registers to the same lane; a wavefront joins every fourth tile of 32 elements.
     if (half == 0) { join_m[wv][li] = m; join_l[wv][li] = l; }
@@ -434,7 +437,7 @@ __global__ __launch_bounds__(64 * W, 2) void cached_attention_kernel(CaParams P)
     for (int w = 1; w < W; ++w) top = __builtin_fmaxf(top, join_m[w][li]);
 #pragma unroll
     for (int w = 0; w < W; ++w) {
-        f[w] = join_m[w][li] == top ? 1.0f : __builtin_amdgcn_exp2f((join_m[w][li] - top) * P.c);
+        f[w] = join_m[w][li] == top ? 1.0f : __builtin_amdgcn_exp2f(join_m[w][li] - top);
         sum = __builtin_fmaf(f[w], join_l[w][li], sum);
     }
     if (r0 + li >= rows) return;
@@ -480,12 +483,12 @@ template <class T, int D, int AT_ONCE> __global__ __launch_bounds__(256) void jo
         float most = l != 0.0f ? m : -__builtin_inff();
 #pragma unroll
         for (int x = 1; x < 64; x *= 2) most = __builtin_fmaxf(most, __shfl_xor(most, x));
-        const float to = __builtin_fmaxf(top, most), f = to == top ? 1.0f : __builtin_amdgcn_exp2f((top - to) * P.c);
+        const float to = __builtin_fmaxf(top, most), f = to == top ? 1.0f : __builtin_amdgcn_exp2f(top - to);
         sum *= f;
 #pragma unroll
         for (int e = 0; e < E; ++e) val[e] *= f;
         top = to;
-        const float w = l == 0.0f ? 0.0f : m == top ? 1.0f : __builtin_amdgcn_exp2f((m - top) * P.c);
+        const float w = l == 0.0f ? 0.0f : m == top ? 1.0f : __builtin_amdgcn_exp2f(m - top);
         const uint64_t there = __ballot(l != 0.0f);
         // AT_ONCE together: those without keys were not written, and one that was is loaded in their place, for nothing
         const int n = min(64, parts - p0), some = there ? __builtin_ctzll(there) : 0;

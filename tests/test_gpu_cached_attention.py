@@ -268,3 +268,17 @@ def test_keys_that_count_and_are_not_finite(ivit, prefix):
                     s.cache["k"][s.pages[1, :-(-lens[1] // 16)].long()] = nan
                     s.call(ivit)
                     assert bool(s.o[1].isnan().all()) and torch.equal(s.o[[0, 2]], want[[0, 2]])
+
+
+def test_queries_of_very_different_size(ivit):
+    """bfloat16 queries over an int8 cache, whose products are float16: from below the normal numbers to near the end of the range."""
+    import torch
+    for power in (-130, -126, -60, 20, 100, 126):
+        s = Setup(3, [60, 33], 20, 4, 2, 128, "bf16", True, 16)
+        s.q = (s.q.double() * 2.0 ** power).bfloat16()
+        s.call(ivit, scale=128 ** -0.5 * 2.0 ** -power if -126 <= -power <= 126 else 1.0)
+        s.compare("power %d" % power, scale=128 ** -0.5 * 2.0 ** -power if -126 <= -power <= 126 else 1.0)
+    s = Setup(3, [60, 33], 20, 4, 2, 128, "bf16", True, 16)
+    s.q.zero_()
+    s.call(ivit)
+    s.compare("zeros")
