@@ -193,7 +193,20 @@ __device__ __forceinline__ void shared_keys(const CaParams& P, int8_t* lds, int 
     v16f even_s[KB], odd_s[KB];
     scores(0, 0, even_s);
     finish(0, 0, even_s);
+    // The values behind the last key, of weight 0, to 0 (with int8 rows, their scales): the last key's are in their place, and may be infinite.
+    auto clear = [&](int n, int buf) __attribute__((always_inline)) {
+        wait_but<0>();
+        const int from = max(last + 1 - (k0 + n * TK + 16 * wv), 0);
+        int8_t* const to = lds + buf * TL::SHARED;
+        if constexpr (I8) {
+            if (lane >= from && lane < 16) *reinterpret_cast<float*>(to + 2 * TK * RB + 256 * wv + 64 + 4 * lane) = 0.0f;
+        } else {
+#pragma unroll 1
+            for (int i = from * PC + lane; i < 16 * PC; i += 64) *reinterpret_cast<v4u*>(to + (TK + 16 * wv) * RB + 16 * i) = v4u{};
+        }
+    };
     auto step = [&](int n, int buf, v16f (&s)[KB], v16f (&next)[KB]) __attribute__((always_inline)) {
+        if (n == tiles - 1 && last - k0 - n * TK < TK - 1) clear(n, buf);
         arrive<0>();
         issue(n + 2, keys);
         issue(n + 1, values);
@@ -402,7 +415,10 @@ __global__ __launch_bounds__(64 * W, 2) void cached_attention_kernel(CaParams P)
             const int rel = len - 1 - blk * BK - 4 * half;
 #pragma unroll
             for (int r = 0; r < 16; ++r)
-                if (8 * (r / 4) + r % 4 > rel) s[0][r] = -__builtin_inff();
+                if (8 * (r / 4) + r % 4 > rel) {
+                    s[0][r] = -__builtin_inff();
+                    vs[r] = 0.0f;                          // (see below)
+                }
         }
         V8 p[1][2];
         if constexpr (I8) {
@@ -413,6 +429,12 @@ __global__ __launch_bounds__(64 * W, 2) void cached_attention_kernel(CaParams P)
         }
         if (n + S < own) wait_but<(S - 1) * PAIR + KL>();                  // behind its values: the next S - 1 blocks, and the keys behind them
         else wait_but<0>();
+        if constexpr (!I8)
+            if ((blk + 1) * BK > len) {                    // behind the last key are its values again, which may be infinite, of weight 0
+#pragma unroll 1
+                for (int i = (len - blk * BK) * PC + lane; i < BK * PC; i += 64) *reinterpret_cast<v4u*>(mine + buf * TL::STAGE + TL::BYTES + 16 * i) = v4u{};
+                wait_lds();
+            }
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll

@@ -282,3 +282,34 @@ def test_queries_of_very_different_size(ivit):
     s.q.zero_()
     s.call(ivit)
     s.compare("zeros")
+
+
+@pytest.mark.parametrize("B,prefix", [(1, 0), (3, 40), (70, 40), (70, 1000)])
+def test_infinite_values(ivit, B, prefix):
+    """A value that counts and is infinite makes its element of the rows that see it so, and no other; the last key of all too."""
+    import torch
+    inf = float("inf")
+    for d, t in ((64, "bf16"), (128, "f16")):
+        for i8 in (False, True):
+            for n, where in ((5, 4), (33, 32), (333, 332), (333, 100), (prefix, prefix - 1), (prefix, prefix // 2)):
+                if not n:
+                    continue
+                shared = n == prefix and prefix > 0
+                s = Setup(13, [7 if shared else n] * B, prefix, 4, 2, d, t, i8, 16)
+                table = s.prefix_pages if shared else s.pages[0]
+                at = (int(table[where // 16]), 1, where % 16)
+                if i8:
+                    s.cache["v"][at] = torch.where(s.cache["v"][at] == 0, 1, s.cache["v"][at]).to(torch.int8)
+                want = s.call(ivit).clone()
+                if i8:
+                    sign = s.cache["v"][at].float().sign()
+                    s.cache["v_scale"][at] = inf
+                else:
+                    sign = torch.where(torch.arange(d, device="cuda") % 3 == 0, -1.0, 1.0)
+                    s.cache["v"][at] = (sign * inf).to(s.q.dtype)
+                s.call(ivit)
+                got, old = s.o.reshape(B, 2, 2 * d), want.reshape(B, 2, 2 * d)
+                hit = slice(0, B if shared else 1)
+                what = "%d x %d %s i8 %s prefix %d: key %d of %d" % (B, d, t, i8, prefix, where, n)
+                assert torch.equal(got[hit, 1].float(), (sign * inf).repeat(2).expand(got[hit, 1].shape)), what
+                assert torch.equal(got[:, 0], old[:, 0]) and (shared or torch.equal(got[1:], old[1:])), what
