@@ -487,16 +487,21 @@ int ivit_gated_quant(void* stream, const void* x, int64_t ldx, int8_t* y, int64_
  *    G: query head h reads key head h / (H / G).
  *  - Rows, leading dimensions and alignment as in the section above, unless stated.  Rows and caches of attention are float16
  *    or bfloat16, its head size d 64 or 128.
- *  - Scores, the statistics of softmax and sums of values are held in 32 bits.  Weights, at most 256 (float16: 2^15) times the
- *    largest, are rounded to the rows' type where the matrix cores multiply them, and their sum is that of the rounded ones.
- *    Results are rounded once.  Equal calls give equal bits.
+ *  - Scores, the statistics of softmax and sums of values are held in 32 bits; q . k, scale q . k and the results have to lie within float32.
+ *    Weights are rounded to the rows' type where the matrix cores multiply them with the values, and divided by the sum of the rounded
+ *    ones.  Results are rounded once.  Equal calls give equal bits.
+ *  - An int8 cache is multiplied in float16: its whole numbers are exact there, bfloat16 queries stand over a power of two of a row's largest
+ *    element (what is less than 2^-14 of it loses bits, 2^-25 of it at most), and the weights times the values' scales are rounded to
+ *    float16, over the sum of weights that are not rounded.
+ *  - NaN or infinite values that count reach the result as in the formula, but for weights below 2^-126 (where float16 is multiplied: 2^-32) of the largest,
+ *    which may count as 0: 0 times an infinite value is NaN.
  *  - A key left out (behind a query, past the end of its sequence) has no part in a result whatever it holds, NaN included; a
  *    row without keys is zeros.  Rows of no sequence are left as they were. */
 
 /* Rotary positions: pair i of a head, i < rotary_dim / 2, is turned by  phi = positions[a][row] * freq[i],  a = axis ? axis[i] : 0:
  *   (x1, x2) -> (x1 cos phi - x2 sin phi, x2 cos phi + x1 sin phi)
  * (x1, x2) being elements (i, i + rotary_dim / 2) of the head, or (2 i, 2 i + 1) if adjacent != 0; elements from rotary_dim on
- * are copied.  phi is formed in 64 bits and brought to one turn there, its sine and cosine are within 2^-22 of themselves plus
+ * are copied.  phi is formed in 64 bits and brought to one turn there; the errors of its sine and cosine are at most 2^-22 +
  * |phi| 2^-51.  Several axes: images (row, column), video (time, row, column); a value of axis outside 0 .. n_axes - 1 is
  * taken as the nearest of them. */
 typedef struct {
@@ -534,7 +539,7 @@ typedef struct {
  * pieces of both.  int8: q = round(127 v / max |v|) of the turned values before any rounding, as ivit_gated_quant has it.
  * q [rows, n_q_heads * d], k, v [rows, G * d] of `type` (float16, bfloat16), slots int32 [rows].  No overlap.
  * Requirements: 0 <= rows < 2^31, n_q_heads * d and G * d <= 2^24.
- * Errors: NULL, SHAPE, PARAM (type, the cache's type, n_axes), ALIGN, HIP. */
+ * Errors: NULL, SHAPE, PARAM (type, the cache's type, n_axes, q_out == q), ALIGN, HIP. */
 int ivit_cache_append(void* stream, const void* q, int64_t ldq, void* q_out, int64_t ldq_out, int32_t n_q_heads, const void* k,
                       int64_t ldk, const void* v, int64_t ldv, const int32_t* slots, int64_t rows, int32_t type,
                       const ivit_rotary_params* r, const ivit_cache* c);
@@ -545,7 +550,7 @@ int ivit_cache_append(void* stream, const void* q, int64_t ldq, void* q_out, int
  * are fewer keys than queries, none).
  * q, o [n_q, H * d], k, v [n_k, G * d] of `type`; starts int32 [n_seq + 1] (device), not falling; a sequence that is not within the
  * rows is left out.  scale > 0 and finite.  No overlap.
- * Requirements: 0 <= n_q, n_k < 2^31, 0 <= n_seq < 2^20, H and G <= 4096, (n_q / 64 + n_seq) H < 2^24; ldq, ldk, ldv <= 2^24; leading dimensions and
+ * Requirements: 0 <= n_q, n_k <= 2^30, 0 <= n_seq < 2^20, H and G <= 4096, (n_q / 64 + n_seq) H < 2^24; ldq, ldk, ldv <= 2^24; leading dimensions and
  * pointers of q, k, v, o whole 16 bytes.
  * Errors: NULL, SHAPE, PARAM (type, scale), ALIGN, HIP. */
 int ivit_prompt_attention(void* stream, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, void* o,

@@ -824,6 +824,7 @@ int ivit_cache_append(void* stream, const void* q, int64_t ldq, void* q_out, int
     if (q && ((st = check_rows(q, ldq, (int64_t)n_q_heads * d, type)) != IVIT_OK || (st = check_rows(q_out, ldq_out, (int64_t)n_q_heads * d, type)) != IVIT_OK))
         return st;
     if (!aligned(slots, 4)) return IVIT_ERR_ALIGN;
+    if (q && q == q_out) return IVIT_ERR_PARAM;             // a lane reads what another turns
     return hip_status(ivit::launch_cache_append(static_cast<hipStream_t>(stream), a));
 }
 
@@ -831,7 +832,7 @@ int ivit_prompt_attention(void* stream, const void* q, int64_t ldq, const void* 
                           const int32_t* q_start, const int32_t* k_start, int32_t n_seq, int64_t n_q, int64_t n_k, int32_t H, int32_t G, int32_t d,
                           int32_t type, float scale, int32_t causal) {
     if ((type != IVIT_F16 && type != IVIT_BF16) || !std::isfinite(scale) || !(scale > 0.0f)) return IVIT_ERR_PARAM;
-    if (n_q < 0 || n_q > 0x7fffffffLL || n_k < 0 || n_k > 0x7fffffffLL || n_seq < 0 || n_seq >= (1 << 20) || (d != 64 && d != 128)) return IVIT_ERR_SHAPE;
+    if (n_q < 0 || n_q > (1 << 30) || n_k < 0 || n_k > (1 << 30) || n_seq < 0 || n_seq >= (1 << 20) || (d != 64 && d != 128)) return IVIT_ERR_SHAPE;
     if (H < 1 || H > 4096 || G < 1 || G > H || H % G || (!k_start && n_q != n_k) || (n_q / 64 + n_seq) * H >= (1 << 24)) return IVIT_ERR_SHAPE;
     if (ldq > (1 << 24) || (n_k > 0 && (ldk > (1 << 24) || ldv > (1 << 24)))) return IVIT_ERR_SHAPE;
     if (n_q == 0 || n_seq == 0) return IVIT_OK;

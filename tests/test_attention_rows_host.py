@@ -74,6 +74,12 @@ def test_append_refusals(lib):
     assert append(lib, k=None, v=None, slots=None, rows=0) == 0
 
 
+def test_append_in_place_and_prompts_beyond_31_bits_are_refused(lib):
+    """Queries turned in place would be read by one lane while another turns them; the numbers of 2^30 rows and of a tile behind them fit 32 bits."""
+    assert append(lib, q=FAKE, qo=FAKE) == E["PARAM"] and append(lib, q=FAKE, qo=FAKE, r=turn()) == E["PARAM"]
+    assert prompt(lib, nk=(1 << 30) + 1, ks=FAKE) == E["SHAPE"] and prompt(lib, nq=(1 << 30) + 1, ks=FAKE, H=1, G=1) == E["SHAPE"]
+
+
 def prompt(lib, q=FAKE, ldq=256, k=FAKE, ldk=128, v=FAKE, ldv=128, o=FAKE, ldo=256, qs=FAKE, ks=None, n=1, nq=8, nk=8, H=4, G=2, d=64, t=BF16, scale=0.125, causal=1):
     return lib.ivit_prompt_attention(None, q, ldq, k, ldk, v, ldv, o, ldo, qs, ks, n, nq, nk, H, G, d, t, scale, causal)
 
