@@ -173,7 +173,7 @@ __device__ __forceinline__ void key_by_key(const T* q, const T* k, int64_t ldk, 
     }
 }
 
-// A query's row of D elements: the halves of a wavefront exchange runs of four, so that 16 bytes leave at once.
+// A query's row of 32 DT elements from a lane's registers, 8 bytes a store (for few rows).
 template <class T, int DT> __device__ __forceinline__ void store_rows(T* o, const v16f (&acc)[DT], float inv, int half) {
     typedef T v4 __attribute__((ext_vector_type(4)));
     typedef float v4f __attribute__((ext_vector_type(4)));
