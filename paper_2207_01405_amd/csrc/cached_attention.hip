@@ -11,6 +11,8 @@
 // quarter an element, which bounds these caches (to bfloat16, which has no place for eight bits under a leading one, they were three, and 48 requests of 8192 keys took
 // 177 us for 163).  bfloat16 queries become float16 with a power of two of their own, which their scores get back.  The keys' scales go to the
 // scores, the values' to the weights.
+#include <cmath>
+
 #include "regst_common.hpp"
 #include "float_attention.hpp"
 
@@ -545,11 +547,13 @@ template <class T, int D, int AT_ONCE> __global__ __launch_bounds__(256) void jo
     for (int e = 0; e < E; ++e) o[e] = (T)(val[e] * inv);
 }
 
-// Parts, each of which costs 2 KB to write and to read for every four heads.  The prefix, where the rows share their tiles: a workgroup a CU (128 requests
-// behind 16000 keys, up to 256 each of their own, 62 us; two workgroups 72, one for two CUs 86) and 512 keys a part at least, or 1024 where the requests' own
-// keys keep the CUs busy beside it (64 behind 8000, up to 600 of their own: 44.3 and 40.2 us; without their own 27.2 and 31.8).  Else two workgroups and 256
-// keys.  Requests: of the greatest length, four workgroups a CU and 1536 keys a part at most, so that requests of different lengths leave no CU waiting (48 of
+// Parts.  Requests: of the greatest length, four workgroups a CU and 1536 keys a part at most, so that requests of different lengths leave no CU waiting (48 of
 // up to 16384 int8 keys 172 us, in parts of 5461 keys 195); shorter ones in as many, of `least` keys at least, which are fewer where there are few requests.
+// The prefix: n parts take about  max(own, chain / n + own / 2) + n part  us.  chain: all its keys by one workgroup, 9 ns a key, or 17 for elements of 128 (34 of int8
+// rows) where a wavefront has rows of its own; own: the requests' own keys from memory, beside which a workgroup of the prefix gets on half as fast; part: writing
+// and reading the rows of a part.  `own` is known for the greatest length only, and counts up to 40 us.  Where the prefix's workgroups take more than three
+// quarters of the CUs, the requests' take a quarter longer.  Heads of 128, 32 on 8, in us with one part / these / the best number: 64 requests behind 1000 keys
+// 28.9 / 17.4 / 17.4, behind 8000 with up to 600 of their own 155 / 42 / 41, 256 behind 16000 291 / 97 / 97, 128 behind 8000 with 1200 of their own 207 / 136 / 125.
 struct Plan { int prefix_tiles, own_tiles, prefix_parts, own_parts, own_least; bool wide; };
 
 Plan plan_of(const CachedArgs& a) {
@@ -561,8 +565,16 @@ Plan plan_of(const CachedArgs& a) {
     p.prefix_tiles = (int)over(rows, p.wide ? WIDE : 32);
     const int64_t items = (int64_t)a.B * p.own_tiles * a.c.G;
     if (a.prefix_len > 0) {
-        const int64_t least = !p.wide ? LEAST : items >= 2 * cus && a.B * most >= a.prefix_len ? 4 * LEAST : 2 * LEAST;
-        p.prefix_parts = (int)min64(over((p.wide ? 1 : 2) * cus, (int64_t)p.prefix_tiles * a.c.G), over(a.prefix_len, BK * least));
+        const int full = (int)over(cus, (int64_t)p.prefix_tiles * a.c.G);                                    // parts that are a workgroup a CU
+        const bool i8 = a.c.type == TYPE_I8;
+        const float chain = a.prefix_len * (p.wide ? a.c.d * (i8 ? 2.66e-4f : 1.33e-4f) : 9e-3f), part = (float)a.B * a.H * a.c.d * (p.wide ? 3.5e-6f : 7e-6f);
+        const float own = std::fmin((float)a.B * most * a.c.G * a.c.d * (i8 ? 4e-7f : 8e-7f), 40.0f), root = std::sqrt(chain / part);
+        auto takes = [&](int n) { return std::fmax(own, chain / n + own / 2) + part * n; };
+        const float best = std::fmax(own * root > 2 * chain ? 2 * chain / own : root, 1.0f);               // where it is least
+        const int most_parts = (int)min64(full, over(a.prefix_len, BK * (p.wide ? W : LEAST))), fewer = max(3 * full / 4, 1);
+        int n = best < most_parts ? (int)best : most_parts;
+        if (n < most_parts && takes(n + 1) < takes(n)) ++n;
+        p.prefix_parts = n > fewer && takes(fewer) < takes(n) + own / 4 ? fewer : n;
     }
     if (most > 0 && items > 0) {
         p.own_least = items >= 2 * cus ? 4 * LEAST : 2 * items >= cus ? 2 * LEAST : LEAST;
