@@ -548,7 +548,8 @@ template <class T, int D, int AT_ONCE> __global__ __launch_bounds__(256) void jo
 }
 
 // Parts.  Requests: of the greatest length, four workgroups a CU and 1536 keys a part at most, so that requests of different lengths leave no CU waiting (48 of
-// up to 16384 int8 keys 172 us, in parts of 5461 keys 195); shorter ones in as many, of `least` keys at least, which are fewer where there are few requests.
+// up to 16384 int8 keys 172 us, in parts of 5461 keys 195); shorter ones in as many, of `least` keys at least, which are fewer where there are few requests.  Without
+// a prefix twice as many are one part, which is one launch (1 request of 500, 32 heads of 128 on 8: 9.0 -> 8.7 us, with the host 11.5 -> 9.0; 32 of 1000 30.6 -> 27.9).
 // The prefix: n parts take about  max(own, chain / n + own / 2) + n part  us.  chain: all its keys by one workgroup, 9 ns a key, or 17 for elements of 128 (34 of int8
 // rows) where a wavefront has rows of its own; own: the requests' own keys from memory, beside which a workgroup of the prefix gets on half as fast; part: writing
 // and reading the rows of a part.  `own` is known for the greatest length only, and counts up to 40 us.  Where the prefix's workgroups take more than three
@@ -579,7 +580,7 @@ Plan plan_of(const CachedArgs& a) {
     if (most > 0 && items > 0) {
         p.own_least = items >= 2 * cus ? 4 * LEAST : 2 * items >= cus ? 2 * LEAST : LEAST;
         const int64_t fill = over(4 * cus, items), even = min64(over(most, 1536), 64);
-        p.own_parts = (int)min64(fill > even ? fill : even, over(most, BK * p.own_least));
+        p.own_parts = a.prefix_len == 0 && most <= 2 * BK * p.own_least ? 1 : (int)min64(fill > even ? fill : even, over(most, BK * p.own_least));
     }
     return p;
 }
