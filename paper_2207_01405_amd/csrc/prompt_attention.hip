@@ -161,11 +161,12 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void prompt_attention_kernel(PaPar
             for (int r = 0; r < 16; ++r) s[b][r] = 32 * b + 8 * (r / 4) + r % 4 > rel ? -__builtin_inff() : s[b][r];
         softmax_step<T, KB, DT>(s, p, m, l, acc, P.c);
         weighted(p, buf);
-        // A key left out has the weight 0, and 0 times an infinite value or NaN is NaN: where these tiles, which come first, leave a value that is
-        // not finite, they are done again, key by key, with those that count only.
-        if (__builtin_expect(__any(not_finite<DT>(acc)), 0))
-            key_by_key<T, D>(qbase + (int64_t)row * P.ldq, kbase, P.ldk, vbase, P.ldv, k0, limit, P.c, half, m, l, acc, [&](int j) { return (tiles - 1 - j / BK) % KG == g; });
     }
+    // A key left out has the weight 0, and 0 times an infinite value or NaN is NaN: where these tiles, which come first, leave a value that is not finite, they
+    // are done again, key by key, with those that count only.
+    if (__builtin_expect(__any(not_finite<DT>(acc)), 0))
+        key_by_key<T, D>(qbase + (int64_t)row * P.ldq, kbase, P.ldk, vbase, P.ldv, max(tiles - ((odd - 1) * KG + g) - 1, 0) * BK, limit, P.c, half, m, l, acc,
+                         [&](int j) { return (tiles - 1 - j / BK) % KG == g; });
     // The tiles that all queries see.  Scores are formed a tile ahead of the values' product, so that its matrix instructions stand between the vector
     // instructions of the softmax.
     if (odd < rounds) {
