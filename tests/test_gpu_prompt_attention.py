@@ -182,3 +182,43 @@ def test_many_sequences(ivit):
             compare(o[i:i + m], q[i:i + m], k[i:i + m], v[i:i + m], [m], [m], 1, 1, d, True, 0.125, "bf16", "sequence %d" % s)
         i += m
     assert not bool((o == 5).all(1).any())
+
+
+@pytest.mark.parametrize("most", [1, 16, 49, 64, 90, 160])
+def test_many_short_sequences(ivit, most):
+    r = random.Random(most)
+    for H, G, d, t in ((8, 2, 64, "bf16"), (8, 4, 128, "f16"), (7, 1, 128, "bf16")):
+        for causal in (True, False):
+            nq = [r.randint(0, most) for _ in range(47)] + [most]
+            run(ivit, most, nq, nq, H, G, d, causal, t)
+            run(ivit, most, nq, [n + r.choice((0, 1, 31, 32, 33, 100)) for n in nq], H, G, d, causal, t)
+            run(ivit, most, nq, [r.randint(0, 70) for _ in nq], H, G, d, causal, t)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+def test_what_is_left_out_has_no_part_in_short_sequences(ivit, causal):
+    """Rows of one sequence are the keys behind another's last, and keys of NaN and infinite values those that a query does not see."""
+    import torch
+    for d in (64, 128):
+        g = gen(d)
+        lengths, heads = [37, 64, 5, 33] * 20, 4
+        n = sum(lengths)
+        q, k, v = (rand(g, n, heads * d).bfloat16() for _ in range(3))
+        clean, at, bad, first = (k.clone(), v.clone()), 0, [], []
+        for i, m in enumerate(lengths):
+            if i % 2:                                                       # the second half of every other sequence (not causal: all of it)
+                cut = m // 2 if causal else 0
+                k[at + cut:at + m:3], v[at + cut:at + m:2] = math.nan, math.inf
+                bad.append(torch.arange(at + cut, at + m))
+                first += list(range(at, at + cut))
+            else:
+                first += list(range(at, at + m))
+            at += m
+        o, want = torch.empty_like(q), torch.empty_like(q)
+        ivit.ivit_prompt_attention(q, *clean, want, d, starts(lengths), causal=causal)
+        ivit.ivit_prompt_attention(q, k, v, o, d, starts(lengths), causal=causal)
+        assert bool(o[first].isfinite().all())
+        compare(want, q, *clean, lengths, lengths, heads, heads, d, causal, d ** -0.5, "bf16", "%d" % d)
+        # either is off by a rounding of the weights and one of the result, 2^-8 each
+        assert float((o[first].float() - want[first].float()).abs().max()) <= 2.0 ** -6 * float(want.abs().max())
+        assert not bool(o[torch.cat(bad)].reshape(-1, heads * d).isfinite().all(1).any())
