@@ -851,7 +851,7 @@ static int check_cached(const ivit_cache* c, int32_t B, int32_t H, int32_t max_p
     int st;
     if ((st = check_cache(c, row_type >= 0 ? row_type : c->type == IVIT_I8 ? IVIT_BF16 : c->type, &a->c)) != IVIT_OK) return st;
     if (B < 0 || B > 65536 || H < 1 || H > 4096 || c->n_heads > H || H % c->n_heads || prefix_len < 0 || prefix_len > (1 << 30) || max_pages < 0 ||
-        (int64_t)max_pages * c->page_size > (1 << 30) || (int64_t)B * H >= (1 << 24)) return IVIT_ERR_SHAPE;
+        (int64_t)max_pages * c->page_size > (1 << 30) || (int64_t)B * H > (1 << 23)) return IVIT_ERR_SHAPE;
     a->B = B; a->H = H; a->max_pages = max_pages; a->prefix_len = prefix_len;
     return IVIT_OK;
 }

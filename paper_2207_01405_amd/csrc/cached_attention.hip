@@ -581,6 +581,8 @@ Plan plan_of(const CachedArgs& a) {
         p.own_least = items >= 2 * cus ? 4 * LEAST : 2 * items >= cus ? 2 * LEAST : LEAST;
         const int64_t fill = over(4 * cus, items), even = min64(over(most, 1536), 64);
         p.own_parts = a.prefix_len == 0 && most <= 2 * BK * p.own_least ? 1 : (int)min64(fill > even ? fill : even, over(most, BK * p.own_least));
+        // (a launch has less than 2^32 threads; B H <= 2^23 leaves room for one part of both)
+        p.own_parts = max((int)min64(p.own_parts, ((1 << 24) - 1 - (int64_t)p.prefix_tiles * p.prefix_parts * a.c.G) / items), 1);
     }
     return p;
 }

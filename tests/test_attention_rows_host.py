@@ -140,6 +140,19 @@ def test_workspace(lib):
     assert size(lib, B=500, mp=1 << 20) <= 64 * 500 * 4 * (64 + 2) * 4 + 4096
 
 
+def test_very_many_requests(lib):
+    """A workgroup of 256 threads for every key head, 32 query heads and part: less than 2^24 of them fit a launch."""
+    for B, H, heads in ((32768, 256, 256), (65536, 128, 128), (65536, 128, 4), (2048, 4096, 4096), (2048, 4096, 64), (4096, 256, 256)):
+        for prefix in (0, 1 << 20):
+            c = pool(heads=heads, page=16)
+            parts = size(lib, B=B, H=H, c=c, mp=1 << 20, pl=prefix) // (B * H * (64 + 2) * 4)
+            group = H // heads
+            least = (-(-B * group // 128) * heads if prefix else 0) + B * heads * -(-group // 32)          # one part of both
+            assert parts >= 1 and least < 1 << 24
+            assert (parts - (1 if prefix else 0)) * B * heads * -(-group // 32) < 1 << 24, (B, H, heads, prefix, parts)
+        assert size(lib, B=65536, H=129, c=pool(heads=129, page=16)) == 0 and cached(lib, B=65536, H=129, c=pool(heads=129), ldq=129 * 64, ldo=129 * 64) == E["SHAPE"]
+
+
 def test_the_binding_refuses_tensors_that_are_not_as_stated(lib):
     """Wrong types, shapes and strides, and host tensors (all of these are)."""
     import torch
