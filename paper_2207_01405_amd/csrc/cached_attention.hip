@@ -565,7 +565,7 @@ Plan plan_of(const CachedArgs& a) {
     Plan p{0, (group + 31) / 32, 0, 0, LEAST, rows > 64};
     p.prefix_tiles = (int)over(rows, p.wide ? WIDE : 32);
     const int64_t items = (int64_t)a.B * p.own_tiles * a.c.G;
-    if (a.prefix_len > 0) {
+    if (a.prefix_len > 0 && rows > 0) {
         const int full = (int)over(cus, (int64_t)p.prefix_tiles * a.c.G);                                    // parts that are a workgroup a CU
         const bool i8 = a.c.type == TYPE_I8;
         const float chain = a.prefix_len * (p.wide ? a.c.d * (i8 ? 2.66e-4f : 1.33e-4f) : 9e-3f), part = (float)a.B * a.H * a.c.d * (p.wide ? 3.5e-6f : 7e-6f);

@@ -136,6 +136,8 @@ def test_workspace(lib):
     # a part's largest score, sum and output for every head of every request
     assert size(lib) >= 3 * 4 * (64 + 2) * 4
     assert size(lib, pl=1000) > size(lib)
+    # no requests, no pages of their own: valid calls
+    assert 0 < size(lib, B=0) <= 4096 and 0 < size(lib, B=0, pl=1000) <= 4096 and 0 < size(lib, mp=0) and 0 < size(lib, B=0, mp=0) and 0 < size(lib, mp=0, pl=1)
     # of 64 parts of a request's keys at most, however long it may get, where there are many requests
     assert size(lib, B=500, mp=1 << 20) <= 64 * 500 * 4 * (64 + 2) * 4 + 4096
 
