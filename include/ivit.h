@@ -492,7 +492,7 @@ int ivit_gated_quant(void* stream, const void* x, int64_t ldx, int8_t* y, int64_
  *    ones.  Results are rounded once.  Equal calls give equal bits.
  *  - An int8 cache is multiplied in float16: its whole numbers are exact there, bfloat16 queries stand over a power of two of a row's largest
  *    element (what is less than 2^-14 of it loses bits, 2^-25 of it at most), and the weights times the values' scales are rounded to
- *    float16, over the sum of weights that are not rounded.
+ *    float16, each by 2^-11 of itself or 2^-32 of the row's largest such product, over the sum of weights that are not rounded.
  *  - NaN or infinite values that count reach the result as in the formula, but for weights below 2^-126 (where float16 is multiplied: 2^-32) of the largest,
  *    which may count as 0: 0 times an infinite value is NaN.
  *  - A key left out (behind a query, past the end of its sequence) has no part in a result whatever it holds, NaN included; a

@@ -162,7 +162,7 @@ __device__ __forceinline__ void shared_keys(const CaParams& P, int8_t* lds, int 
         c *= query<T, I8>(static_cast<const T*>(P.q) + (int64_t)rb * P.ldq + (int64_t)rh * D + 8 * half, qf);
     }
     v16f acc[DT];
-    float m = -__builtin_inff(), l = 0.0f, ref = 0.0f;
+    float m = -__builtin_inff(), l = 0.0f, ref = kRefLeast;
 #pragma unroll
     for (int i = 0; i < DT; ++i) acc[i] = v16f{};
     auto scale_at = [&](int buf, int b, int r) __attribute__((always_inline)) {        // of the keys; 16 further on: of the values
@@ -220,7 +220,7 @@ __device__ __forceinline__ void shared_keys(const CaParams& P, int8_t* lds, int 
                 float vs[16];
 #pragma unroll
                 for (int r = 0; r < 16; ++r) vs[r] = *reinterpret_cast<const float*>(scale_at(buf, b, r) + 64);
-                softmax_step_scaled<DT>(one, p[b], m, l, acc, c, ref, n == 0 && b == 0, vs);
+                softmax_step_scaled<DT>(one, p[b], m, l, acc, c, ref, vs);
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -253,7 +253,7 @@ __device__ __forceinline__ void shared_keys(const CaParams& P, int8_t* lds, int 
     // results as whole lines: a lane's registers into LDS of the wavefront's own, and out of it 4 elements of row lane / 8 + 8 n at 4 (lane % 8)
     __syncthreads();
     float* const out = reinterpret_cast<float*>(lds + wv * TL::WAVE);
-    const float up = I8 ? __builtin_amdgcn_exp2f(ref) : 1.0f;
+    const float up = I8 ? __builtin_amdgcn_exp2f(ref - 15.0f) : 1.0f;
 #pragma unroll
     for (int i = 0; i < DT; ++i)
 #pragma unroll
@@ -382,7 +382,7 @@ __global__ __launch_bounds__(64 * W, 2) void cached_attention_kernel(CaParams P)
     // (here, where all loads so far are waited for: the waits in the loop count its own ones)
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     v16f acc[DT];
-    float m = -__builtin_inff(), l = 0.0f, ref = 0.0f;
+    float m = -__builtin_inff(), l = 0.0f, ref = kRefLeast;
 #pragma unroll
     for (int i = 0; i < DT; ++i) acc[i] = v16f{};
 
@@ -424,8 +424,7 @@ __global__ __launch_bounds__(64 * W, 2) void cached_attention_kernel(CaParams P)
         }
         V8 p[1][2];
         if constexpr (I8) {
-            // Weights times the values' scales, over 2^ref: what float16 holds goes by the largest scale so far.
-            softmax_step_scaled<DT>(s, p[0], m, l, acc, c, ref, n == 0, vs);
+            softmax_step_scaled<DT>(s, p[0], m, l, acc, c, ref, vs);
         } else {
             softmax_step<T, 1, DT>(s, p, m, l, acc, c);
         }
@@ -449,7 +448,7 @@ __global__ __launch_bounds__(64 * W, 2) void cached_attention_kernel(CaParams P)
 
     // The wavefronts' parts: largest scores and sums, then the outputs, a lane's registers to the same lane; a wavefront joins every fourth tile of 32 elements.
     if (half == 0) { join_m[wv][li] = m; join_l[wv][li] = l; }
-    const float up = I8 ? __builtin_amdgcn_exp2f(ref) : 1.0f;
+    const float up = I8 ? __builtin_amdgcn_exp2f(ref - 15.0f) : 1.0f;
     float* const out = reinterpret_cast<float*>(mine) + lane;
 #pragma unroll
     for (int i = 0; i < DT; ++i)

@@ -101,35 +101,42 @@ __device__ __forceinline__ void softmax_step(const v16f (&s)[KB], typename Elem<
         for (int r = 0; r < 16; r += 2) weigh<T>(s[b], r, p[b], l, c, base);
 }
 
-// The same over 16 scores, for values of int8 rows: the weights that leave are times the values' scales over 2^ref, ref following
-// the largest scale of the block, the same for all lanes; the sum is that of the weights alone.  The output is in units of 2^ref.
+// The same over 16 scores, for values of int8 rows: what leaves are weights times the values' scales, in float16 and in units of 2^(ref - 15), as the output is; the sum
+// is that of the weights alone.  ref is a query's own and goes by the largest product so far, not by the largest scale (a key of next to no weight and large
+// values would push those that count below float16's numbers): products of less than 2^ref are less than 2^15, the largest is 2^7 at least when ref is set, so a product is off by
+// 2^-11 of itself or by 2^-32 of the largest.  ref falls as the weights do that a new largest score leaves to what came before.
+constexpr float kRefLeast = -110.0f;                                    // (2^(15 - ref) and 2^(ref - 15) are normal numbers; ref starts here)
 template <int DT>
 __device__ __forceinline__ void softmax_step_scaled(const v16f (&s)[1], Elem<_Float16>::v8 (&p)[2], float& m, float& l, v16f (&acc)[DT], float c, float& ref,
-                                                    bool first, const float (&scale)[16]) {
+                                                    const float (&scale)[16]) {
     const float top = largest_of(s);
-    float largest = 0.0f;                                               // (a NaN among them leaves the others)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) largest = __builtin_fmaxf(largest, scale[r]);
-    largest = __builtin_fmaxf(largest, __shfl_xor(largest, 32));
-    const float power = __builtin_fminf(__builtin_fmaxf(__builtin_ceilf(__builtin_amdgcn_logf(largest)), -120.0f), 120.0f);
-    if (__builtin_expect(__any((top - m) * c > 8.0f) || first || power > ref, 0)) {
-        const float to = (top - m) * c > 8.0f ? top : m, by = first ? power : __builtin_fmaxf(power, ref);
-        const float f = to > m ? __builtin_amdgcn_exp2f((m - to) * c) : 1.0f, g = f * __builtin_amdgcn_exp2f(ref - by);
-        m = to;
-        l *= f;
-        ref = by;
-#pragma unroll
-        for (int i = 0; i < DT; ++i)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) acc[i][r] *= g;
-    }
-    const float base = Elem<_Float16>::kUp - (m == -__builtin_inff() ? 0.0f : m * c), down = __builtin_amdgcn_exp2f(-ref);
+    const bool moves = (top - m) * c > 8.0f;                            // (as in move_largest)
+    const float down = moves ? (m - top) * c : 0.0f;                    // what came before is to be multiplied by 2^down
+    m = moves ? top : m;
+    l *= __builtin_amdgcn_exp2f(down);
+    const float base = m == -__builtin_inff() ? 0.0f : -(m * c);
+    float t[16], largest = 0x1p-118f;                                   // (a NaN among them leaves the others)
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
         const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[0][r], c, base));
         l += w;
-        p[r / 8][r % 8] = (_Float16)(w * (scale[r] * down));
+        t[r] = w * scale[r];
+        largest = __builtin_fmaxf(largest, t[r]);
     }
+    const float most = __builtin_fminf(max_halves(largest), 0x1p121f);
+    const float power = (float)__builtin_amdgcn_frexp_expf(most);       // products are less than 2^power
+    if (__builtin_expect(__any(moves || power > ref), 0)) {
+        const float to = moves || power > ref ? __builtin_fmaxf(power + 7.0f, __builtin_floorf(ref + down)) : ref;
+        const float f = __builtin_amdgcn_exp2f(down + (ref - to));
+        ref = to;
+#pragma unroll
+        for (int i = 0; i < DT; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][r] *= f;
+    }
+    const float unit = __builtin_amdgcn_exp2f(15.0f - ref);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) p[r / 8][r % 8] = (_Float16)(t[r] * unit);
 }
 
 template <int DT> __device__ __forceinline__ bool not_finite(const v16f (&acc)[DT]) {
