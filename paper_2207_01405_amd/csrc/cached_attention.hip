@@ -11,8 +11,7 @@
 // quarter an element, which bounds these caches (to bfloat16, which has no place for eight bits under a leading one, they were three, and 48 requests of 8192 keys took
 // 177 us for 163).  bfloat16 queries become float16 with a power of two of their own, which their scores get back.  The keys' scales go to the
 // scores, the values' to the weights.
-#include <cmath>
-
+#include "cached_form.hpp"
 #include "regst_common.hpp"
 #include "float_attention.hpp"
 
@@ -21,16 +20,14 @@ namespace {
 
 using namespace regst;
 using namespace fatt;
+using namespace cached;
 
 typedef float v4f __attribute__((ext_vector_type(4)));
-
-constexpr int W = 4, BK = 32, LEAST = 2 * W;   // wavefronts; keys of a block; blocks of the smallest part
-constexpr int WIDE = 32 * W, TK = 16 * W;      // rows of a workgroup that shares its keys, keys of its tiles
 
 struct CaParams {
     const void* q; void* o; const int8_t *k, *v; const float *ks, *vs; const int32_t *prefix_pages, *pages, *lens; float *ml, *part;
     int64_t ldq, ldo, ld_pages, ld_page;       // ld_page in bytes
-    int prefix_len, max_len, B, H, G, group, page_shift, n_pages, prefix_parts, own_parts, own_least, prefix_tiles, wide; float c;
+    int prefix_len, max_len, B, H, G, group, page_shift, n_pages, prefix_parts, own_parts, prefix_least, own_least, prefix_tiles, wide; float c;
     FastDiv by_head, by_prefix_part, by_own_part, by_own_tile, by_group, by_heads;
 };
 
@@ -293,13 +290,13 @@ __global__ __launch_bounds__(64 * W, 2) void cached_attention_kernel(CaParams P)
     uint32_t g_, part_;
     const uint32_t item = P.by_head.divide(blockIdx.x, g_), prefix_items = (uint32_t)(P.prefix_tiles * P.prefix_parts);
     const int g = (int)g_;
-    int b = 0, r0, rows, len, parts, least = LEAST;
+    int b = 0, r0, rows, len, parts, least;
     const bool prefix = item < prefix_items;
     const int32_t* table;
     if (prefix) {
         r0 = (P.wide ? WIDE : 32) * (int)P.by_prefix_part.divide(item, part_);
         rows = P.B * P.group;
-        len = P.prefix_len; parts = P.prefix_parts; table = P.prefix_pages;
+        len = P.prefix_len; parts = P.prefix_parts; least = P.prefix_least; table = P.prefix_pages;
     } else {
         uint32_t t;
         b = (int)P.by_own_tile.divide(P.by_own_part.divide(item - prefix_items, part_), t);
@@ -546,44 +543,8 @@ template <class T, int D, int AT_ONCE> __global__ __launch_bounds__(256) void jo
     for (int e = 0; e < E; ++e) o[e] = (T)(val[e] * inv);
 }
 
-// Parts.  Requests: of the greatest length, four workgroups a CU and 1536 keys a part at most, so that requests of different lengths leave no CU waiting (48 of
-// up to 16384 int8 keys 172 us, in parts of 5461 keys 195); shorter ones in as many, of `least` keys at least, which are fewer where there are few requests.  Without
-// a prefix twice as many are one part, which is one launch (1 request of 500, 32 heads of 128 on 8: 9.0 -> 8.7 us, with the host 11.5 -> 9.0; 32 of 1000 30.6 -> 27.9).
-// The prefix: n parts take about  max(own, chain / n + own / 2) + n part  us.  chain: all its keys by one workgroup, 9 ns a key, or 17 for elements of 128 (34 of int8
-// rows) where a wavefront has rows of its own; own: the requests' own keys from memory, beside which a workgroup of the prefix gets on half as fast; part: writing
-// and reading the rows of a part.  `own` is known for the greatest length only, and counts up to 40 us.  Where the prefix's workgroups take more than three
-// quarters of the CUs, the requests' take a quarter longer.  Heads of 128, 32 on 8, in us with one part / these / the best number: 64 requests behind 1000 keys
-// 28.9 / 17.4 / 17.4, behind 8000 with up to 600 of their own 155 / 42 / 41, 256 behind 16000 291 / 97 / 97, 128 behind 8000 with 1200 of their own 207 / 136 / 125.
-struct Plan { int prefix_tiles, own_tiles, prefix_parts, own_parts, own_least; bool wide; };
-
 Plan plan_of(const CachedArgs& a) {
-    const int group = a.H / a.c.G;
-    const int64_t cus = num_cus(), most = (int64_t)a.max_pages * a.c.page_size;
-    auto over = [](int64_t n, int64_t d) { return (n + d - 1) / d; };
-    const int64_t rows = (int64_t)a.B * group;
-    Plan p{0, (group + 31) / 32, 0, 0, LEAST, rows > 64};
-    p.prefix_tiles = (int)over(rows, p.wide ? WIDE : 32);
-    const int64_t items = (int64_t)a.B * p.own_tiles * a.c.G;
-    if (a.prefix_len > 0 && rows > 0) {
-        const int full = (int)over(cus, (int64_t)p.prefix_tiles * a.c.G);                                    // parts that are a workgroup a CU
-        const bool i8 = a.c.type == TYPE_I8;
-        const float chain = a.prefix_len * (p.wide ? a.c.d * (i8 ? 2.66e-4f : 1.33e-4f) : 9e-3f), part = (float)a.B * a.H * a.c.d * (p.wide ? 3.5e-6f : 7e-6f);
-        const float own = std::fmin((float)a.B * most * a.c.G * a.c.d * (i8 ? 4e-7f : 8e-7f), 40.0f), root = std::sqrt(chain / part);
-        auto takes = [&](int n) { return std::fmax(own, chain / n + own / 2) + part * n; };
-        const float best = std::fmax(own * root > 2 * chain ? 2 * chain / own : root, 1.0f);               // where it is least
-        const int most_parts = (int)min64(full, over(a.prefix_len, BK * (p.wide ? W : LEAST))), fewer = max(3 * full / 4, 1);
-        int n = best < most_parts ? (int)best : most_parts;
-        if (n < most_parts && takes(n + 1) < takes(n)) ++n;
-        p.prefix_parts = n > fewer && takes(fewer) < takes(n) + own / 4 ? fewer : n;
-    }
-    if (most > 0 && items > 0) {
-        p.own_least = items >= 2 * cus ? 4 * LEAST : 2 * items >= cus ? 2 * LEAST : LEAST;
-        const int64_t fill = over(4 * cus, items), even = min64(over(most, 1536), 64);
-        p.own_parts = a.prefix_len == 0 && most <= 2 * BK * p.own_least ? 1 : (int)min64(fill > even ? fill : even, over(most, BK * p.own_least));
-        // (a launch has less than 2^32 threads; B H <= 2^23 leaves room for one part of both)
-        p.own_parts = max((int)min64(p.own_parts, ((1 << 24) - 1 - (int64_t)p.prefix_tiles * p.prefix_parts * a.c.G) / items), 1);
-    }
-    return p;
+    return cached::plan_of(a.B, a.H, a.c.G, a.c.d, a.c.type == TYPE_I8, a.c.page_size, a.max_pages, a.prefix_len, num_cus());
 }
 size_t ml_bytes(const CachedArgs& a, int parts) { return ((size_t)parts * a.B * a.H * 8 + 255) & ~(size_t)255; }
 
@@ -595,7 +556,7 @@ template <class T, int D, bool I8> hipError_t launch(hipStream_t s, const Cached
     const CaParams P{a.q, a.o, static_cast<const int8_t*>(a.c.k), static_cast<const int8_t*>(a.c.v), a.c.k_scale, a.c.v_scale, a.prefix_pages, a.pages, a.lens,
                      ml, reinterpret_cast<float*>(static_cast<int8_t*>(a.workspace) + ml_bytes(a, parts)), a.ldq, a.ldo, a.ld_pages,
                      a.c.ld_page * (I8 ? 1 : 2), a.prefix_len, a.max_pages * a.c.page_size, a.B, a.H, a.c.G, a.H / a.c.G, __builtin_ctz(a.c.page_size), a.c.n_pages,
-                     p.prefix_parts, p.own_parts, p.own_least, p.prefix_tiles, p.wide, a.scale * 1.44269504088896341f,
+                     p.prefix_parts, p.own_parts, p.prefix_least, p.own_least, p.prefix_tiles, p.wide, a.scale * 1.44269504088896341f,
                      div(a.c.G), div(p.prefix_parts), div(p.own_parts), div(p.own_tiles), div(a.H / a.c.G), div(a.H)};
     const int64_t items = ((int64_t)p.prefix_tiles * p.prefix_parts + (int64_t)a.B * p.own_tiles * p.own_parts) * a.c.G;
     const int64_t keys = a.prefix_len + (int64_t)a.B * a.max_pages * a.c.page_size;
