@@ -62,3 +62,10 @@ def test_every_part_has_keys_at_the_greatest_length(plan):
         p = plan(B, H, G, r.choice((64, 128)), prefix, keys, r.random() < 0.5)
         assert (p["prefix_parts"] > 0) == (prefix > 0) and (p["own_parts"] > 0) == (keys > 0)
         check(p, prefix, keys, (B, H, G, prefix, keys))
+
+
+def test_more_than_64_parts(plan):
+    """What the tests of the join go by: one request with a table of 32768 keys and 8 key heads, and a prefix before it."""
+    assert plan(1, 32, 8, 128, 0, 33024)["own_parts"] > 64 and plan(1, 32, 8, 128, 20000, 20032)["own_parts"] > 64
+    p = plan(1, 32, 8, 128, 9000, 13056)
+    assert p["prefix_parts"] < 64 and p["own_parts"] < 64 and p["prefix_parts"] + p["own_parts"] > 64
