@@ -7,8 +7,9 @@
 // of a wavefront joins the maximum), and its registers, rounded and packed, are as they stand the "B" operand of the second product, values x queries:
 // that product sums over keys, in any order that both operands agree on, and the values' fragments come by the transposing LDS read in the order
 // in which the scores' registers hold the keys.
-#include "regst_common.hpp"
 #include "float_attention.hpp"
+#include "prompt_form.hpp"
+#include "regst_common.hpp"
 
 namespace ivit {
 namespace {
@@ -260,19 +261,13 @@ template <class T, int D, int RW, int KG, int BK> hipError_t launch(hipStream_t 
     prompt_attention_kernel<T, D, RW, KG, BK><<<dim3((unsigned)units), 64 * RW * KG, 0, s>>>(P);
     return hipGetLastError();
 }
-// Where 128 rows a workgroup leave CUs without one (taking the sequences for equally long), the keys are shared out inside a workgroup: 500 queries after 7500
-// keys, 32 heads of 128, are 128 such workgroups, 128 us; two groups of 128 rows 106, four of 64 rows 88.  1000 after 7000: 140, 130, 155; 1500 after
-// 7000: 213, 226, 237.
-// Short sequences: 64 rows and tiles of 32 keys, four workgroups a CU, leave fewer rows empty and more loads in flight.  16384 rows, 32 heads of 128 on 8, causal, in
-// sequences of 16, 49, 64, 100, 160, 197, 300, 512: 155, 83, 75, 90, 92, 107, 104, 129 us (128 rows 310, 120, 101, 93, 111, 109, 115, 123); not causal 64, 100, 128, 160, 197:
-// 77, 102, 90, 106, 131 (103, 98, 88, 123, 127); 12 heads of 64, causal, 49, 160, 300: 21, 27, 34 (30, 28, 30).  Of different lengths, 55, 106, 199, 261, 358 on average:
-// 57, 54, 59, 67, 74 (74, 62, 61, 68, 72), not causal 59, 61, 76, 93, 103 (70, 67, 73, 89, 97).
 template <class T, int D> hipError_t choose(hipStream_t s, const PromptArgs& a) {
-    const int64_t blocks = (int64_t)a.n_seq * ((a.n_q + 128 * (int64_t)a.n_seq - 1) / (128 * (int64_t)a.n_seq)) * a.H, cus = num_cus();
-    if (2 * blocks <= cus) return launch<T, D, 2, 4, 32>(s, a);
-    if (a.n_q <= (a.causal ? 200 : 128) * (int64_t)a.n_seq) return launch<T, D, 2, 1, 32>(s, a);
-    if (blocks <= cus) return launch<T, D, 4, 2, 64>(s, a);
-    return launch<T, D, 4, 1, 64>(s, a);
+    switch (prompt::form_of(a.n_q, a.n_seq, a.H, a.causal, num_cus())) {
+        case prompt::R64X4_K32: return launch<T, D, 2, 4, 32>(s, a);
+        case prompt::R64_K32: return launch<T, D, 2, 1, 32>(s, a);
+        case prompt::R128X2_K64: return launch<T, D, 4, 2, 64>(s, a);
+        default: return launch<T, D, 4, 1, 64>(s, a);
+    }
 }
 
 }  // namespace
