@@ -549,7 +549,7 @@ int ivit_cache_append(void* stream, const void* q, int64_t ldq, void* q_out, int
  * q_start).  causal != 0: query i of n sees keys j <= i + (m - n) of m, so that the last query sees all (the first ones, where there
  * are fewer keys than queries, none).
  * q, o [n_q, H * d], k, v [n_k, G * d] of `type`; starts int32 [n_seq + 1] (device), not falling; a sequence that is not within the
- * rows is left out.  scale > 0 and finite.  No overlap.
+ * rows is left out.  scale > 0, at most 2^127.  No overlap.
  * Requirements: 0 <= n_q, n_k <= 2^30, 0 <= n_seq < 2^20, H and G <= 4096, (n_q / 64 + n_seq) H < 2^24; ldq, ldk, ldv <= 2^24; leading dimensions and
  * pointers of q, k, v, o whole 16 bytes.
  * Errors: NULL, SHAPE, PARAM (type, scale), ALIGN, HIP. */
@@ -564,7 +564,7 @@ int ivit_prompt_attention(void* stream, const void* q, int64_t ldq, const void* 
  * q, o [B, H * d] of `type`; the cache of `type` or IVIT_I8; pages int32 [B, max_pages], lens int32 [B], prefix_pages int32
  * [ceil(prefix_len / page_size)] (device; NULL where empty).  Graphs that may run at the same time need a workspace each; it holds nothing
  * between calls.
- * Requirements: 0 <= B <= 65536, H <= 4096, B H <= 2^23, 0 <= prefix_len <= 2^30, max_pages * page_size <= 2^30; leading dimensions and pointers of q and o whole
+ * Requirements: scale > 0, at most 2^127, 0 <= B <= 65536, H <= 4096, B H <= 2^23, 0 <= prefix_len <= 2^30, max_pages * page_size <= 2^30; leading dimensions and pointers of q and o whole
  * 16 bytes; workspace 256-byte aligned, at least ivit_cached_attention_workspace_bytes (0 for arguments that the call refuses).
  * Errors: NULL, SHAPE, PARAM (types, scale), ALIGN, WORKSPACE, HIP. */
 size_t ivit_cached_attention_workspace_bytes(int32_t B, int32_t H, const ivit_cache* c, int32_t max_pages, int32_t prefix_len);

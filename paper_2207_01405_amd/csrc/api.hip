@@ -758,6 +758,9 @@ int ivit_gated_quant(void* stream, const void* x, int64_t ldx, int8_t* y, int64_
 
 static bool whole16(const void* p, int64_t ld, int type) { return aligned(p, 16) && (ld * ivit::element_bytes(type)) % 16 == 0; }
 
+// Scores enter powers of two with scale log2 e, which has to be finite: infinity times a score of 0 is NaN.
+static bool right_scale(float scale) { return scale > 0.0f && std::isfinite(scale * 1.44269504088896341f); }
+
 // Rows that attention reads or writes 16 bytes at a time.
 static int check_wide_rows(const void* p, int64_t ld, int64_t cols, int type) {
     const int st = check_rows(p, ld, cols, type);
@@ -831,7 +834,7 @@ int ivit_cache_append(void* stream, const void* q, int64_t ldq, void* q_out, int
 int ivit_prompt_attention(void* stream, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, void* o, int64_t ldo,
                           const int32_t* q_start, const int32_t* k_start, int32_t n_seq, int64_t n_q, int64_t n_k, int32_t H, int32_t G, int32_t d,
                           int32_t type, float scale, int32_t causal) {
-    if ((type != IVIT_F16 && type != IVIT_BF16) || !std::isfinite(scale) || !(scale > 0.0f)) return IVIT_ERR_PARAM;
+    if ((type != IVIT_F16 && type != IVIT_BF16) || !right_scale(scale)) return IVIT_ERR_PARAM;
     if (n_q < 0 || n_q > (1 << 30) || n_k < 0 || n_k > (1 << 30) || n_seq < 0 || n_seq >= (1 << 20) || (d != 64 && d != 128)) return IVIT_ERR_SHAPE;
     if (H < 1 || H > 4096 || G < 1 || G > H || H % G || (!k_start && n_q != n_k) || (n_q / 64 + n_seq) * H >= (1 << 24)) return IVIT_ERR_SHAPE;
     if (ldq > (1 << 24) || (n_k > 0 && (ldk > (1 << 24) || ldv > (1 << 24)))) return IVIT_ERR_SHAPE;
@@ -864,7 +867,7 @@ size_t ivit_cached_attention_workspace_bytes(int32_t B, int32_t H, const ivit_ca
 int ivit_cached_attention(void* stream, const void* q, int64_t ldq, void* o, int64_t ldo, const ivit_cache* c, const int32_t* prefix_pages,
                           int32_t prefix_len, const int32_t* pages, int64_t ld_pages, int32_t max_pages, const int32_t* lens, int32_t B, int32_t H,
                           int32_t type, float scale, void* workspace, size_t workspace_bytes) {
-    if ((type != IVIT_F16 && type != IVIT_BF16) || !std::isfinite(scale) || !(scale > 0.0f)) return IVIT_ERR_PARAM;
+    if ((type != IVIT_F16 && type != IVIT_BF16) || !right_scale(scale)) return IVIT_ERR_PARAM;
     ivit::CachedArgs a{};
     int st;
     if ((st = check_cached(c, B, H, max_pages, prefix_len, type, &a)) != IVIT_OK) return st;
