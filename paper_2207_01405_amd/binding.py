@@ -729,6 +729,8 @@ def _whole_numbers(t, shape, device, where):
 def rotary_params(r, rows, device, where="rotary_params"):
     """RotaryParams from a dict: positions int32 [rows] or [axes, rows]; freq float64 [rotary_dim / 2], radians a step; axis int32
     [rotary_dim / 2] or absent; adjacent: pairs (2 i, 2 i + 1) in place of (i, i + rotary_dim / 2)."""
+    if _TYPES is None:
+        _setup()
     pos, freq, axis = r["positions"], r["freq"], r.get("axis")
     shape = pos.shape
     axes = shape[0] if len(shape) == 2 else 1

@@ -16,3 +16,17 @@ def test_a_scale_beyond_the_range_of_its_exponents(lib):
         assert cached(lib, scale=scale, c=pool(t=I8, ks=FAKE, vs=FAKE)) == E["PARAM"]
     for scale in (most * 0.9999, 1.0e-38, 1.4e-45):
         assert prompt(lib, scale=scale, nq=0, nk=0, q=None, o=None) == 0 and cached(lib, scale=scale, B=0) == 0
+
+
+def test_the_structures_alone_before_any_call(monkeypatch):
+    """rotary_params and cache_struct take tensors before another call of the binding has looked up torch's types."""
+    import torch
+    for name in ("_TYPES", "_INT8", "_INT32", "_FLOAT32", "_FLOAT64"):
+        monkeypatch.setattr(binding, name, None)
+    r = binding.rotary_params({"positions": torch.zeros(4, dtype=torch.int32), "freq": torch.ones(32, dtype=torch.float64)}, 4, -1)
+    assert r.n_axes == 1 and r.rotary_dim == 64
+    for name in ("_TYPES", "_INT8", "_INT32", "_FLOAT32", "_FLOAT64"):
+        monkeypatch.setattr(binding, name, None)
+    c = {n: torch.zeros(2, 1, 16, 64, dtype=torch.int8) for n in "kv"}
+    c.update({n + "_scale": torch.zeros(2, 1, 16) for n in "kv"})
+    assert binding.cache_struct(c, -1).n_pages == 2
