@@ -734,8 +734,10 @@ def rotary_params(r, rows, device, where="rotary_params"):
     pos, freq, axis = r["positions"], r["freq"], r.get("axis")
     shape = pos.shape
     axes = shape[0] if len(shape) == 2 else 1
-    if len(shape) not in (1, 2) or shape[-1] != rows or pos.dtype is not _INT32 or pos.get_device() != device or (rows > 1 and pos.stride(-1) != 1):
-        raise ValueError("%s: positions %s of %s on %s, wanted int32 [%d] or [axes, %d] on device %d" % (where, tuple(shape), pos.dtype, pos.device, rows, rows, device))
+    if (len(shape) not in (1, 2) or shape[-1] != rows or pos.dtype is not _INT32 or pos.get_device() != device or (rows > 1 and pos.stride(-1) != 1) or
+            (axes > 1 and pos.stride(0) < rows)):
+        raise ValueError("%s: positions %s of %s with strides %s on %s, wanted int32 [%d] or [axes, %d], each axis dense and apart, on device %d" % (
+            where, tuple(shape), pos.dtype, pos.stride(), pos.device, rows, rows, device))
     if freq.dim() != 1 or freq.dtype is not _FLOAT64 or freq.get_device() != device or not freq.is_contiguous():
         raise ValueError("%s: freq has to be dense float64 [rotary_dim / 2] on device %d" % (where, device))
     half = freq.shape[0]

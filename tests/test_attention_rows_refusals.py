@@ -30,3 +30,18 @@ def test_the_structures_alone_before_any_call(monkeypatch):
     c = {n: torch.zeros(2, 1, 16, 64, dtype=torch.int8) for n in "kv"}
     c.update({n + "_scale": torch.zeros(2, 1, 16) for n in "kv"})
     assert binding.cache_struct(c, -1).n_pages == 2
+
+
+def test_positions_expanded_over_their_axes_and_other_strides():
+    """The binding names what is wrong, as for every other tensor, in place of the C call's status; tensors here are on the host, which is device -1."""
+    import torch
+    freq = torch.ones(32, dtype=torch.float64)
+    one = torch.zeros(1, 4, dtype=torch.int32)
+    for pos in (one.expand(3, 4), torch.zeros(4, 3, dtype=torch.int32).t(), torch.zeros(9, dtype=torch.int32).as_strided((3, 4), (2, 1))):
+        with pytest.raises(ValueError, match="positions"):
+            binding.rotary_params({"positions": pos, "freq": freq}, 4, -1)
+    for pos in (one, one[0], torch.zeros(3, 4, dtype=torch.int32), torch.zeros(3, 9, dtype=torch.int32)[:, 2:6], one.expand(1, 4)):
+        r = binding.rotary_params({"positions": pos, "freq": freq}, 4, -1)
+        assert r.ld_positions >= 4 and r.n_axes == (pos.shape[0] if pos.dim() == 2 else 1)
+    r = binding.rotary_params({"positions": torch.zeros(3, 1, dtype=torch.int32), "freq": freq}, 1, -1)
+    assert r.ld_positions == 1 and r.n_axes == 3
