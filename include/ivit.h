@@ -487,9 +487,10 @@ int ivit_gated_quant(void* stream, const void* x, int64_t ldx, int8_t* y, int64_
  *    G: query head h reads key head h / (H / G).
  *  - Rows, leading dimensions and alignment as in the section above, unless stated.  Rows and caches of attention are float16
  *    or bfloat16, its head size d 64 or 128.
- *  - Scores, the statistics of softmax and sums of values are held in 32 bits; q . k, scale q . k and the results have to lie within float32.
- *    Weights are rounded to the rows' type where the matrix cores multiply them with the values, and divided by the sum of the rounded
- *    ones.  Results are rounded once.  Equal calls give equal bits.
+ *  - Scores, the statistics of softmax and sums of values are held in 32 bits; q . k, 2 scale q . k (over an int8 cache 4 scale |q| too) and 2^9 times
+ *    the sum of a row's |v| have to lie within float32.  Weights are rounded to the rows' type where the matrix cores multiply them with the
+ *    values (float16: by 2^-11 of themselves or 2^-32 of the largest), and divided by the sum of the rounded ones.  Results are rounded once.  Equal calls
+ *    give equal bits.
  *  - An int8 cache is multiplied in float16: its whole numbers are exact there, bfloat16 queries stand over a power of two of a row's largest
  *    element (what is less than 2^-14 of it loses bits, 2^-25 of it at most), and the weights times the values' scales are rounded to
  *    float16, each by 2^-11 of itself or 2^-32 of the row's largest such product, over the sum of weights that are not rounded.
@@ -564,8 +565,8 @@ int ivit_prompt_attention(void* stream, const void* q, int64_t ldq, const void* 
  * q, o [B, H * d] of `type`; the cache of `type` or IVIT_I8; pages int32 [B, max_pages], lens int32 [B], prefix_pages int32
  * [ceil(prefix_len / page_size)] (device; NULL where empty).  Graphs that may run at the same time need a workspace each; it holds nothing
  * between calls.
- * Requirements: scale > 0, at most 2^127, 0 <= B <= 65536, H <= 4096, B H <= 2^23, 0 <= prefix_len <= 2^30, max_pages * page_size <= 2^30; leading dimensions and pointers of q and o whole
- * 16 bytes; workspace 256-byte aligned, at least ivit_cached_attention_workspace_bytes (0 for arguments that the call refuses).
+ * Requirements: scale > 0, at most 2^127; 0 <= B <= 65536, H <= 4096, B H <= 2^23, 0 <= prefix_len <= 2^30, max_pages * page_size <= 2^30; leading dimensions
+ * and pointers of q and o whole 16 bytes; workspace 256-byte aligned, at least ivit_cached_attention_workspace_bytes (0 for arguments that the call refuses).
  * Errors: NULL, SHAPE, PARAM (types, scale), ALIGN, WORKSPACE, HIP. */
 size_t ivit_cached_attention_workspace_bytes(int32_t B, int32_t H, const ivit_cache* c, int32_t max_pages, int32_t prefix_len);
 int ivit_cached_attention(void* stream, const void* q, int64_t ldq, void* o, int64_t ldo, const ivit_cache* c,
